@@ -287,6 +287,126 @@ qnn_status qnn_quantize_matrix_static(const float *x, int64_t rows, int64_t cols
                                       void *stream);
 
 /* ---------------------------------------------------------------------------------------------
+ * Selective state-space layers on 8-bit activations. The paper's layers are fully connected and LSTM ones; these calls
+ * apply its quantization scheme (activations on the fly, one unit per row; weights offline, in units of sub-matrices) to a
+ * layer whose state update is element-wise:
+ *   qnn_rmsnorm_quantize -> qnn_qmatmul4 (or qnn_qmatmul) -> qnn_causal_conv -> qnn_ssm_scan -> qnn_quantize -> a product.
+ * For these calls device pointers have to belong to the current device (or be managed memory), and an output may not
+ * overlap an input unless a call allows it; QNN_ERR_INVALID_ARG otherwise, before anything runs. They allocate nothing and
+ * may be captured into a graph.
+ * ------------------------------------------------------------------------------------------- */
+
+/* Types of the values that pass between layers. All arithmetic is fp32 or wider, each output rounded once. */
+typedef enum { QNN_F32 = 0, QNN_BF16 = 1, QNN_F16 = 2 } qnn_dtype;
+
+/*
+ * qnn_rmsnorm_quantize — residual addition, root-mean-square norm and the on-the-fly quantizer (Sec. 3, eq. 2) in one pass.
+ *   x, residual   [rows x cols] of `dtype` (leading dimensions ldx, ldr >= cols); residual nullable.
+ *   residual_out  [rows x cols] of `dtype` (ldh >= cols), nullable: h = x + residual (fp32), rounded once. It may be x or
+ *                 residual itself (same pointer and leading dimension).
+ *   weight        [cols] fp32. eps: 1e-20 .. 1e20.
+ *   codes, params, code_sums  as qnn_quantize with QNN_PER_ROW gives them for the fp32 rows
+ *                 v = (h s) weight, s = 1 / sqrt(sum h^2 / cols + eps); code_sums nullable.
+ *   values        [rows x cols] fp32 (ldv >= cols), nullable: the values that the codes stand for, (code + z) / Q (eq. 3),
+ *                 for consumers in float (the "quant" output layer of Sec. 5).
+ * The codes are defined to the bit: the norm is taken of h before it is rounded to `dtype`; s is computed to about 2^-45
+ * relative and rounded once to fp32; h s and its product with the weight are each rounded once to fp32.
+ * 1 <= cols <= 2^24. A row with a value of v that is not finite: its codes and values are unspecified and QNN_ERR_NONFINITE
+ * is recorded, as for qnn_quantize (h is stored all the same).
+ */
+qnn_status qnn_rmsnorm_quantize(const void *x, int64_t ldx, const void *residual, int64_t ldr, int dtype,
+                                const float *weight, double eps, int64_t rows, int64_t cols, void *residual_out,
+                                int64_t ldh, uint8_t *codes, int64_t ldc, qnn_qparams *params, int32_t *code_sums,
+                                float *values, int64_t ldv, void *stream);
+
+/*
+ * qnn_quantize4 — weights to 4-bit codes, offline: eq. (2) with S = 15 on sub-matrices (Sec. 3.1) of `group` (32, 64 or
+ * 128) consecutive weights of a row, the last of a row perhaps shorter.
+ *   w          [N x K] fp32, leading dimension ldw >= K.
+ *   Per unit, the range taken to include 0: scale = (max / 15 - min / 15) rounded up to bf16, offset = round(min / scale)
+ *   (-15 .. 0), code = clamp(round(w / scale) - offset, 0, 15); a code stands for (code + offset) scale, at most half a
+ *   scale from w. A unit of zeros has scale 0. The least scale is 2^-126.
+ *   codes      [ceil(N/16)][ceil(K/128)][1024] bytes: tiles of 16 rows x 128 columns. Row 8 h + g and column
+ *              32 j + 8 t + e of a tile are in the four bytes from 512 h + 64 g + 16 t + 4 j on, whose eight halves,
+ *              low ones first, hold e = 0 2 4 6 1 3 5 7. Rows and columns past the matrix have code 0.
+ *   units      [ceil(N/16)][ceil(K/128)][16][128 / group] entries: bf16 offset in the low half, bf16 scale in the high
+ *              half; 0 past the matrix.
+ *   row_sums   [N] fp32: the sum of the values that the row's codes stand for.
+ * The three are 16-byte aligned. 1 <= N, 1 <= K <= QNN_K_MAX (QNN_ERR_K_TOO_LARGE). A unit with a value that is not finite:
+ * unspecified codes, QNN_ERR_NONFINITE is recorded.
+ */
+qnn_status qnn_quantize4(const float *w, int64_t N, int64_t K, int64_t ldw, int32_t group, uint8_t *codes, uint32_t *units,
+                         float *row_sums, void *stream);
+
+/*
+ * qnn_qmatmul4 — the recovered product of Fig. 1 with 4-bit weights of qnn_quantize4, for few rows (each 32 of them read
+ * the weights once).
+ *   A, lda, pa, ga  [M x K] uint8 activation codes and their units, as for qnn_qmatmul.
+ *   codes, units, group, row_sums  of a matrix [N x K].
+ *   bias [N] fp32, nullable; Y [M x N] fp32 out (ldy >= N):
+ *     Y[m,n] = (1 / Qa) sum_groups scale sum_{k in group} (A[m,k] + za)(code[n,k] + offset) + bias[n].
+ *   The sums of a group's codes are exact; the groups' terms are added in fp32, in an order that depends on the sizes and the
+ *   device only. Codes past K are not read as products whatever A holds there.
+ */
+qnn_status qnn_qmatmul4(const uint8_t *A, int64_t lda, const qnn_qparams *pa, int ga, int64_t M, int64_t K,
+                        const uint8_t *codes, const uint32_t *units, int32_t group, const float *row_sums, int64_t N,
+                        const float *bias, float *Y, int64_t ldy, void *stream);
+
+/*
+ * qnn_causal_conv — short causal convolution of each channel over time, optionally through SiLU:
+ *   y[b][t][d] = f(bias[d] + sum_{j < W} w[d][j] x[b][t - W + 1 + j][d]),  f(v) = v / (1 + exp(-v)) or v.
+ *   x, y   [B][T][D] of `dtype`: frame t of sequence b at b * seq + t * frame elements (strides in elements, channels
+ *          contiguous). Outputs of different frames must not overlap.
+ *   w [D][W] fp32 (1 <= W <= 8), bias [D] fp32, nullable.
+ *   state_in, state_out  [B][W - 1][D] of `dtype`, nullable: the W - 1 inputs before the first frame, oldest first (NULL:
+ *          zeros), and the last W - 1 inputs after the last one. They may be the same buffer, for streaming.
+ *   lengths [B] int32, nullable: frames of each sequence (values outside 0 .. T count as the nearer of them). Frames behind a
+ *          sequence's end are not read for it and their outputs are left as they are.
+ * One frame of many sequences (T = 1 with states) is the serving form; T = 0 only carries the states over.
+ */
+qnn_status qnn_causal_conv(const void *x, int64_t x_seq, int64_t x_frame, int dtype, int64_t B, int64_t T, int64_t D,
+                           const float *w, int32_t W, const float *bias, int silu, const void *state_in, void *state_out,
+                           const int32_t *lengths, void *y, int64_t y_seq, int64_t y_frame, void *stream);
+
+/* Arguments of qnn_ssm_scan. Strides in elements: frame t of sequence b at b * seq + t * frame, its channels contiguous. */
+typedef struct {
+    int64_t B, T, D;  /* sequences, frames, channels */
+    int32_t N;        /* states of a channel, 1 .. 128 */
+    int32_t groups;   /* groups of D / groups channels that share Bm and Cm; divides D */
+    int32_t dtype;    /* of u, dt, Bm, Cm, z and y */
+    int32_t softplus; /* 1: the step is log(1 + exp(dt + dt_bias)); 0: dt + dt_bias */
+    const void *u;    /* [B][T][D] inputs */
+    int64_t u_seq, u_frame;
+    const void *dt;   /* [B][T][D] steps, before dt_bias and softplus */
+    int64_t dt_seq, dt_frame;
+    const void *Bm;   /* [B][T][groups * N] */
+    int64_t Bm_seq, Bm_frame;
+    const void *Cm;   /* [B][T][groups * N] */
+    int64_t Cm_seq, Cm_frame;
+    const void *z;    /* [B][T][D] gates, nullable */
+    int64_t z_seq, z_frame;
+    void *y;          /* [B][T][D] out */
+    int64_t y_seq, y_frame;
+    const float *A;       /* [D][N] */
+    const float *skip;    /* [D], nullable */
+    const float *dt_bias; /* [D], nullable */
+    const float *state_in; /* [B][D][N], nullable: zeros */
+    float *state_out;      /* [B][D][N], nullable; may be state_in */
+    const int32_t *lengths; /* [B], nullable */
+} qnn_ssm_args;
+
+/*
+ * qnn_ssm_scan — selective scan over time, every channel d of every sequence b with N states h of its own:
+ *   s = softplus(dt[t][d] + dt_bias[d]);  h[n] = exp(s A[d][n]) h[n] + s u[t][d] Bm[t][g][n];
+ *   y[t][d] = (sum_n Cm[t][g][n] h[n] + skip[d] u[t][d]) * z / (1 + exp(-z)),  z = z[t][d],
+ * with the last factor only where z is given and g = d / (D / groups). States and sums are fp32. lengths, frames behind a
+ * sequence's end and T = 0 as for qnn_causal_conv; state_out is the state after each sequence's last frame, and
+ * the states of a sequence do not depend on the others. One frame of many sequences is the serving form. Non-finite
+ * inputs give non-finite outputs by the formulas, in their own channel and sequence (group, for Bm and Cm).
+ */
+qnn_status qnn_ssm_scan(const qnn_ssm_args *args, void *stream);
+
+/* ---------------------------------------------------------------------------------------------
  * Kernel timing (diagnostics and benchmarks; no counterpart in the paper).
  * ------------------------------------------------------------------------------------------- */
 

@@ -53,6 +53,17 @@ bool is_device_ptr(const void *p) {
     return at.type == cudaMemoryTypeDevice || at.type == cudaMemoryTypeManaged;
 }
 
+bool is_local_ptr(const void *p) {
+    if (!p) return false;
+    cudaPointerAttributes at;
+    int dev = -1;
+    if (cudaGetDevice(&dev) != cudaSuccess || cudaPointerGetAttributes(&at, p) != cudaSuccess) {
+        cudaGetLastError();
+        return false;
+    }
+    return at.type == cudaMemoryTypeManaged || (at.type == cudaMemoryTypeDevice && at.device == dev);
+}
+
 void *host_mapped_ptr(void *p) {
     if (!p) return nullptr;
     cudaPointerAttributes at;

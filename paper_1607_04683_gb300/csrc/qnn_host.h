@@ -41,6 +41,21 @@ inline cudaStream_t as_stream(void *s) { return reinterpret_cast<cudaStream_t>(s
 // allocations). Pinned or pageable host memory is rejected by the compute calls.
 bool is_device_ptr(const void *p);
 
+// The same for memory of the current device itself (or managed): a kernel of this device reaches another's memory only
+// where peer access is on, and faults where it is not.
+bool is_local_ptr(const void *p);
+
+// The bytes from the first to past the last one of an argument, for the checks that an output overlaps no input.
+struct Span {
+    uintptr_t lo = 0, hi = 0;
+    Span() = default;
+    Span(const void *p, int64_t bytes) : lo(reinterpret_cast<uintptr_t>(p)), hi(lo + (p ? (uintptr_t)bytes : 0)) {}
+    bool meets(const Span &o) const { return lo < o.hi && o.lo < hi; }
+};
+
+inline int dtype_size(int dtype) { return dtype == QNN_F32 ? 4 : 2; }
+inline bool dtype_ok(int dtype) { return dtype == QNN_F32 || dtype == QNN_BF16 || dtype == QNN_F16; }
+
 // The address under which kernels of the current device reach p when p is pinned (page-locked)
 // host memory mapped into the device's address space; null for any other memory. Kernels that
 // write a host output through it send each byte over the host link once, with no staging copy.

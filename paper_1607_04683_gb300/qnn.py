@@ -35,7 +35,11 @@ EXPORTS = ("qnn_status_string", "qnn_device_status", "qnn_quantize", "qnn_qmatmu
            "qnn_lstm_forward_logits",
            "qnn_profile_enable", "qnn_profile_read", "qnn_measure_peak", "qnn_quantize_matrix_static",
            "qnn_selftest_s64_to_f32", "qnn_stack_frames", "qnn_selftest_wait_timeout", "qnn_selftest_pair_functions", "qnn_lstm_stream_open",
-           "qnn_lstm_stream_push", "qnn_lstm_stream_pull", "qnn_lstm_stream_close", "qnn_measure_exchange_floor")
+           "qnn_lstm_stream_push", "qnn_lstm_stream_pull", "qnn_lstm_stream_close", "qnn_measure_exchange_floor",
+           "qnn_rmsnorm_quantize", "qnn_quantize4", "qnn_qmatmul4", "qnn_causal_conv", "qnn_ssm_scan")
+
+# qnn_dtype by a torch type's name
+_DTYPES = {"torch.float32": 0, "torch.bfloat16": 1, "torch.float16": 2}
 
 
 class QnnError(RuntimeError):
@@ -49,6 +53,16 @@ class LstmDesc(C.Structure):
     _fields_ = [("num_layers", C.c_int32), ("input_dim", C.c_int32), ("hidden", C.c_int32),
                 ("proj", C.c_int32), ("num_classes", C.c_int32), ("output_mode", C.c_int32),
                 ("stack", C.c_int32), ("stack_stride", C.c_int32), ("weight_blocks", C.c_int32)]
+
+
+class SsmArgs(C.Structure):
+    """qnn_ssm_args"""
+    _fields_ = [("B", C.c_int64), ("T", C.c_int64), ("D", C.c_int64), ("N", C.c_int32), ("groups", C.c_int32),
+                ("dtype", C.c_int32), ("softplus", C.c_int32),
+                *[(n + f, C.c_void_p if f == "" else C.c_int64) for n in ("u", "dt", "Bm", "Cm", "z", "y")
+                  for f in ("", "_seq", "_frame")],
+                ("A", C.c_void_p), ("skip", C.c_void_p), ("dt_bias", C.c_void_p), ("state_in", C.c_void_p),
+                ("state_out", C.c_void_p), ("lengths", C.c_void_p)]
 
 
 _lib = None
@@ -108,6 +122,16 @@ def lib():
         L.qnn_lstm_stream_close.restype = i32
         L.qnn_quantize_matrix_static.argtypes = [P, i64, i64, i64, P, i64, P, P, P, P]
         L.qnn_quantize_matrix_static.restype = i32
+        L.qnn_rmsnorm_quantize.argtypes = [P, i64, P, i64, i32, P, C.c_double, i64, i64, P, i64, P, i64, P, P, P, i64, P]
+        L.qnn_rmsnorm_quantize.restype = i32
+        L.qnn_quantize4.argtypes = [P, i64, i64, i64, C.c_int32, P, P, P, P]
+        L.qnn_quantize4.restype = i32
+        L.qnn_qmatmul4.argtypes = [P, i64, P, i32, i64, i64, P, P, C.c_int32, P, i64, P, P, i64, P]
+        L.qnn_qmatmul4.restype = i32
+        L.qnn_causal_conv.argtypes = [P, i64, i64, i32, i64, i64, i64, P, C.c_int32, P, i32, P, P, P, P, i64, i64, P]
+        L.qnn_causal_conv.restype = i32
+        L.qnn_ssm_scan.argtypes = [C.POINTER(SsmArgs), P]
+        L.qnn_ssm_scan.restype = i32
         _lib = L
     return _lib
 
@@ -236,6 +260,173 @@ def qnn_qmatmul(A, pa, ga, rsA, W, pw, csW, n_blocks=1, bias=None, want_acc=Fals
                              _p(csW), N, _p(bias), _p(Y), N if out is None else out.stride(0), _p(acc),
                              _stream(stream)), "qnn_qmatmul")
     return Y, acc
+
+
+def _want(ok: bool, what: str):
+    if not ok:
+        raise ValueError(what)
+
+
+def _dtype(t, what: str) -> int:
+    d = _DTYPES.get(str(t.dtype))
+    _want(d is not None, f"{what}: fp32, bf16 or fp16")
+    return d
+
+
+def _rows(t, what: str, dtype, shape) -> int:
+    """Leading dimension of a matrix whose rows are contiguous."""
+    _want(t.dtype == dtype and t.shape == shape, f"{what}: {dtype} {tuple(shape)}")
+    s0, s1 = t.stride()
+    _want((s1 == 1 or shape[1] <= 1) and (s0 >= shape[1] or shape[0] <= 1), f"{what}: rows of contiguous values, apart")
+    return s0 if s0 >= shape[1] else shape[1]
+
+
+def _flat(t, what: str, dtype, shape):
+    """A contiguous array, or None."""
+    _want(t is None or (t.dtype == dtype and t.shape == shape and t.is_contiguous()), f"{what}: contiguous {dtype} {tuple(shape)}")
+    return None if t is None else t.data_ptr()
+
+
+def _frames(t, what: str, dtype, shape):
+    """Address, sequence stride and frame stride of [B, T, ...] values whose frames are contiguous."""
+    _want(t.dtype == dtype and t.shape == shape, f"{what}: {dtype} {tuple(shape)}")
+    st = t.stride()
+    width = 1
+    for n, s in zip(reversed(shape[2:]), reversed(st[2:])):
+        _want(s == width or n <= 1, f"{what}: frames of contiguous values")
+        width *= n
+    return t.data_ptr(), st[0], st[1]
+
+
+def _result(shape, dtype, like, stream):
+    """A new tensor for a call on stream: where that is not the current one, its memory is not given to others before
+    what the call queued there is done."""
+    import torch
+    t = torch.empty(shape, dtype=dtype, device=like.device)
+    if stream is not None:
+        t.record_stream(stream)
+    return t
+
+
+def qnn_rmsnorm_quantize(x, weight, residual=None, eps=1e-5, residual_out=None, want_values=False, stream=None):
+    """Rows of x (+ residual) [rows, cols] (fp32, bf16 or fp16), through a root-mean-square norm with weight [cols] fp32, to
+    8-bit codes, one unit per row. Returns (codes u8, params int32 [rows, 4], code_sums int32 [rows], h, values): h = x +
+    residual in x's type (residual_out, which may be x or residual, or a new tensor; None without a residual), values the
+    fp32 values that the codes stand for (None unless wanted)."""
+    import torch
+    _want(x.dim() == 2 and x.is_cuda, "x: a CUDA matrix")
+    dt = _dtype(x, "x")
+    rows, cols = shape = x.shape
+    ldx = _rows(x, "x", x.dtype, shape)
+    ldr = _rows(residual, "residual", x.dtype, shape) if residual is not None else 0
+    _want(residual_out is None or residual is not None, "residual_out: needs a residual")
+    h = residual_out if residual_out is not None or residual is None else _result(shape, x.dtype, x, stream)
+    ldh = _rows(h, "residual_out", x.dtype, shape) if h is not None else 0
+    w = _flat(weight, "weight", torch.float32, (cols,))
+    codes = _result(shape, torch.uint8, x, stream)
+    params = _result((rows, 4), torch.int32, x, stream)
+    sums = _result((rows,), torch.int32, x, stream)
+    values = _result(shape, torch.float32, x, stream) if want_values else None
+    _check(lib().qnn_rmsnorm_quantize(x.data_ptr(), ldx, _p(residual), ldr, dt, w, eps, rows, cols, _p(h), ldh,
+                                      codes.data_ptr(), cols, params.data_ptr(), sums.data_ptr(), _p(values), cols,
+                                      _stream(stream)), "qnn_rmsnorm_quantize")
+    return codes, params, sums, h, values
+
+
+class Weights4:
+    """4-bit weights [N, K] with a scale and an offset per `group` columns of a row, as qnn_quantize4 lays them out: codes
+    u8 [ceil(N/16), ceil(K/128), 1024], units bf16 [ceil(N/16), ceil(K/128), 16, 128 / group, 2] (offset, scale),
+    row_sums fp32 [N]."""
+    __slots__ = ("codes", "units", "row_sums", "N", "K", "group")
+
+    def __init__(self, codes, units, row_sums, N: int, K: int, group: int):
+        import torch
+        _want(group in (32, 64, 128), "group: 32, 64 or 128")
+        tiles = ((N + 15) // 16, (K + 127) // 128)
+        _flat(codes, "codes", torch.uint8, (*tiles, 1024))
+        _flat(units, "units", torch.bfloat16, (*tiles, 16, 128 // group, 2))
+        _flat(row_sums, "row_sums", torch.float32, (N,))
+        self.codes, self.units, self.row_sums, self.N, self.K, self.group = codes, units, row_sums, N, K, group
+
+
+def qnn_quantize4(w, group: int = 64, stream=None) -> Weights4:
+    """Weights w, CUDA fp32 [N, K], to 4-bit codes offline, one unit per group (32, 64 or 128) of a row's columns."""
+    import torch
+    _want(w.dim() == 2 and w.is_cuda, "w: a CUDA matrix")
+    _want(group in (32, 64, 128), "group: 32, 64 or 128")
+    N, K = w.shape
+    ldw = _rows(w, "w", torch.float32, w.shape)
+    tiles = ((N + 15) // 16, (K + 127) // 128)
+    codes = _result((*tiles, 1024), torch.uint8, w, stream)
+    units = _result((*tiles, 16, 128 // group, 2), torch.bfloat16, w, stream)
+    sums = _result((N,), torch.float32, w, stream)
+    _check(lib().qnn_quantize4(w.data_ptr(), N, K, ldw, group, codes.data_ptr(), units.data_ptr(), sums.data_ptr(),
+                               _stream(stream)), "qnn_quantize4")
+    return Weights4(codes, units, sums, N, K, group)
+
+
+def qnn_qmatmul4(A, pa, weights: Weights4, ga=PER_ROW, bias=None, out=None, stream=None):
+    """Y = R(A' W'^T) + bias with 4-bit weights: A u8 [M, K] codes with their units pa int32 [M, 4] (or [1, 4] with
+    ga = PER_MATRIX), as qnn_quantize and qnn_rmsnorm_quantize give them. Returns Y fp32 [M, N]."""
+    import torch
+    _want(A.dim() == 2 and A.is_cuda and A.shape[1] == weights.K, "A: a CUDA matrix of the weights' K columns")
+    M, K = A.shape
+    N = weights.N
+    lda = _rows(A, "A", torch.uint8, A.shape)
+    p = _flat(pa, "pa", torch.int32, (M if ga == PER_ROW else 1, 4))
+    b = _flat(bias, "bias", torch.float32, (N,))
+    Y = out if out is not None else _result((M, N), torch.float32, A, stream)
+    ldy = _rows(Y, "out", torch.float32, (M, N)) if out is not None else N
+    _check(lib().qnn_qmatmul4(A.data_ptr(), lda, p, ga, M, K, weights.codes.data_ptr(), weights.units.data_ptr(), weights.group,
+                              weights.row_sums.data_ptr(), N, b, Y.data_ptr(), ldy, _stream(stream)), "qnn_qmatmul4")
+    return Y
+
+
+def qnn_causal_conv(x, weight, bias=None, silu=True, state_in=None, state_out=None, lengths=None, out=None, stream=None):
+    """Short causal convolution over time of each channel, through SiLU unless silu is False: x [B, T, D] (fp32, bf16 or
+    fp16; frames may be slices of wider ones), weight [D, W] and bias [D] fp32, states [B, W - 1, D] in x's type (state_out
+    may be state_in), lengths int32 [B]. Returns out, [B, T, D]; without an out given, the frames behind a sequence's end
+    hold nothing in particular."""
+    import torch
+    _want(x.dim() == 3 and x.is_cuda, "x: CUDA [B, T, D]")
+    dt = _dtype(x, "x")
+    B, T, D = shape = x.shape
+    _want(weight.dim() == 2, "weight: [D, W]")
+    W = weight.shape[1]
+    y = out if out is not None else _result(shape, x.dtype, x, stream)
+    _check(lib().qnn_causal_conv(*_frames(x, "x", x.dtype, shape), dt, B, T, D, _flat(weight, "weight", torch.float32, (D, W)), W,
+                                 _flat(bias, "bias", torch.float32, (D,)), 1 if silu else 0,
+                                 _flat(state_in, "state_in", x.dtype, (B, W - 1, D)),
+                                 _flat(state_out, "state_out", x.dtype, (B, W - 1, D)),
+                                 _flat(lengths, "lengths", torch.int32, (B,)), *_frames(y, "out", x.dtype, shape),
+                                 _stream(stream)), "qnn_causal_conv")
+    return y
+
+
+def qnn_ssm_scan(u, dt, A, B, C, D=None, z=None, dt_bias=None, softplus=True, state_in=None, state_out=None, lengths=None,
+                 out=None, stream=None):
+    """Selective scan over time: u, dt and z [B, T, D] and B, C [B, T, groups, N] or [B, T, N] (fp32, bf16 or fp16, all of one
+    type; frames may be slices of wider ones), A [D, N], D [D], dt_bias [D] and states [B, D, N] fp32 (state_out may be
+    state_in), lengths int32 [B]. Returns out, [B, T, D]; without an out given, the frames behind a sequence's end hold
+    nothing in particular."""
+    import torch
+    _want(u.dim() == 3 and u.is_cuda, "u: CUDA [B, T, D]")
+    ty, f32 = u.dtype, torch.float32
+    kind = _dtype(u, "u")
+    nb, nt, nd = shape = u.shape
+    _want(A.dim() == 2, "A: [D, N]")
+    ns = A.shape[1]
+    groups = B.shape[2] if B.dim() == 4 else 1
+    bc = (nb, nt, groups, ns) if B.dim() == 4 else (nb, nt, ns)
+    y = out if out is not None else _result(shape, ty, u, stream)
+    state = (nb, nd, ns)
+    a = SsmArgs(nb, nt, nd, ns, groups, kind, 1 if softplus else 0, *_frames(u, "u", ty, shape), *_frames(dt, "dt", ty, shape),
+                *_frames(B, "B", ty, bc), *_frames(C, "C", ty, bc), *((None, 0, 0) if z is None else _frames(z, "z", ty, shape)),
+                *_frames(y, "out", ty, shape), _flat(A, "A", f32, (nd, ns)), _flat(D, "D", f32, (nd,)),
+                _flat(dt_bias, "dt_bias", f32, (nd,)), _flat(state_in, "state_in", f32, state),
+                _flat(state_out, "state_out", f32, state), _flat(lengths, "lengths", torch.int32, (nb,)))
+    _check(lib().qnn_ssm_scan(a, _stream(stream)), "qnn_ssm_scan")
+    return y
 
 
 def lstm_desc(num_layers, input_dim, hidden, proj=0, num_classes=0, output_mode=None, stack=0,
