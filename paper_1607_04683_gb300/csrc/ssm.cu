@@ -9,92 +9,541 @@
 namespace qnn {
 namespace {
 
-__device__ __forceinline__ float silu(float v) { return __fdiv_rn(v, __fadd_rn(1.0f, expf(-v))); }
-
 // Frames of sequence b.
-__device__ __forceinline__ int64_t frames_of(const int32_t *lengths, int64_t b, int64_t T) {
-    if (!lengths) return T;
-    const int64_t n = __ldg(lengths + b);
-    return n < 0 ? 0 : n > T ? T : n;
+__device__ __forceinline__ int frames_of(const int32_t *lengths, int64_t b, int64_t T) {
+    if (!lengths) return (int)T;
+    const int n = __ldg(lengths + b);
+    return n < 0 ? 0 : n > T ? (int)T : n;
 }
+
+// ------------------------------------------------------------------------------------------------
+// Convolution
+// ------------------------------------------------------------------------------------------------
 
 struct ConvArgs {
     const void *x, *state_in;
     void *state_out, *y;
     const float *w, *bias;
     const int32_t *lengths;
-    int64_t x_seq, x_frame, y_seq, y_frame, B, T, D;
-    int W, silu;
+    int64_t x_seq, x_frame, y_seq, y_frame, B, T, D, runs, chunks;
+    int W, silu, chunk;
 };
 
-// A thread a channel of a sequence, all its frames in turn; it alone reads and writes the channel's state.
-constexpr int kMostTaps = 8;
-template <typename T>
-__global__ void __launch_bounds__(128) causal_conv_plain_kernel(const ConvArgs a) {
-    const int64_t at = (int64_t)blockIdx.x * 128 + threadIdx.x, b = at / a.D, d = at % a.D;
+// A thread takes V neighbouring channels of a sequence over a chunk of its frames, the last WT - 1 inputs in registers and
+// kAhead frames' loads in flight. The first chunk's thread alone reads and writes the channels' state: it has read the old
+// state before it writes the new one, and later chunks (at least WT - 1 frames on) never look at it. W < WT taps stand at
+// the end of WT, the others are not loaded and count 0.
+constexpr int kMostTaps = 8, kConvThreads = 128, kAhead = 4;
+template <typename T, int WT, int V>
+__global__ void __launch_bounds__(kConvThreads) causal_conv_kernel(const ConvArgs a) {
+    const int64_t at = (int64_t)blockIdx.x * kConvThreads + threadIdx.x;
+    const int64_t run = at % a.runs, rest = at / a.runs, chunk = rest % a.chunks, b = rest / a.chunks;
     if (b >= a.B) return;
-    const int64_t n = frames_of(a.lengths, b, a.T);
-    const int W = a.W;
+    const int n = frames_of(a.lengths, b, a.T), t0 = (int)chunk * a.chunk, t1 = min(n, t0 + a.chunk), W = a.W;
+    if (chunk > 0 && t0 >= n) return;
+    const int64_t d = run * V;
     const T *x = static_cast<const T *>(a.x) + b * a.x_seq + d;
     T *y = static_cast<T *>(a.y) + b * a.y_seq + d;
-    const T *in = static_cast<const T *>(a.state_in) + (b * (W - 1)) * a.D + d;
-    T *out = static_cast<T *>(a.state_out) + (b * (W - 1)) * a.D + d;
-    T taps[kMostTaps];  // the last W inputs, taps[W - 1] the newest
-    float w[kMostTaps];
-    for (int j = 0; j < W; ++j) w[j] = __ldg(a.w + d * W + j);
-    for (int j = 0; j + 1 < W; ++j) taps[j + 1] = a.state_in ? in[j * a.D] : from_f32<T>(0.0f);
-    const float bias = a.bias ? __ldg(a.bias + d) : 0.0f;
-    for (int64_t t = 0; t < n; ++t) {
-        for (int j = 0; j + 1 < W; ++j) taps[j] = taps[j + 1];
-        taps[W - 1] = x[t * a.x_frame];
-        float v = bias;
-        for (int j = 0; j < W; ++j) v = __fmaf_rn(w[j], to_f32(taps[j]), v);
-        y[t * a.y_frame] = from_f32<T>(a.silu ? silu(v) : v);
+    const T *s_in = static_cast<const T *>(a.state_in) + b * (W - 1) * a.D + d;
+    T *s_out = static_cast<T *>(a.state_out) + b * (W - 1) * a.D + d;
+    Run<T, V> taps[WT];  // taps[j]: the input WT - 1 - j frames back
+#pragma unroll
+    for (int j = 0; j < WT; ++j) taps[j].clear();
+#pragma unroll
+    for (int j = 0; j < WT - 1; ++j) {  // before the chunk: WT - 1 - j frames back of t0
+        const int t = t0 - (WT - 1) + j;
+        if (j < WT - W) continue;
+        if (chunk > 0)
+            taps[j].load(x + t * a.x_frame);
+        else if (a.state_in)
+            taps[j].load(s_in + (t + W - 1) * a.D);
     }
-    if (a.state_out)
-        for (int j = 0; j + 1 < W; ++j) out[j * a.D] = taps[j + 1];
+    if (t0 < t1) {
+        float w[WT][V], bias[V];
+#pragma unroll
+        for (int v = 0; v < V; ++v) {
+            bias[v] = a.bias ? __ldg(a.bias + d + v) : 0.0f;
+#pragma unroll
+            for (int j = 0; j < WT; ++j) w[j][v] = j >= WT - W ? __ldg(a.w + (d + v) * W + j - (WT - W)) : 0.0f;
+        }
+        Run<T, V> next[kAhead];
+        auto fetch = [&](int t) {
+#pragma unroll
+            for (int i = 0; i < kAhead; ++i)
+                if (t + i < t1) next[i].load(x + (int64_t)(t + i) * a.x_frame);
+        };
+        fetch(t0);
+        for (int t = t0; t < t1; t += kAhead) {
+            Run<T, V> now[kAhead];
+#pragma unroll
+            for (int i = 0; i < kAhead; ++i) now[i] = next[i];
+            fetch(t + kAhead);
+#pragma unroll
+            for (int i = 0; i < kAhead; ++i) {
+                if (t + i >= t1) break;
+                taps[WT - 1] = now[i];
+                float o[V];
+#pragma unroll
+                for (int v = 0; v < V; ++v) {
+                    o[v] = bias[v];
+#pragma unroll
+                    for (int j = 0; j < WT; ++j) o[v] = __fmaf_rn(w[j][v], taps[j].get(v), o[v]);
+                    if (a.silu) o[v] = silu(o[v]);
+                }
+                Run<T, V> out;
+                out.set(o);
+                out.store(y + (int64_t)(t + i) * a.y_frame);
+#pragma unroll
+                for (int j = 0; j < WT - 1; ++j) taps[j] = taps[j + 1];
+            }
+        }
+    }
+    if (chunk > 0 || !a.state_out) return;
+    // the last W - 1 of old state and n frames. Where the chunk holds all frames they are the taps (shifted once a frame)
+    if (n <= a.chunk) {
+#pragma unroll
+        for (int j = 0; j < WT - 1; ++j)
+            if (j >= WT - W) taps[j].store(s_out + (j - (WT - W)) * a.D);
+    } else {
+        for (int j = 0; j < W - 1; ++j) {
+            Run<T, V> last;
+            last.load(x + (int64_t)(n - (W - 1) + j) * a.x_frame);
+            last.store(s_out + j * a.D);
+        }
+    }
 }
+
+// ------------------------------------------------------------------------------------------------
+// Scan
+// ------------------------------------------------------------------------------------------------
 
 constexpr int kMostStates = 128;
 
-// A warp a channel of a sequence, a lane every 32nd state.
+struct ScanArgs : qnn_ssm_args {
+    int vec;              // kVec*: arrays whose runs of channels may be loaded or stored whole
+    int64_t group_chans;  // D / groups
+    int group_blocks;     // blocks a group
+    int parts;            // blocks (a cluster of them) that share a sequence's frames
+};
+enum { kVecU = 1, kVecDt = 2, kVecZ = 4, kVecY = 8, kVecStates = 16, kVecBC = 32 };
+
+// Few frames: no frame waits for another for long, and states are most of the traffic (8 N bytes a channel, in and out).
+// A lane holds four states of a channel, 1 .. 32 lanes a channel; each step's sum over the states by shuffles.
+constexpr int kStepFrames = 4, kStepThreads = 128;
 template <typename T>
-__global__ void __launch_bounds__(128) ssm_scan_plain_kernel(const qnn_ssm_args a) {
-    const int64_t at = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 5), b = at / a.D, d = at % a.D;
-    const int lane = threadIdx.x & 31;
-    if (b >= a.B) return;
-    const int64_t frames = frames_of(a.lengths, b, a.T), g = d / (a.D / a.groups);
-    float h[4], A[4];
+__global__ void __launch_bounds__(kStepThreads) ssm_step_kernel(const ScanArgs a, int lanes) {
+    const int64_t at = (int64_t)blockIdx.x * kStepThreads + threadIdx.x, chan = at / lanes;
+    const int n0 = 4 * (int)(at % lanes);
+    const bool there = chan < a.B * a.D;
+    const int64_t b = there ? chan / a.D : a.B - 1, d = there ? chan % a.D : a.D - 1, g = d / a.group_chans;
+    const int count = there ? max(min(a.N - n0, 4), 0) : 0;
+    const int frames = frames_of(a.lengths, b, a.T);
+    float h[4] = {}, A[4] = {};
+    const int64_t state = (b * a.D + d) * a.N + n0;
+    if (a.vec & kVecStates) {
+        if (count) {
+            Run<float, 4> r;
+            r.load(a.A + d * a.N + n0);
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        const int n = lane + 32 * i;
-        h[i] = n < a.N && a.state_in ? a.state_in[(b * a.D + d) * a.N + n] : 0.0f;
-        A[i] = n < a.N ? a.A[d * a.N + n] : 0.0f;
-    }
-    const float skip = a.skip ? a.skip[d] : 0.0f, bias = a.dt_bias ? a.dt_bias[d] : 0.0f;
-    for (int64_t t = 0; t < frames; ++t) {
-        const float u = to_f32(static_cast<const T *>(a.u)[b * a.u_seq + t * a.u_frame + d]);
-        float s = __fadd_rn(to_f32(static_cast<const T *>(a.dt)[b * a.dt_seq + t * a.dt_frame + d]), bias);
-        if (a.softplus && s <= 20.0f) s = log1pf(expf(s));
-        const T *Bm = static_cast<const T *>(a.Bm) + b * a.Bm_seq + t * a.Bm_frame + g * a.N;
-        const T *Cm = static_cast<const T *>(a.Cm) + b * a.Cm_seq + t * a.Cm_frame + g * a.N;
-        float y = 0.0f;
+            for (int i = 0; i < 4; ++i) A[i] = r.get(i);
+            if (a.state_in) {
+                r.load(a.state_in + state);
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const int n = lane + 32 * i;
-            if (n < a.N) {
-                h[i] = __fmaf_rn(expf(__fmul_rn(s, A[i])), h[i], __fmul_rn(__fmul_rn(s, u), to_f32(Bm[n])));
-                y = __fmaf_rn(to_f32(Cm[n]), h[i], y);
+                for (int i = 0; i < 4; ++i) h[i] = r.get(i);
             }
         }
-        y = __fmaf_rn(skip, u, warp_sum_f(y));
-        if (a.z) y = __fmul_rn(y, silu(to_f32(static_cast<const T *>(a.z)[b * a.z_seq + t * a.z_frame + d])));
-        if (lane == 0) static_cast<T *>(a.y)[b * a.y_seq + t * a.y_frame + d] = from_f32<T>(y);
-    }
-    if (a.state_out)
+    } else {
 #pragma unroll
         for (int i = 0; i < 4; ++i)
-            if (lane + 32 * i < a.N) a.state_out[(b * a.D + d) * a.N + lane + 32 * i] = h[i];
+            if (i < count) {
+                A[i] = __ldg(a.A + d * a.N + n0 + i);
+                if (a.state_in) h[i] = a.state_in[state + i];
+            }
+    }
+    const float skip = a.skip ? __ldg(a.skip + d) : 0.0f, bias = a.dt_bias ? __ldg(a.dt_bias + d) : 0.0f;
+    for (int t = 0; t < a.T; ++t) {  // (frames differ within a warp: all lanes take part in the shuffles)
+        const bool on = t < frames;
+        float y = 0.0f, u = 0.0f, gate = 1.0f;
+        if (on && count) {
+            u = to_f32(static_cast<const T *>(a.u)[b * a.u_seq + t * a.u_frame + d]);
+            float s = __fadd_rn(to_f32(static_cast<const T *>(a.dt)[b * a.dt_seq + t * a.dt_frame + d]), bias);
+            const T *pB = static_cast<const T *>(a.Bm) + b * a.Bm_seq + t * a.Bm_frame + g * a.N + n0;
+            const T *pC = static_cast<const T *>(a.Cm) + b * a.Cm_seq + t * a.Cm_frame + g * a.N + n0;
+            Run<T, 4> rB, rC;
+            if (a.vec & kVecBC)
+                rB.load(pB), rC.load(pC);
+            else
+                rB.load_some(pB, count), rC.load_some(pC, count);
+            if (a.z) gate = silu(to_f32(static_cast<const T *>(a.z)[b * a.z_seq + t * a.z_frame + d]));
+            if (a.softplus) s = softplus(s);
+            const float su = __fmul_rn(s, u), s2 = __fmul_rn(s, kLog2e);
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+                if (i < count) {
+                    h[i] = __fmaf_rn(exp2_hw(__fmul_rn(s2, A[i])), h[i], __fmul_rn(su, rB.get(i)));
+                    y = __fmaf_rn(rC.get(i), h[i], y);
+                }
+        }
+        for (int o = lanes >> 1; o > 0; o >>= 1) y = __fadd_rn(y, __shfl_xor_sync(0xffffffffu, y, o));
+        if (on && there && n0 == 0)
+            static_cast<T *>(a.y)[b * a.y_seq + t * a.y_frame + d] = from_f32<T>(__fmul_rn(__fmaf_rn(skip, u, y), gate));
+    }
+    if (!a.state_out) return;
+    if (a.vec & kVecStates) {
+        if (count) *reinterpret_cast<float4 *>(a.state_out + state) = make_float4(h[0], h[1], h[2], h[3]);
+    } else {
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            if (i < count) a.state_out[state + i] = h[i];
+    }
+}
+
+__device__ __forceinline__ uint32_t cluster_rank() {
+    uint32_t r;
+    asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(r));
+    return r;
+}
+__device__ __forceinline__ void cluster_arrive() { asm volatile("barrier.cluster.arrive.release;" ::: "memory"); }
+__device__ __forceinline__ void cluster_wait() { asm volatile("barrier.cluster.wait.acquire;" ::: "memory"); }
+// The address of a shared variable in another block of the cluster, and a load from it.
+__device__ __forceinline__ uint32_t peer_address(const void *p, uint32_t rank) {
+    uint32_t r;
+    asm("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(r) : "r"((uint32_t)__cvta_generic_to_shared(p)), "r"(rank));
+    return r;
+}
+__device__ __forceinline__ float peer_load(uint32_t at) {
+    float v;
+    asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v) : "r"(at) : "memory");
+    return v;
+}
+
+// Whole sequences. A block takes 128 / L channels of one group over a part of a sequence's frames, tile by tile of kTile
+// frames: its threads load u, dt (and z) in runs of channels, form s = softplus(dt) and s u, and leave them in shared memory
+// beside the tile's Bm and Cm; then L lanes a channel, NS states each, carry the states over the tile's frames; then the
+// threads that loaded u and z finish the outputs. The loads of the next tile are in flight meanwhile.
+//
+// Where sequences are few, a cluster of `parts` blocks shares each one's frames. The recurrence is linear: over a part,
+// h' = exp(A S) h + r, with S the sum of its steps and r what it reaches from h = 0. Each block first finds S and r of its part
+// (no Cm, z or outputs), reads those of the parts before its own from their shared memory, composes its first state from
+// them, and then goes over its part once more with it.
+constexpr int kScanThreads = 128, kTile = 16;
+template <typename T, int NS, int L>
+struct ScanBlock {
+    static constexpr int kChans = kScanThreads / L;             // a block
+    static constexpr int kStates = NS * L;                      // of a channel, padded
+    static constexpr int kEach = kTile / L;                     // values a thread loads of each array
+    static constexpr int V = kEach < 4 ? kEach : 4, kRuns = kEach / V;
+    static constexpr int kRowThreads = kChans / kEach;          // 8: threads a frame
+    static constexpr int kBC = (kTile * kStates + kScanThreads - 1) / kScanThreads;
+    static_assert(kRowThreads * kTile == kScanThreads, "a thread has a place in one frame of the tile");
+
+    alignas(16) float s[kTile][kChans];    // steps, then outputs' sums
+    alignas(16) float su[kTile][kChans];
+    alignas(16) float y[kTile][kChans];
+    alignas(16) float B[kTile][kStates], C[kTile][kStates];
+    alignas(16) float bias[kChans], skip[kChans];
+    alignas(16) float part[NS][kScanThreads];
+    float sum[kScanThreads];
+};
+
+// h <- exp2(s A) h + su B for NS states, y += C h, in pairs: one instruction issues for two results (a state costs 2.5
+// issue slots and the hardware's exponential instead of 4.5).
+template <int NS>
+__device__ __forceinline__ void advance(float2 (&h)[NS / 2], const float2 (&A)[NS / 2], float s, float su, const float *B) {
+    const float2 s2 = make_float2(s, s), su2 = make_float2(su, su);
+#pragma unroll
+    for (int i = 0; i < NS / 2; i += 2) {
+        const float4 b = *reinterpret_cast<const float4 *>(B + 2 * i);
+        float2 x = fmul2_rn(s2, A[i]), x1 = fmul2_rn(s2, A[i + 1]);
+        x.x = exp2_hw(x.x), x.y = exp2_hw(x.y), x1.x = exp2_hw(x1.x), x1.y = exp2_hw(x1.y);
+        h[i] = ffma2_rn(x, h[i], fmul2_rn(su2, make_float2(b.x, b.y)));
+        h[i + 1] = ffma2_rn(x1, h[i + 1], fmul2_rn(su2, make_float2(b.z, b.w)));
+    }
+}
+template <int NS>
+__device__ __forceinline__ float dot(const float2 (&h)[NS / 2], const float *C) {
+    float2 y = make_float2(0.0f, 0.0f);
+#pragma unroll
+    for (int i = 0; i < NS / 2; i += 2) {
+        const float4 c = *reinterpret_cast<const float4 *>(C + 2 * i);
+        y = ffma2_rn(h[i], make_float2(c.x, c.y), y);
+        y = ffma2_rn(h[i + 1], make_float2(c.z, c.w), y);
+    }
+    return __fadd_rn(y.x, y.y);
+}
+
+template <typename T, int NS, int L>
+__global__ void __launch_bounds__(kScanThreads) ssm_scan_kernel(const ScanArgs a) {
+    using Sh = ScanBlock<T, NS, L>;
+    constexpr int V = Sh::V, R = Sh::kRuns;
+    __shared__ Sh sh;
+    const int tid = threadIdx.x;
+    const int rank = a.parts > 1 ? (int)cluster_rank() : 0;
+    int64_t rest = blockIdx.x / a.parts;
+    const int blk = (int)(rest % a.group_blocks);
+    rest /= a.group_blocks;
+    const int g = (int)(rest % a.groups);
+    const int64_t b = rest / a.groups;
+    const int64_t d0 = g * a.group_chans + (int64_t)blk * Sh::kChans;
+    const int chans = (int)min((int64_t)Sh::kChans, (g + 1) * a.group_chans - d0);
+    const int n = frames_of(a.lengths, b, a.T);
+    const int tiles = (n + kTile - 1) / kTile, each = (tiles + a.parts - 1) / a.parts * kTile;
+    const int first = min(n, rank * each), last = min(n, first + each);
+
+    // this thread's place in the loads and stores: frame `row` of the tile, channels run(j) .. run(j) + V
+    const int row = tid / Sh::kRowThreads;
+    auto run = [&](int j) { return V * (tid % Sh::kRowThreads + j * Sh::kRowThreads); };
+    for (int c = tid; c < Sh::kChans; c += kScanThreads) {
+        sh.bias[c] = a.dt_bias && c < chans ? __ldg(a.dt_bias + d0 + c) : 0.0f;
+        sh.skip[c] = a.skip && c < chans ? __ldg(a.skip + d0 + c) : 0.0f;
+    }
+    // and in the recurrence: channel c, states n0 .. n0 + NS
+    const int c = tid / L, q = tid % L, n0 = q * NS;
+    float2 A[NS / 2], h[NS / 2];
+    const bool start = rank == 0 && a.state_in;
+#pragma unroll
+    for (int i = 0; i < NS; ++i) {
+        const bool ok = c < chans && n0 + i < a.N;
+        const float v = ok ? __fmul_rn(__ldg(a.A + (d0 + c) * a.N + n0 + i), kLog2e) : 0.0f;
+        const float s = ok && start ? a.state_in[(b * a.D + d0 + c) * a.N + n0 + i] : 0.0f;
+        if (i & 1)
+            A[i / 2].y = v, h[i / 2].y = s;
+        else
+            A[i / 2].x = v, h[i / 2].x = s;
+    }
+    float2 h0[NS / 2];
+#pragma unroll
+    for (int i = 0; i < NS / 2; ++i) h0[i] = h[i];
+
+    Run<T, V> ru[R], rd[R], rz[R];
+    Run<T, 1> rB[Sh::kBC], rC[Sh::kBC];
+    auto fetch = [&](int t0, bool final) {
+        const int t = t0 + row;
+        auto get = [&](Run<T, V> *r, const void *p, int64_t seq, int64_t frame, bool vec) {
+            const T *at = static_cast<const T *>(p) + b * seq + t * frame + d0;
+#pragma unroll
+            for (int j = 0; j < R; ++j) {
+                const int left = t < last ? chans - run(j) : 0;
+                if (vec && left >= V)
+                    r[j].load(at + run(j));
+                else
+                    r[j].load_some(at + run(j), left);
+            }
+        };
+        get(ru, a.u, a.u_seq, a.u_frame, a.vec & kVecU);
+        get(rd, a.dt, a.dt_seq, a.dt_frame, a.vec & kVecDt);
+        if (final && a.z) get(rz, a.z, a.z_seq, a.z_frame, a.vec & kVecZ);
+#pragma unroll
+        for (int i = 0; i < Sh::kBC; ++i) {
+            const int e = tid + i * kScanThreads, tt = t0 + e / Sh::kStates, k = e % Sh::kStates;
+            const bool ok = tt < last && k < a.N && e < kTile * Sh::kStates;
+            rB[i].load_some(static_cast<const T *>(a.Bm) + b * a.Bm_seq + tt * a.Bm_frame + (int64_t)g * a.N + k, ok);
+            if (final) rC[i].load_some(static_cast<const T *>(a.Cm) + b * a.Cm_seq + tt * a.Cm_frame + (int64_t)g * a.N + k, ok);
+        }
+    };
+    float du[R][V], gate[R][V];
+    auto stage = [&](int t0, bool final) {  // a frame that is not there has a step of 0, which leaves the states as they are
+        const bool on = t0 + row < last;
+#pragma unroll
+        for (int j = 0; j < R; ++j) {
+            float s[V], su[V];
+#pragma unroll
+            for (int v = 0; v < V; ++v) {
+                const float u = ru[j].get(v);
+                s[v] = __fadd_rn(rd[j].get(v), sh.bias[run(j) + v]);
+                if (a.softplus) s[v] = softplus(s[v]);
+                if (!on) s[v] = 0.0f;
+                su[v] = __fmul_rn(s[v], u);
+                if (final) {
+                    du[j][v] = __fmul_rn(sh.skip[run(j) + v], u);
+                    gate[j][v] = a.z ? silu(rz[j].get(v)) : 1.0f;
+                }
+            }
+            Run<float, V> o;
+            o.set(s), o.store(&sh.s[row][run(j)]);
+            o.set(su), o.store(&sh.su[row][run(j)]);
+        }
+#pragma unroll
+        for (int i = 0; i < Sh::kBC; ++i) {
+            const int e = tid + i * kScanThreads;
+            if (e < kTile * Sh::kStates) {
+                (&sh.B[0][0])[e] = rB[i].get(0);
+                if (final) (&sh.C[0][0])[e] = rC[i].get(0);
+            }
+        }
+    };
+    __syncthreads();  // bias and skip
+
+    if (a.parts > 1) {
+        float sum = 0.0f;
+        fetch(first, false);
+        for (int t0 = first; t0 < last; t0 += kTile) {
+            stage(t0, false);
+            __syncthreads();
+            fetch(t0 + kTile, false);
+#pragma unroll 4
+            for (int t = 0; t < kTile; ++t) {
+                const float s = sh.s[t][c];
+                sum = __fadd_rn(sum, s);
+                advance<NS>(h, A, s, sh.su[t][c], &sh.B[t][n0]);
+            }
+            __syncthreads();
+        }
+#pragma unroll
+        for (int i = 0; i < NS; ++i) sh.part[i][tid] = i & 1 ? h[i / 2].y : h[i / 2].x;
+        sh.sum[tid] = sum;
+        cluster_arrive();
+        cluster_wait();
+#pragma unroll
+        for (int i = 0; i < NS / 2; ++i) h[i] = h0[i];
+        for (int p = 0; p < rank; ++p) {
+            const float s = peer_load(peer_address(&sh.sum[tid], p));
+#pragma unroll
+            for (int i = 0; i < NS / 2; ++i) {
+                const float x = peer_load(peer_address(&sh.part[2 * i][tid], p)), y = peer_load(peer_address(&sh.part[2 * i + 1][tid], p));
+                h[i].x = p ? __fmaf_rn(exp2_hw(__fmul_rn(s, A[i].x)), h[i].x, x) : x;
+                h[i].y = p ? __fmaf_rn(exp2_hw(__fmul_rn(s, A[i].y)), h[i].y, y) : y;
+            }
+        }
+        cluster_arrive();  // waited for at the end: the others may still read this block's part
+    }
+
+    fetch(first, true);
+    for (int t0 = first; t0 < last; t0 += kTile) {
+        stage(t0, true);
+        __syncthreads();
+        fetch(t0 + kTile, true);
+#pragma unroll(L >= 4 ? 1 : 4 / L)
+        for (int tb = 0; tb < kTile; tb += L) {
+            float y[L];
+#pragma unroll
+            for (int i = 0; i < L; ++i) {
+                advance<NS>(h, A, sh.s[tb + i][c], sh.su[tb + i][c], &sh.B[tb + i][n0]);
+                y[i] = dot<NS>(h, &sh.C[tb + i][n0]);
+            }
+            // L frames' sums over L lanes: each exchange halves the frames a lane holds, until lane q has frame tb + q
+#pragma unroll
+            for (int o = L / 2; o > 0; o >>= 1)
+#pragma unroll
+                for (int i = 0; i < o; ++i) {
+                    const float send = q & o ? y[i] : y[i + o], keep = q & o ? y[i + o] : y[i];
+                    y[i] = __fadd_rn(keep, __shfl_xor_sync(0xffffffffu, send, o));
+                }
+            sh.y[tb + q][c] = y[0];
+        }
+        __syncthreads();
+        if (t0 + row < last) {
+            T *out = static_cast<T *>(a.y) + b * a.y_seq + (t0 + row) * a.y_frame + d0;
+#pragma unroll
+            for (int j = 0; j < R; ++j) {
+                float o[V];
+#pragma unroll
+                for (int v = 0; v < V; ++v) o[v] = __fmul_rn(__fadd_rn(sh.y[row][run(j) + v], du[j][v]), gate[j][v]);
+                Run<T, V> r;
+                r.set(o);
+                const int left = chans - run(j);
+                if ((a.vec & kVecY) && left >= V)
+                    r.store(out + run(j));
+                else
+                    r.store_some(out + run(j), left);
+            }
+        }
+    }
+    if (a.state_out && rank == a.parts - 1) {
+#pragma unroll
+        for (int i = 0; i < NS; ++i)
+            if (c < chans && n0 + i < a.N) a.state_out[(b * a.D + d0 + c) * a.N + n0 + i] = i & 1 ? h[i / 2].y : h[i / 2].x;
+    }
+    if (a.parts > 1) cluster_wait();
+}
+
+bool aligned_to(const void *p, int64_t seq, int64_t frame, int e, int bytes) {
+    return reinterpret_cast<uintptr_t>(p) % bytes == 0 && seq * e % bytes == 0 && frame * e % bytes == 0;
+}
+
+template <typename T>
+qnn_status launch_step(const ScanArgs &a, cudaStream_t st) {
+    int lanes = 1;
+    while (4 * lanes < a.N) lanes *= 2;
+    const int64_t blocks = (a.B * a.D * lanes + kStepThreads - 1) / kStepThreads;
+    if (blocks > INT32_MAX) return QNN_FAIL(QNN_ERR_INVALID_ARG);
+    ssm_step_kernel<T><<<(unsigned)blocks, kStepThreads, 0, st>>>(a, lanes);
+    return QNN_OK;
+}
+
+template <typename T, int NS, int L>
+qnn_status launch_tiles(ScanArgs a, cudaStream_t st) {
+    using Sh = ScanBlock<T, NS, L>;
+    const int e = sizeof(T), bytes = Sh::V * e;
+    const bool group_ok = a.groups == 1 || a.group_chans * e % bytes == 0;
+    auto flag = [&](const void *p, int64_t seq, int64_t frame, int bit) {
+        return p && group_ok && aligned_to(p, seq, frame, e, bytes) ? bit : 0;
+    };
+    a.vec = flag(a.u, a.u_seq, a.u_frame, kVecU) | flag(a.dt, a.dt_seq, a.dt_frame, kVecDt) | flag(a.z, a.z_seq, a.z_frame, kVecZ) |
+            flag(a.y, a.y_seq, a.y_frame, kVecY);
+    const int64_t blocks_g = (a.group_chans + Sh::kChans - 1) / Sh::kChans;
+    const int64_t blocks = a.B * a.groups * blocks_g;
+    // parts: as many as give every SM six blocks, but no fewer than two tiles each
+    const int64_t tiles = (a.T + kTile - 1) / kTile;
+    int parts = 1;
+    while (parts < 16 && blocks * parts < 6 * (int64_t)sm_count() && 4 * parts <= tiles) parts *= 2;
+    if (blocks * parts > INT32_MAX || blocks_g > INT32_MAX) return QNN_FAIL(QNN_ERR_INVALID_ARG);
+    a.group_blocks = (int)blocks_g;
+    const auto kern = ssm_scan_kernel<T, NS, L>;
+    if (parts > 8) QNN_CUDA_TRY(cudaFuncSetAttribute(kern, cudaFuncAttributeNonPortableClusterSizeAllowed, 1));
+    a.parts = parts;
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3((unsigned)(blocks * parts));
+    cfg.blockDim = dim3(kScanThreads);
+    cfg.stream = st;
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeClusterDimension;
+    attr[0].val.clusterDim.x = (unsigned)parts;
+    attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = parts > 1 ? 1 : 0;
+    QNN_CUDA_TRY(cudaLaunchKernelEx(&cfg, kern, a));
+    return QNN_OK;
+}
+
+template <typename T>
+qnn_status launch_scan(ScanArgs &a, cudaStream_t st) {
+    const int e = sizeof(T);
+    a.group_chans = a.D / a.groups;
+    a.parts = 1;
+    a.vec = 0;
+    if (a.T <= kStepFrames) {
+        auto at16 = [](const void *p) { return reinterpret_cast<uintptr_t>(p) % 16 == 0; };
+        if (a.N % 4 == 0 && at16(a.A) && at16(a.state_in) && at16(a.state_out)) a.vec |= kVecStates;
+        if (a.N % 4 == 0 && aligned_to(a.Bm, a.Bm_seq, a.Bm_frame, e, 4 * e) && aligned_to(a.Cm, a.Cm_seq, a.Cm_frame, e, 4 * e))
+            a.vec |= kVecBC;
+        return launch_step<T>(a, st);
+    }
+    if (a.N <= 4) return launch_tiles<T, 4, 1>(a, st);
+    if (a.N <= 8) return launch_tiles<T, 8, 1>(a, st);
+    if (a.N <= 16) return launch_tiles<T, 8, 2>(a, st);
+    if (a.N <= 32) return launch_tiles<T, 8, 4>(a, st);
+    if (a.N <= 64) return launch_tiles<T, 8, 8>(a, st);
+    return launch_tiles<T, 8, 16>(a, st);
+}
+
+template <typename T, int WT>
+qnn_status launch_conv(ConvArgs a, cudaStream_t st) {
+    constexpr int V = 16 / (int)sizeof(T);
+    const int e = sizeof(T);
+    auto at16 = [](const void *p) { return reinterpret_cast<uintptr_t>(p) % 16 == 0; };
+    const bool vec = a.D % V == 0 && (a.T == 0 || (aligned_to(a.x, a.x_seq, a.x_frame, e, 16) && aligned_to(a.y, a.y_seq, a.y_frame, e, 16))) &&
+                     at16(a.state_in) && at16(a.state_out);
+    a.runs = vec ? a.D / V : a.D;
+    a.chunk = 32;
+    a.chunks = std::max<int64_t>(1, (a.T + a.chunk - 1) / a.chunk);
+    const int64_t blocks = (a.B * a.runs * a.chunks + kConvThreads - 1) / kConvThreads;
+    if (blocks > INT32_MAX) return QNN_FAIL(QNN_ERR_INVALID_ARG);
+    if (vec)
+        causal_conv_kernel<T, WT, V><<<(unsigned)blocks, kConvThreads, 0, st>>>(a);
+    else
+        causal_conv_kernel<T, WT, 1><<<(unsigned)blocks, kConvThreads, 0, st>>>(a);
+    return QNN_OK;
 }
 
 constexpr int64_t kMostStride = (int64_t)1 << 40, kMostCount = (int64_t)1 << 40;
@@ -145,11 +594,11 @@ extern "C" qnn_status qnn_causal_conv(const void *x, int64_t x_seq, int64_t x_fr
     ConvArgs a;
     a.x = x, a.state_in = state_in, a.state_out = state_out, a.y = y, a.w = w, a.bias = bias, a.lengths = lengths;
     a.x_seq = x_seq, a.x_frame = x_frame, a.y_seq = y_seq, a.y_frame = y_frame, a.B = B, a.T = T, a.D = D, a.W = W, a.silu = silu != 0;
-    const int64_t blocks = (B * D + 127) / 128;
-    if (blocks > INT32_MAX) return QNN_ERR_INVALID_ARG;
     cudaStream_t st = as_stream(stream);
     ProfScope prof("causal_conv", st);
-    with_type(dtype, [&](auto t) { causal_conv_plain_kernel<decltype(t)><<<(unsigned)blocks, 128, 0, st>>>(a); });
+    QNN_TRY(with_type(dtype, [&](auto t) {
+        return W <= 4 ? launch_conv<decltype(t), 4>(a, st) : launch_conv<decltype(t), kMostTaps>(a, st);
+    }));
     QNN_CUDA_TRY(cudaGetLastError());
     return QNN_OK;
 }
@@ -188,11 +637,11 @@ extern "C" qnn_status qnn_ssm_scan(const qnn_ssm_args *args, void *stream) {
     if (ys.meets(so)) return QNN_ERR_INVALID_ARG;
     for (int i = 0; i < 10; ++i)
         if (ys.meets(in[i]) || (so.meets(in[i]) && !(i == 9 && a.state_in == a.state_out))) return QNN_ERR_INVALID_ARG;
-    const int64_t blocks = (a.B * a.D + 3) / 4;
-    if (blocks > INT32_MAX) return QNN_ERR_INVALID_ARG;
+    ScanArgs k;
+    static_cast<qnn_ssm_args &>(k) = a;
     cudaStream_t st = as_stream(stream);
     ProfScope prof("ssm_scan", st);
-    with_type(a.dtype, [&](auto t) { ssm_scan_plain_kernel<decltype(t)><<<(unsigned)blocks, 128, 0, st>>>(a); });
+    QNN_TRY(with_type(a.dtype, [&](auto t) { return launch_scan<decltype(t)>(k, st); }));
     QNN_CUDA_TRY(cudaGetLastError());
     return QNN_OK;
 }
