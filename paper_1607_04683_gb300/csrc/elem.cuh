@@ -9,6 +9,7 @@
 #include <type_traits>
 
 #include "../../include/qnn.h"
+#include "qnn_device.cuh"
 
 namespace qnn {
 
@@ -135,15 +136,32 @@ __device__ __forceinline__ float silu(float v) { return __fmul_rn(v, rcp_hw(__fa
 // log(1 + exp(x)) = max(x, 0) + log(1 + e), e = exp(-|x|) in (0, 1], to a few ulp of the result also where e is small:
 // log(1 + e) = 2 atanh(q), q = e / (2 + e) <= 1/3, and atanh(q) / q as a polynomial in q^2 on [0, 1/9], fitted to
 // the series 2 (1 + q^2/3 + q^4/5 + ...) at five Chebyshev points (relative error 8e-9). A NaN stays one.
+constexpr float kAtanh0 = 2.0f, kAtanh1 = 0.6666632294654846f, kAtanh2 = 0.4002459645271301f, kAtanh3 = 0.27965158224105835f,
+                kAtanh4 = 0.28157779574394226f;
 __device__ __forceinline__ float softplus(float x) {
     const float e = exp2_hw(__fmul_rn(fabsf(x), -kLog2e));
     const float q = __fmul_rn(e, rcp_hw(__fadd_rn(2.0f, e))), s = __fmul_rn(q, q);
-    float p = 0.28157779574394226f;
-    p = __fmaf_rn(p, s, 0.27965158224105835f);
-    p = __fmaf_rn(p, s, 0.4002459645271301f);
-    p = __fmaf_rn(p, s, 0.6666632294654846f);
-    p = __fmaf_rn(p, s, 2.0f);
+    float p = __fmaf_rn(s, kAtanh4, kAtanh3);
+    p = __fmaf_rn(p, s, kAtanh2);
+    p = __fmaf_rn(p, s, kAtanh1);
+    p = __fmaf_rn(p, s, kAtanh0);
     return __fmaf_rn(p, q, fmaxf(x, 0.0f));
+}
+
+// silu and softplus of two values, in paired instructions (one issue slot for two results).
+__device__ __forceinline__ float2 silu2(float2 v) {
+    const float2 x = fmul2_rn(v, f2(-kLog2e)), d = fadd2_rn(make_float2(exp2_hw(x.x), exp2_hw(x.y)), f2(1.0f));
+    return fmul2_rn(v, make_float2(rcp_hw(d.x), rcp_hw(d.y)));
+}
+__device__ __forceinline__ float2 softplus2(float2 x) {
+    const float2 y = fmul2_rn(make_float2(fabsf(x.x), fabsf(x.y)), f2(-kLog2e));
+    const float2 e = make_float2(exp2_hw(y.x), exp2_hw(y.y)), d = fadd2_rn(e, f2(2.0f));
+    const float2 q = fmul2_rn(e, make_float2(rcp_hw(d.x), rcp_hw(d.y))), s = fmul2_rn(q, q);
+    float2 p = ffma2_rn(s, f2(kAtanh4), f2(kAtanh3));
+    p = ffma2_rn(p, s, f2(kAtanh2));
+    p = ffma2_rn(p, s, f2(kAtanh1));
+    p = ffma2_rn(p, s, f2(kAtanh0));
+    return ffma2_rn(p, q, make_float2(fmaxf(x.x, 0.0f), fmaxf(x.y, 0.0f)));
 }
 
 }  // namespace qnn

@@ -120,12 +120,13 @@ __global__ void __launch_bounds__(kConvThreads) causal_conv_kernel(const ConvArg
 constexpr int kMostStates = 128;
 
 struct ScanArgs : qnn_ssm_args {
-    int vec;              // kVec*: arrays whose runs of channels may be loaded or stored whole
+    int vec;              // (few frames) kVec*: arrays whose runs of four states may be loaded or stored whole
     int64_t group_chans;  // D / groups
-    int group_blocks;     // blocks a group
-    int parts;            // blocks (a cluster of them) that share a sequence's frames
+    int64_t units;        // warps' shares of channels, of all sequences
+    int group_blocks;     // of them a group
+    int parts;            // warps that share a unit's frames
 };
-enum { kVecU = 1, kVecDt = 2, kVecZ = 4, kVecY = 8, kVecStates = 16, kVecBC = 32 };
+enum { kVecStates = 1, kVecBC = 2 };
 
 // Few frames: no frame waits for another for long, and states are most of the traffic (8 N bytes a channel, in and out).
 // A lane holds four states of a channel, 1 .. 32 lanes a channel; each step's sum over the states by shuffles.
@@ -217,33 +218,33 @@ __device__ __forceinline__ float peer_load(uint32_t at) {
     return v;
 }
 
-// Whole sequences. A block takes 128 / L channels of one group over a part of a sequence's frames, tile by tile of kTile
-// frames: its threads load u, dt (and z) in runs of channels, form s = softplus(dt) and s u, and leave them in shared memory
+// Whole sequences, a warp by itself: 32 / L channels of one group over a part of a sequence's frames, tile by tile of kTile
+// frames. Its lanes load u, dt (and z) in runs of channels, form s = softplus(dt) and s u, and leave them in shared memory
 // beside the tile's Bm and Cm; then L lanes a channel, NS states each, carry the states over the tile's frames; then the
-// threads that loaded u and z finish the outputs. The loads of the next tile are in flight meanwhile.
+// lanes that loaded u and z finish the outputs. The next tile's loads are in flight meanwhile. No block-wide barriers: the
+// phases of a block's warps overlap.
 //
-// Where sequences are few, a cluster of `parts` blocks shares each one's frames. The recurrence is linear: over a part,
-// h' = exp(A S) h + r, with S the sum of its steps and r what it reaches from h = 0. Each block first finds S and r of its part
-// (no Cm, z or outputs), reads those of the parts before its own from their shared memory, composes its first state from
-// them, and then goes over its part once more with it.
-constexpr int kScanThreads = 128, kTile = 16;
-template <typename T, int NS, int L>
-struct ScanBlock {
-    static constexpr int kChans = kScanThreads / L;             // a block
-    static constexpr int kStates = NS * L;                      // of a channel, padded
-    static constexpr int kEach = kTile / L;                     // values a thread loads of each array
+// Where sequences are few, `parts` warps (of a block, or of a cluster of blocks) share each one's frames. The recurrence is
+// linear: over a part, h' = exp(A S) h + r, with S the sum of its steps and r what it reaches from h = 0. Each warp first
+// finds S and r of its part (no Cm, z or outputs), reads those of the parts before its own from shared memory, composes its
+// first state from them, and then goes over its part once more with it.
+constexpr int kTile = 16;
+template <int NS, int L>
+struct ScanWarp {
+    static constexpr int kChans = 32 / L;                // of a warp
+    static constexpr int kStates = NS * L;               // of a channel, padded
+    static constexpr int kEach = kTile / L;              // values a lane loads of each array
     static constexpr int V = kEach < 4 ? kEach : 4, kRuns = kEach / V;
-    static constexpr int kRowThreads = kChans / kEach;          // 8: threads a frame
-    static constexpr int kBC = (kTile * kStates + kScanThreads - 1) / kScanThreads;
-    static_assert(kRowThreads * kTile == kScanThreads, "a thread has a place in one frame of the tile");
+    static constexpr int kRowLanes = kChans / V, kRows = 32 / kRowLanes;  // lanes a frame, frames a load
+    static constexpr int kBCEach = (kTile * kStates / 4 + 31) / 32;       // runs of four a lane loads of Bm and Cm
+    static constexpr bool kBCAhead = kBCEach <= 4;       // a tile ahead, while registers allow it
+    static constexpr int kBlockWarps = kStates <= 64 ? 4 : 2;
 
-    alignas(16) float s[kTile][kChans];    // steps, then outputs' sums
-    alignas(16) float su[kTile][kChans];
-    alignas(16) float y[kTile][kChans];
+    alignas(16) float2 s[kTile][kChans];  // steps s and s u
+    alignas(16) float y[kTile][kChans];   // sums over the states
     alignas(16) float B[kTile][kStates], C[kTile][kStates];
-    alignas(16) float bias[kChans], skip[kChans];
-    alignas(16) float part[NS][kScanThreads];
-    float sum[kScanThreads];
+    float part[NS][32], sum[32];          // r and S
+    float2 start[NS / 2][32];             // the states that a part starts from, where it is the first
 };
 
 // h <- exp2(s A) h + su B for NS states, y += C h, in pairs: one instruction issues for two results (a state costs 2.5
@@ -272,35 +273,37 @@ __device__ __forceinline__ float dot(const float2 (&h)[NS / 2], const float *C) 
     return __fadd_rn(y.x, y.y);
 }
 
-template <typename T, int NS, int L>
-__global__ void __launch_bounds__(kScanThreads) ssm_scan_kernel(const ScanArgs a) {
-    using Sh = ScanBlock<T, NS, L>;
-    constexpr int V = Sh::V, R = Sh::kRuns;
-    __shared__ Sh sh;
-    const int tid = threadIdx.x;
-    const int rank = a.parts > 1 ? (int)cluster_rank() : 0;
-    int64_t rest = blockIdx.x / a.parts;
-    const int blk = (int)(rest % a.group_blocks);
-    rest /= a.group_blocks;
-    const int g = (int)(rest % a.groups);
-    const int64_t b = rest / a.groups;
-    const int64_t d0 = g * a.group_chans + (int64_t)blk * Sh::kChans;
+template <typename T, int NS, int L, bool VEC>
+__global__ void __launch_bounds__(32 * ScanWarp<NS, L>::kBlockWarps, 3) ssm_scan_kernel(const ScanArgs a) {
+    using Sh = ScanWarp<NS, L>;
+    constexpr int V = Sh::V, R = Sh::kRuns, W = Sh::kBlockWarps, BC = Sh::kBCEach;
+    __shared__ Sh all[W];
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    Sh &sh = all[warp];
+    const int64_t at = (int64_t)blockIdx.x * W + warp;
+    const int rank = (int)(at % a.parts);
+    int64_t unit = at / a.parts;
+    const bool there = unit < a.units;  // (a warp without work still takes part in the barriers)
+    if (!there) unit = 0;
+    const int blk = (int)(unit % a.group_blocks), g = (int)(unit / a.group_blocks % a.groups);
+    const int64_t b = unit / a.group_blocks / a.groups, d0 = g * a.group_chans + (int64_t)blk * Sh::kChans;
     const int chans = (int)min((int64_t)Sh::kChans, (g + 1) * a.group_chans - d0);
-    const int n = frames_of(a.lengths, b, a.T);
+    const int n = there ? frames_of(a.lengths, b, a.T) : 0;
     const int tiles = (n + kTile - 1) / kTile, each = (tiles + a.parts - 1) / a.parts * kTile;
     const int first = min(n, rank * each), last = min(n, first + each);
 
-    // this thread's place in the loads and stores: frame `row` of the tile, channels run(j) .. run(j) + V
-    const int row = tid / Sh::kRowThreads;
-    auto run = [&](int j) { return V * (tid % Sh::kRowThreads + j * Sh::kRowThreads); };
-    for (int c = tid; c < Sh::kChans; c += kScanThreads) {
-        sh.bias[c] = a.dt_bias && c < chans ? __ldg(a.dt_bias + d0 + c) : 0.0f;
-        sh.skip[c] = a.skip && c < chans ? __ldg(a.skip + d0 + c) : 0.0f;
+    // this lane's place in the loads and stores: frames row + j kRows of the tile, channels run .. run + V
+    const int row = lane / Sh::kRowLanes, run = V * (lane % Sh::kRowLanes), left = chans - run;
+    float bias[V], skip[V];
+#pragma unroll
+    for (int v = 0; v < V; ++v) {
+        bias[v] = a.dt_bias && v < left ? __ldg(a.dt_bias + d0 + run + v) : 0.0f;
+        skip[v] = a.skip && v < left ? __ldg(a.skip + d0 + run + v) : 0.0f;
     }
     // and in the recurrence: channel c, states n0 .. n0 + NS
-    const int c = tid / L, q = tid % L, n0 = q * NS;
+    const int c = lane / L, q = lane % L, n0 = q * NS;
     float2 A[NS / 2], h[NS / 2];
-    const bool start = rank == 0 && a.state_in;
+    const bool start = there && rank == 0 && a.state_in;
 #pragma unroll
     for (int i = 0; i < NS; ++i) {
         const bool ok = c < chans && n0 + i < a.N;
@@ -311,150 +314,201 @@ __global__ void __launch_bounds__(kScanThreads) ssm_scan_kernel(const ScanArgs a
         else
             A[i / 2].x = v, h[i / 2].x = s;
     }
-    float2 h0[NS / 2];
-#pragma unroll
-    for (int i = 0; i < NS / 2; ++i) h0[i] = h[i];
-
+    // the next tile's values, and where they lie
     Run<T, V> ru[R], rd[R], rz[R];
-    Run<T, 1> rB[Sh::kBC], rC[Sh::kBC];
-    auto fetch = [&](int t0, bool final) {
-        const int t = t0 + row;
-        auto get = [&](Run<T, V> *r, const void *p, int64_t seq, int64_t frame, bool vec) {
-            const T *at = static_cast<const T *>(p) + b * seq + t * frame + d0;
-#pragma unroll
-            for (int j = 0; j < R; ++j) {
-                const int left = t < last ? chans - run(j) : 0;
-                if (vec && left >= V)
-                    r[j].load(at + run(j));
-                else
-                    r[j].load_some(at + run(j), left);
-            }
+    Run<T, 4> rB[BC], rC[BC];
+    Run<T, V> cu[R];  // u of the tile at work, for its outputs
+    const T *pu, *pd, *pz, *pB, *pC;
+    auto seek = [&](int t0) {
+        auto at = [&](const void *p, int64_t seq, int64_t frame, int t, int64_t i) {
+            return static_cast<const T *>(p) + b * seq + t * frame + i;
         };
-        get(ru, a.u, a.u_seq, a.u_frame, a.vec & kVecU);
-        get(rd, a.dt, a.dt_seq, a.dt_frame, a.vec & kVecDt);
-        if (final && a.z) get(rz, a.z, a.z_seq, a.z_frame, a.vec & kVecZ);
-#pragma unroll
-        for (int i = 0; i < Sh::kBC; ++i) {
-            const int e = tid + i * kScanThreads, tt = t0 + e / Sh::kStates, k = e % Sh::kStates;
-            const bool ok = tt < last && k < a.N && e < kTile * Sh::kStates;
-            rB[i].load_some(static_cast<const T *>(a.Bm) + b * a.Bm_seq + tt * a.Bm_frame + (int64_t)g * a.N + k, ok);
-            if (final) rC[i].load_some(static_cast<const T *>(a.Cm) + b * a.Cm_seq + tt * a.Cm_frame + (int64_t)g * a.N + k, ok);
-        }
+        pu = at(a.u, a.u_seq, a.u_frame, t0 + row, d0 + run);
+        pd = at(a.dt, a.dt_seq, a.dt_frame, t0 + row, d0 + run);
+        pz = at(a.z, a.z_seq, a.z_frame, t0 + row, d0 + run);
+        pB = at(a.Bm, a.Bm_seq, a.Bm_frame, t0, (int64_t)g * a.N);
+        pC = at(a.Cm, a.Cm_seq, a.Cm_frame, t0, (int64_t)g * a.N);
     };
-    float du[R][V], gate[R][V];
-    auto stage = [&](int t0, bool final) {  // a frame that is not there has a step of 0, which leaves the states as they are
-        const bool on = t0 + row < last;
+    auto fetch_bc = [&](int t0, Run<T, 4> *r, const T *&p, int64_t frame) {
+#pragma unroll
+        for (int i = 0; i < BC; ++i) {
+            const int e = 4 * (lane + 32 * i), t = e / Sh::kStates, k = e % Sh::kStates;
+            const int count = t0 + t < last && e < kTile * Sh::kStates ? a.N - k : 0;
+            if constexpr (VEC) {
+                r[i].clear();
+                if (count > 0) r[i].load(p + t * frame + k);
+            } else {
+                r[i].load_some(p + t * frame + k, count);
+            }
+        }
+        p += kTile * frame;
+    };
+    auto get = [&](int t0, Run<T, V> *r, const T *&p, int64_t frame) {  // reads tile t0, where p stands, and moves p on
 #pragma unroll
         for (int j = 0; j < R; ++j) {
-            float s[V], su[V];
-#pragma unroll
-            for (int v = 0; v < V; ++v) {
-                const float u = ru[j].get(v);
-                s[v] = __fadd_rn(rd[j].get(v), sh.bias[run(j) + v]);
-                if (a.softplus) s[v] = softplus(s[v]);
-                if (!on) s[v] = 0.0f;
-                su[v] = __fmul_rn(s[v], u);
-                if (final) {
-                    du[j][v] = __fmul_rn(sh.skip[run(j) + v], u);
-                    gate[j][v] = a.z ? silu(rz[j].get(v)) : 1.0f;
-                }
+            const int count = t0 + row + j * Sh::kRows < last ? left : 0;
+            if constexpr (VEC) {
+                r[j].clear();
+                if (count > 0) r[j].load(p + j * Sh::kRows * frame);
+            } else {
+                r[j].load_some(p + j * Sh::kRows * frame, count);
             }
-            Run<float, V> o;
-            o.set(s), o.store(&sh.s[row][run(j)]);
-            o.set(su), o.store(&sh.su[row][run(j)]);
+        }
+        p += kTile * frame;
+    };
+    auto fetch = [&](int t0, bool final) {
+        get(t0, ru, pu, a.u_frame);
+        get(t0, rd, pd, a.dt_frame);
+        if constexpr (Sh::kBCAhead) {
+            fetch_bc(t0, rB, pB, a.Bm_frame);
+            if (final) fetch_bc(t0, rC, pC, a.Cm_frame);
+        }
+    };
+    auto stage = [&](int t0, bool final) {  // a frame that is not there has a step of 0, which leaves the states as they are
+        if constexpr (!Sh::kBCAhead) {
+            fetch_bc(t0, rB, pB, a.Bm_frame);
+            if (final) fetch_bc(t0, rC, pC, a.Cm_frame);
         }
 #pragma unroll
-        for (int i = 0; i < Sh::kBC; ++i) {
-            const int e = tid + i * kScanThreads;
+        for (int j = 0; j < R; ++j) {
+            const int r = row + j * Sh::kRows;
+            const bool on = t0 + r < last;
+#pragma unroll
+            for (int v = 0; v < V; v += 2) {
+                const int w = v + 1 < V ? v + 1 : v;
+                const float2 u = make_float2(ru[j].get(v), ru[j].get(w));
+                float2 s = fadd2_rn(make_float2(rd[j].get(v), rd[j].get(w)), make_float2(bias[v], bias[w]));
+                if (a.softplus) s = softplus2(s);
+                if (!on) s = make_float2(0.0f, 0.0f);
+                const float2 su = fmul2_rn(s, u);
+                if constexpr (V > 1)
+                    *reinterpret_cast<float4 *>(&sh.s[r][run + v]) = make_float4(s.x, su.x, s.y, su.y);
+                else
+                    sh.s[r][run] = make_float2(s.x, su.x);
+            }
+        }
+#pragma unroll
+        for (int i = 0; i < BC; ++i) {
+            const int e = 4 * (lane + 32 * i);
             if (e < kTile * Sh::kStates) {
-                (&sh.B[0][0])[e] = rB[i].get(0);
-                if (final) (&sh.C[0][0])[e] = rC[i].get(0);
+                *reinterpret_cast<float4 *>(&sh.B[0][0] + e) = make_float4(rB[i].get(0), rB[i].get(1), rB[i].get(2), rB[i].get(3));
+                if (final)
+                    *reinterpret_cast<float4 *>(&sh.C[0][0] + e) = make_float4(rC[i].get(0), rC[i].get(1), rC[i].get(2), rC[i].get(3));
             }
         }
     };
-    __syncthreads();  // bias and skip
 
     if (a.parts > 1) {
+#pragma unroll
+        for (int i = 0; i < NS / 2; ++i) sh.start[i][lane] = h[i];
         float sum = 0.0f;
+        seek(first);
         fetch(first, false);
         for (int t0 = first; t0 < last; t0 += kTile) {
             stage(t0, false);
-            __syncthreads();
+            __syncwarp();
             fetch(t0 + kTile, false);
 #pragma unroll 4
             for (int t = 0; t < kTile; ++t) {
-                const float s = sh.s[t][c];
-                sum = __fadd_rn(sum, s);
-                advance<NS>(h, A, s, sh.su[t][c], &sh.B[t][n0]);
+                const float2 s = sh.s[t][c];
+                sum = __fadd_rn(sum, s.x);
+                advance<NS>(h, A, s.x, s.y, &sh.B[t][n0]);
             }
+            __syncwarp();
+        }
+#pragma unroll
+        for (int i = 0; i < NS; ++i) sh.part[i][lane] = i & 1 ? h[i / 2].y : h[i / 2].x;
+        sh.sum[lane] = sum;
+        const bool cluster = a.parts > W;
+        if (cluster) {
+            cluster_arrive();
+            cluster_wait();
+        } else {
             __syncthreads();
         }
 #pragma unroll
-        for (int i = 0; i < NS; ++i) sh.part[i][tid] = i & 1 ? h[i / 2].y : h[i / 2].x;
-        sh.sum[tid] = sum;
-        cluster_arrive();
-        cluster_wait();
-#pragma unroll
-        for (int i = 0; i < NS / 2; ++i) h[i] = h0[i];
+        for (int i = 0; i < NS / 2; ++i) h[i] = sh.start[i][lane];
+        const int w0 = warp - rank;  // (in one block) the first part's warp
         for (int p = 0; p < rank; ++p) {
-            const float s = peer_load(peer_address(&sh.sum[tid], p));
+            const Sh &its = all[cluster ? p % W : w0 + p];
+            auto get = [&](const float &v) { return cluster ? peer_load(peer_address(&v, p / W)) : v; };
+            const float s = get(its.sum[lane]);
 #pragma unroll
             for (int i = 0; i < NS / 2; ++i) {
-                const float x = peer_load(peer_address(&sh.part[2 * i][tid], p)), y = peer_load(peer_address(&sh.part[2 * i + 1][tid], p));
+                const float x = get(its.part[2 * i][lane]), y = get(its.part[2 * i + 1][lane]);
                 h[i].x = p ? __fmaf_rn(exp2_hw(__fmul_rn(s, A[i].x)), h[i].x, x) : x;
                 h[i].y = p ? __fmaf_rn(exp2_hw(__fmul_rn(s, A[i].y)), h[i].y, y) : y;
             }
         }
-        cluster_arrive();  // waited for at the end: the others may still read this block's part
+        if (cluster) cluster_arrive();  // waited for at the end: the others may still read this block's parts
     }
 
+    constexpr int kSteps = L > 8 ? L : 8;  // frames between stores: their loads and products overlap
+    seek(first);
     fetch(first, true);
+    T *py = static_cast<T *>(a.y) + b * a.y_seq + (first + row) * a.y_frame + d0 + run;
     for (int t0 = first; t0 < last; t0 += kTile) {
         stage(t0, true);
-        __syncthreads();
-        fetch(t0 + kTile, true);
-#pragma unroll(L >= 4 ? 1 : 4 / L)
-        for (int tb = 0; tb < kTile; tb += L) {
-            float y[L];
 #pragma unroll
-            for (int i = 0; i < L; ++i) {
-                advance<NS>(h, A, sh.s[tb + i][c], sh.su[tb + i][c], &sh.B[tb + i][n0]);
+        for (int j = 0; j < R; ++j) cu[j] = ru[j];
+        if (a.z) get(t0, rz, pz, a.z_frame);  // for the outputs, after the steps
+        __syncwarp();
+        fetch(t0 + kTile, true);
+#pragma unroll 1
+        for (int tb = 0; tb < kTile; tb += kSteps) {
+            float y[kSteps];
+#pragma unroll
+            for (int i = 0; i < kSteps; ++i) {
+                const float2 s = sh.s[tb + i][c];
+                advance<NS>(h, A, s.x, s.y, &sh.B[tb + i][n0]);
                 y[i] = dot<NS>(h, &sh.C[tb + i][n0]);
             }
-            // L frames' sums over L lanes: each exchange halves the frames a lane holds, until lane q has frame tb + q
+            // the sums of L frames at a time over L lanes: each exchange halves the frames a lane holds, until lane q has
+            // frame q of them
 #pragma unroll
-            for (int o = L / 2; o > 0; o >>= 1)
+            for (int f = 0; f < kSteps; f += L) {
 #pragma unroll
-                for (int i = 0; i < o; ++i) {
-                    const float send = q & o ? y[i] : y[i + o], keep = q & o ? y[i + o] : y[i];
-                    y[i] = __fadd_rn(keep, __shfl_xor_sync(0xffffffffu, send, o));
-                }
-            sh.y[tb + q][c] = y[0];
-        }
-        __syncthreads();
-        if (t0 + row < last) {
-            T *out = static_cast<T *>(a.y) + b * a.y_seq + (t0 + row) * a.y_frame + d0;
+                for (int o = L / 2; o > 0; o >>= 1)
 #pragma unroll
-            for (int j = 0; j < R; ++j) {
-                float o[V];
-#pragma unroll
-                for (int v = 0; v < V; ++v) o[v] = __fmul_rn(__fadd_rn(sh.y[row][run(j) + v], du[j][v]), gate[j][v]);
-                Run<T, V> r;
-                r.set(o);
-                const int left = chans - run(j);
-                if ((a.vec & kVecY) && left >= V)
-                    r.store(out + run(j));
-                else
-                    r.store_some(out + run(j), left);
+                    for (int i = 0; i < o; ++i) {
+                        const float send = q & o ? y[f + i] : y[f + i + o], keep = q & o ? y[f + i + o] : y[f + i];
+                        y[f + i] = __fadd_rn(keep, __shfl_xor_sync(0xffffffffu, send, o));
+                    }
+                sh.y[tb + f + q][c] = y[f];
             }
         }
+        __syncwarp();
+#pragma unroll
+        for (int j = 0; j < R; ++j) {
+            const int r = row + j * Sh::kRows;
+            if (t0 + r < last) {
+                float o[V];
+#pragma unroll
+                for (int v = 0; v < V; v += 2) {
+                    const int w = v + 1 < V ? v + 1 : v;
+                    float2 y = ffma2_rn(make_float2(skip[v], skip[w]), make_float2(cu[j].get(v), cu[j].get(w)),
+                                        make_float2(sh.y[r][run + v], sh.y[r][run + w]));
+                    if (a.z) y = fmul2_rn(y, silu2(make_float2(rz[j].get(v), rz[j].get(w))));
+                    o[v] = y.x;
+                    if (w > v) o[w] = y.y;
+                }
+                Run<T, V> out;
+                out.set(o);
+                if constexpr (VEC) {
+                    if (left > 0) out.store(py + j * Sh::kRows * a.y_frame);
+                } else {
+                    out.store_some(py + j * Sh::kRows * a.y_frame, left);
+                }
+            }
+        }
+        py += kTile * a.y_frame;
     }
-    if (a.state_out && rank == a.parts - 1) {
+    if (there && a.state_out && rank == a.parts - 1) {
 #pragma unroll
         for (int i = 0; i < NS; ++i)
             if (c < chans && n0 + i < a.N) a.state_out[(b * a.D + d0 + c) * a.N + n0 + i] = i & 1 ? h[i / 2].y : h[i / 2].x;
     }
-    if (a.parts > 1) cluster_wait();
+    if (a.parts > W) cluster_wait();
 }
 
 bool aligned_to(const void *p, int64_t seq, int64_t frame, int e, int bytes) {
@@ -473,35 +527,37 @@ qnn_status launch_step(const ScanArgs &a, cudaStream_t st) {
 
 template <typename T, int NS, int L>
 qnn_status launch_tiles(ScanArgs a, cudaStream_t st) {
-    using Sh = ScanBlock<T, NS, L>;
-    const int e = sizeof(T), bytes = Sh::V * e;
-    const bool group_ok = a.groups == 1 || a.group_chans * e % bytes == 0;
-    auto flag = [&](const void *p, int64_t seq, int64_t frame, int bit) {
-        return p && group_ok && aligned_to(p, seq, frame, e, bytes) ? bit : 0;
-    };
-    a.vec = flag(a.u, a.u_seq, a.u_frame, kVecU) | flag(a.dt, a.dt_seq, a.dt_frame, kVecDt) | flag(a.z, a.z_seq, a.z_frame, kVecZ) |
-            flag(a.y, a.y_seq, a.y_frame, kVecY);
+    using Sh = ScanWarp<NS, L>;
+    constexpr int W = Sh::kBlockWarps;
+    const int e = sizeof(T);
+    // runs of channels and of states are loaded and stored whole where every one of them is aligned and full
+    auto whole = [&](const void *p, int64_t seq, int64_t frame, int values) { return !p || aligned_to(p, seq, frame, e, values * e); };
+    const bool vec = a.group_chans % Sh::V == 0 && a.N % 4 == 0 && whole(a.u, a.u_seq, a.u_frame, Sh::V) &&
+                     whole(a.dt, a.dt_seq, a.dt_frame, Sh::V) && whole(a.z, a.z_seq, a.z_frame, Sh::V) &&
+                     whole(a.y, a.y_seq, a.y_frame, Sh::V) && whole(a.Bm, a.Bm_seq, a.Bm_frame, 4) && whole(a.Cm, a.Cm_seq, a.Cm_frame, 4);
     const int64_t blocks_g = (a.group_chans + Sh::kChans - 1) / Sh::kChans;
-    const int64_t blocks = a.B * a.groups * blocks_g;
-    // parts: as many as give every SM six blocks, but no fewer than two tiles each
+    a.units = a.B * a.groups * blocks_g;
+    a.group_blocks = (int)blocks_g;
+    // parts: while the SMs have fewer than four warps each, but no fewer than two tiles a part
     const int64_t tiles = (a.T + kTile - 1) / kTile;
     int parts = 1;
-    while (parts < 16 && blocks * parts < 6 * (int64_t)sm_count() && 4 * parts <= tiles) parts *= 2;
-    if (blocks * parts > INT32_MAX || blocks_g > INT32_MAX) return QNN_FAIL(QNN_ERR_INVALID_ARG);
-    a.group_blocks = (int)blocks_g;
-    const auto kern = ssm_scan_kernel<T, NS, L>;
-    if (parts > 8) QNN_CUDA_TRY(cudaFuncSetAttribute(kern, cudaFuncAttributeNonPortableClusterSizeAllowed, 1));
+    while (parts < 16 * W && a.units * parts < 4 * (int64_t)sm_count() && 4 * parts <= tiles) parts *= 2;
+    const int64_t blocks = (a.units * parts + W - 1) / W;
+    if (blocks > INT32_MAX) return QNN_FAIL(QNN_ERR_INVALID_ARG);
+    const auto kern = vec ? ssm_scan_kernel<T, NS, L, true> : ssm_scan_kernel<T, NS, L, false>;
+    const int cluster = std::max(1, parts / W);
+    if (cluster > 8) QNN_CUDA_TRY(cudaFuncSetAttribute(kern, cudaFuncAttributeNonPortableClusterSizeAllowed, 1));
     a.parts = parts;
     cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3((unsigned)(blocks * parts));
-    cfg.blockDim = dim3(kScanThreads);
+    cfg.gridDim = dim3((unsigned)blocks);
+    cfg.blockDim = dim3(32 * W);
     cfg.stream = st;
     cudaLaunchAttribute attr[1];
     attr[0].id = cudaLaunchAttributeClusterDimension;
-    attr[0].val.clusterDim.x = (unsigned)parts;
+    attr[0].val.clusterDim.x = (unsigned)cluster;
     attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
     cfg.attrs = attr;
-    cfg.numAttrs = parts > 1 ? 1 : 0;
+    cfg.numAttrs = cluster > 1 ? 1 : 0;
     QNN_CUDA_TRY(cudaLaunchKernelEx(&cfg, kern, a));
     return QNN_OK;
 }

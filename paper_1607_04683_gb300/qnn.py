@@ -262,39 +262,45 @@ def qnn_qmatmul(A, pa, ga, rsA, W, pw, csW, n_blocks=1, bias=None, want_acc=Fals
     return Y, acc
 
 
-def _want(ok: bool, what: str):
-    if not ok:
-        raise ValueError(what)
+def _bad(what: str, *more):
+    """Raises; messages are put together only here (a formatted type alone costs a microsecond)."""
+    raise ValueError(what + "".join(f" {tuple(m) if isinstance(m, (tuple, list)) else m}" for m in more))
 
 
 def _dtype(t, what: str) -> int:
     d = _DTYPES.get(str(t.dtype))
-    _want(d is not None, f"{what}: fp32, bf16 or fp16")
+    if d is None:
+        _bad(f"{what}: fp32, bf16 or fp16")
     return d
 
 
 def _rows(t, what: str, dtype, shape) -> int:
     """Leading dimension of a matrix whose rows are contiguous."""
-    _want(t.dtype == dtype and t.shape == shape, f"{what}: {dtype} {tuple(shape)}")
+    if t.dtype is not dtype or t.shape != shape:
+        _bad(what + ":", dtype, shape)
     s0, s1 = t.stride()
-    _want((s1 == 1 or shape[1] <= 1) and (s0 >= shape[1] or shape[0] <= 1), f"{what}: rows of contiguous values, apart")
-    return s0 if s0 >= shape[1] else shape[1]
+    cols = shape[1]
+    if (s1 != 1 and cols > 1) or (s0 < cols and shape[0] > 1):
+        _bad(what + ": rows of contiguous values, apart")
+    return s0 if s0 >= cols else cols
 
 
 def _flat(t, what: str, dtype, shape):
-    """A contiguous array, or None."""
-    _want(t is None or (t.dtype == dtype and t.shape == shape and t.is_contiguous()), f"{what}: contiguous {dtype} {tuple(shape)}")
-    return None if t is None else t.data_ptr()
+    """Address of a contiguous array, or None."""
+    if t is None:
+        return None
+    if t.dtype is not dtype or t.shape != shape or not t.is_contiguous():
+        _bad(what + ": contiguous", dtype, shape)
+    return t.data_ptr()
 
 
 def _frames(t, what: str, dtype, shape):
     """Address, sequence stride and frame stride of [B, T, ...] values whose frames are contiguous."""
-    _want(t.dtype == dtype and t.shape == shape, f"{what}: {dtype} {tuple(shape)}")
+    if t.dtype is not dtype or t.shape != shape:
+        _bad(what + ":", dtype, shape)
     st = t.stride()
-    width = 1
-    for n, s in zip(reversed(shape[2:]), reversed(st[2:])):
-        _want(s == width or n <= 1, f"{what}: frames of contiguous values")
-        width *= n
+    if (st[-1] != 1 and shape[-1] > 1) or (len(st) == 4 and st[2] != shape[3] and shape[2] > 1):
+        _bad(what + ": frames of contiguous values")
     return t.data_ptr(), st[0], st[1]
 
 
@@ -314,22 +320,33 @@ def qnn_rmsnorm_quantize(x, weight, residual=None, eps=1e-5, residual_out=None, 
     residual in x's type (residual_out, which may be x or residual, or a new tensor; None without a residual), values the
     fp32 values that the codes stand for (None unless wanted)."""
     import torch
-    _want(x.dim() == 2 and x.is_cuda, "x: a CUDA matrix")
+    if x.dim() != 2 or not x.is_cuda:
+        _bad("x: a CUDA matrix")
     dt = _dtype(x, "x")
     rows, cols = shape = x.shape
     ldx = _rows(x, "x", x.dtype, shape)
     ldr = _rows(residual, "residual", x.dtype, shape) if residual is not None else 0
-    _want(residual_out is None or residual is not None, "residual_out: needs a residual")
-    h = residual_out if residual_out is not None or residual is None else _result(shape, x.dtype, x, stream)
+    if residual_out is not None and residual is None:
+        _bad("residual_out: needs a residual")
+    dev, empty = x.device, torch.empty
+    h = residual_out
+    if residual is not None and h is None:
+        h = empty(shape, dtype=x.dtype, device=dev)
     ldh = _rows(h, "residual_out", x.dtype, shape) if h is not None else 0
     w = _flat(weight, "weight", torch.float32, (cols,))
-    codes = _result(shape, torch.uint8, x, stream)
-    params = _result((rows, 4), torch.int32, x, stream)
-    sums = _result((rows,), torch.int32, x, stream)
-    values = _result(shape, torch.float32, x, stream) if want_values else None
-    _check(lib().qnn_rmsnorm_quantize(x.data_ptr(), ldx, _p(residual), ldr, dt, w, eps, rows, cols, _p(h), ldh,
-                                      codes.data_ptr(), cols, params.data_ptr(), sums.data_ptr(), _p(values), cols,
-                                      _stream(stream)), "qnn_rmsnorm_quantize")
+    codes = empty(shape, dtype=torch.uint8, device=dev)
+    params = empty((rows, 4), dtype=torch.int32, device=dev)
+    sums = empty((rows,), dtype=torch.int32, device=dev)
+    values = empty(shape, dtype=torch.float32, device=dev) if want_values else None
+    if stream is not None:
+        for t in (h, codes, params, sums, values):
+            if t is not None:
+                t.record_stream(stream)
+    st = lib().qnn_rmsnorm_quantize(x.data_ptr(), ldx, None if residual is None else residual.data_ptr(), ldr, dt, w, eps, rows,
+                                    cols, None if h is None else h.data_ptr(), ldh, codes.data_ptr(), cols, params.data_ptr(),
+                                    sums.data_ptr(), None if values is None else values.data_ptr(), cols, _stream(stream))
+    if st != QNN_OK:
+        _check(st, "qnn_rmsnorm_quantize")
     return codes, params, sums, h, values
 
 
@@ -341,7 +358,8 @@ class Weights4:
 
     def __init__(self, codes, units, row_sums, N: int, K: int, group: int):
         import torch
-        _want(group in (32, 64, 128), "group: 32, 64 or 128")
+        if group not in (32, 64, 128):
+            _bad("group: 32, 64 or 128")
         tiles = ((N + 15) // 16, (K + 127) // 128)
         _flat(codes, "codes", torch.uint8, (*tiles, 1024))
         _flat(units, "units", torch.bfloat16, (*tiles, 16, 128 // group, 2))
@@ -352,8 +370,10 @@ class Weights4:
 def qnn_quantize4(w, group: int = 64, stream=None) -> Weights4:
     """Weights w, CUDA fp32 [N, K], to 4-bit codes offline, one unit per group (32, 64 or 128) of a row's columns."""
     import torch
-    _want(w.dim() == 2 and w.is_cuda, "w: a CUDA matrix")
-    _want(group in (32, 64, 128), "group: 32, 64 or 128")
+    if w.dim() != 2 or not w.is_cuda:
+        _bad("w: a CUDA matrix")
+    if group not in (32, 64, 128):
+        _bad("group: 32, 64 or 128")
     N, K = w.shape
     ldw = _rows(w, "w", torch.float32, w.shape)
     tiles = ((N + 15) // 16, (K + 127) // 128)
@@ -369,7 +389,8 @@ def qnn_qmatmul4(A, pa, weights: Weights4, ga=PER_ROW, bias=None, out=None, stre
     """Y = R(A' W'^T) + bias with 4-bit weights: A u8 [M, K] codes with their units pa int32 [M, 4] (or [1, 4] with
     ga = PER_MATRIX), as qnn_quantize and qnn_rmsnorm_quantize give them. Returns Y fp32 [M, N]."""
     import torch
-    _want(A.dim() == 2 and A.is_cuda and A.shape[1] == weights.K, "A: a CUDA matrix of the weights' K columns")
+    if A.dim() != 2 or not A.is_cuda or A.shape[1] != weights.K:
+        _bad("A: a CUDA matrix of the weights' K columns")
     M, K = A.shape
     N = weights.N
     lda = _rows(A, "A", torch.uint8, A.shape)
@@ -388,10 +409,12 @@ def qnn_causal_conv(x, weight, bias=None, silu=True, state_in=None, state_out=No
     may be state_in), lengths int32 [B]. Returns out, [B, T, D]; without an out given, the frames behind a sequence's end
     hold nothing in particular."""
     import torch
-    _want(x.dim() == 3 and x.is_cuda, "x: CUDA [B, T, D]")
+    if x.dim() != 3 or not x.is_cuda:
+        _bad("x: CUDA [B, T, D]")
     dt = _dtype(x, "x")
     B, T, D = shape = x.shape
-    _want(weight.dim() == 2, "weight: [D, W]")
+    if weight.dim() != 2:
+        _bad("weight: [D, W]")
     W = weight.shape[1]
     y = out if out is not None else _result(shape, x.dtype, x, stream)
     _check(lib().qnn_causal_conv(*_frames(x, "x", x.dtype, shape), dt, B, T, D, _flat(weight, "weight", torch.float32, (D, W)), W,
@@ -410,11 +433,13 @@ def qnn_ssm_scan(u, dt, A, B, C, D=None, z=None, dt_bias=None, softplus=True, st
     state_in), lengths int32 [B]. Returns out, [B, T, D]; without an out given, the frames behind a sequence's end hold
     nothing in particular."""
     import torch
-    _want(u.dim() == 3 and u.is_cuda, "u: CUDA [B, T, D]")
+    if u.dim() != 3 or not u.is_cuda:
+        _bad("u: CUDA [B, T, D]")
     ty, f32 = u.dtype, torch.float32
     kind = _dtype(u, "u")
     nb, nt, nd = shape = u.shape
-    _want(A.dim() == 2, "A: [D, N]")
+    if A.dim() != 2:
+        _bad("A: [D, N]")
     ns = A.shape[1]
     groups = B.shape[2] if B.dim() == 4 else 1
     bc = (nb, nt, groups, ns) if B.dim() == 4 else (nb, nt, ns)
