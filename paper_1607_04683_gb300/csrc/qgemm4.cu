@@ -109,6 +109,14 @@ __device__ __forceinline__ uint32_t hfma2_bits(uint32_t x, uint32_t m, uint32_t 
 }
 __device__ __forceinline__ uint32_t both(float v) { return __half_as_ushort(__float2half_rn(v)) * 0x10001u; }
 
+// Two 8-bit codes b (the bytes of v that sel picks, 4: the byte 0x64) as 16 (b - 128) and as b - 128.
+__device__ __forceinline__ uint32_t codes_x16(uint32_t v, uint32_t sel) {
+    return hfma2_bits(__byte_perm(v, 0x64646464u, sel), both(16.0f), both(-18432.0f));
+}
+__device__ __forceinline__ uint32_t codes_x1(uint32_t v, uint32_t sel) {
+    return hfma2_bits(__byte_perm(v, 0x64646464u, sel), both(1.0f), both(-1152.0f));
+}
+
 // The products run on the fp16 tensor-core instruction, exactly, on codes that cost next to nothing to convert:
 //   - a 4-bit code masked out of its word in place is a subnormal fp16 number, code 2^-24 in a half's lowest four bits and
 //     16 code 2^-24 in the next four (0x000f000f and 0x00f000f0 give two of a word's eight columns each; one shift gives the
@@ -118,12 +126,21 @@ __device__ __forceinline__ uint32_t both(float v) { return __half_as_ushort(__fl
 // So every product is (b - 128) code 2^-20, and a group's sum, below 2^24 of that unit, is exact in fp32. The sum of a
 // group starts from offset x (sum of b - 128) and is taken into the output's sum by its scale, in fp32.
 //
-// A block's 16 warps split the columns of its row tiles (each of the `segments` a part of every stretch of as many tiles, so
-// that a block reads long contiguous stretches) and add up through shared memory at the end, in a fixed order. RT row tiles
-// a warp share the converted activations. Bound: the weights' bytes; the loads of the next column tile are in flight
-// while one is worked on.
+// A block's 16 warps split the columns of its row tiles (`segments` of them, tile by tile in turn, so that a block reads long
+// contiguous stretches) and add up through shared memory at the end, in a fixed order. Bound: the weights' bytes. Each
+// warp streams its own column tiles through kStages slots of shared memory by asynchronous copies, across row tiles, so that
+// 16 kStages KB a block are in flight at any time; a slot is read into registers and filled again before its products.
 constexpr int kMmThreads = 512, kMmWarps = kMmThreads / 32, kRedStride = 20;
 constexpr float kUnit = 0x1p-20f, kPerUnit = 0x1p20f;
+
+__device__ __forceinline__ void copy16_async(uint32_t to, const void *from) {
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(to), "l"(from) : "memory");
+}
+__device__ __forceinline__ void copies_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int N>
+__device__ __forceinline__ void copies_wait() {  // until all but the last N groups are there
+    asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory");
+}
 
 template <int GROUP>
 struct Units {  // of a row's 128 columns
@@ -131,202 +148,241 @@ struct Units {  // of a row's 128 columns
     uint32_t u[kCount];
     __device__ __forceinline__ void load(const uint32_t *p) {
         if constexpr (kCount == 4) {
-            const uint4 v = __ldg(reinterpret_cast<const uint4 *>(p));
+            const uint4 v = *reinterpret_cast<const uint4 *>(p);
             u[0] = v.x, u[1] = v.y, u[2] = v.z, u[3] = v.w;
         } else if constexpr (kCount == 2) {
-            const uint2 v = __ldg(reinterpret_cast<const uint2 *>(p));
+            const uint2 v = *reinterpret_cast<const uint2 *>(p);
             u[0] = v.x, u[1] = v.y;
         } else {
-            u[0] = __ldg(p);
+            u[0] = *p;
         }
     }
 };
 
-template <int GROUP, int NT, int RT>
+template <int GROUP, int NT>
+struct Mm4Plan {
+    static constexpr int kRows = 8 * NT, kGroups = kTileCols / GROUP;
+    static constexpr int kStages = NT == 1 ? 3 : 2;
+    static constexpr int kUnitBytes = kTileRows * kGroups * 4, kSlot = kTileBytes + kUnitBytes;
+    static constexpr int kRing = kMmWarps * kStages * kSlot;
+    static constexpr int kReds = NT == 1 ? 2 : 1, kRed = kMmWarps * kRows * kRedStride * 4;  // two: one barrier a row tile
+    // shared memory: the slots, the warps' sums, A's codes, their group sums
+};
+
+template <int GROUP, int NT, bool F16>
 __global__ void __launch_bounds__(kMmThreads, 1) qmatmul4_kernel(const Mm4Args a) {
+    using P = Mm4Plan<GROUP, NT>;
+    constexpr int kRows = P::kRows, kGroups = P::kGroups;
     extern __shared__ __align__(16) uint8_t smem[];
-    constexpr int kRows = 8 * NT, kGroups = kTileCols / GROUP;
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, g = lane >> 2, t = lane & 3;
     const int64_t m0 = (int64_t)blockIdx.y * kRows;
     const int rows = (int)min((int64_t)kRows, a.M - m0);
-    uint8_t *sA = smem;                                              // [rows][stride]
+    uint8_t *ring = smem + warp * P::kStages * P::kSlot;
+    float *reds = reinterpret_cast<float *>(smem + P::kRing);        // [kReds][warps][kRows][kRedStride]
+    uint8_t *sA = smem + P::kRing + P::kReds * P::kRed;              // [rows][stride]
     float *sR = reinterpret_cast<float *>(sA + rows * a.stride);     // [chunk groups][kRows]: group sums of b - 128
-    float *red = sR + a.chunk * kGroups * kRows;                     // [warps][RT][kRows][kRedStride]
     const int seg = warp % a.segments, tile_group = warp / a.segments, tile_groups = kMmWarps / a.segments;
     const int64_t ntiles = (a.N + kTileRows - 1) / kTileRows;
     const int chunks = (a.ktiles + a.chunk - 1) / a.chunk;
 
-    struct Tile {
-        uint4 w[RT][2];
-        Units<GROUP> u[RT][2];
+    // the copies' place: the next of `left` column tiles of this warp's row tile of item_next
+    const uint32_t ring_at = (uint32_t)__cvta_generic_to_shared(ring) + 16 * lane;
+    const int steps = seg < a.ktiles ? (a.ktiles - 1 - seg) / a.segments + 1 : 0;
+    int64_t item_next = blockIdx.x;
+    int left = 0;
+    const uint8_t *code_next = nullptr, *unit_next = nullptr;
+    auto seek = [&]() {
+        const int64_t tile = item_next * tile_groups + tile_group, at = tile * a.ktiles + seg;
+        left = item_next < a.items && tile < ntiles ? steps : 0;
+        code_next = a.codes + at * kTileBytes + 16 * lane;
+        unit_next = reinterpret_cast<const uint8_t *>(a.units) + at * P::kUnitBytes + 16 * lane;
     };
-    for (int64_t item = blockIdx.x; item < a.items; item += gridDim.x) {
-        const int64_t tile0 = (item * tile_groups + tile_group) * RT;
-        auto load = [&](Tile &x, int kt, int end) {
-#pragma unroll
-            for (int r = 0; r < RT; ++r) {
-                if (kt < end && tile0 + r < ntiles) {
-                    const int64_t at = (tile0 + r) * a.ktiles + kt;
-                    const uint4 *p = reinterpret_cast<const uint4 *>(a.codes + at * kTileBytes) + lane;
-                    x.w[r][0] = __ldg(p), x.w[r][1] = __ldg(p + 32);
-                    const uint32_t *q = a.units + (at * kTileRows + g) * kGroups;
-                    x.u[r][0].load(q), x.u[r][1].load(q + 8 * kGroups);
-                }
+    seek();
+    auto issue = [&](int slot) {
+        if (left > 0) {
+            const uint32_t to = ring_at + slot * P::kSlot;
+            copy16_async(to, code_next);
+            copy16_async(to + 512, code_next + 512);
+            if (16 * lane < P::kUnitBytes) copy16_async(to + kTileBytes, unit_next);
+            code_next += a.segments * kTileBytes;
+            unit_next += a.segments * P::kUnitBytes;
+            if (--left == 0) {
+                item_next += gridDim.x;
+                seek();
             }
-        };
-        float acc[RT][NT][4] = {};
+        }
+        copies_commit();
+    };
+#pragma unroll
+    for (int i = 0; i < P::kStages; ++i) issue(i);
+    int slot = 0, red_at = 0;
+    // what this thread's first output of a row tile needs is loaded ahead
+    const int wide = tile_groups * kTileRows;
+    const bool mine = tid < wide * rows;
+    qnn_qparams my_unit = {};
+    if (mine) my_unit = a.pa[a.per_row ? m0 + tid / wide : 0];
+
+    for (int64_t item = blockIdx.x; item < a.items; item += gridDim.x) {
+        float acc[NT][4] = {}, my_sum = 0.0f, my_bias = 0.0f;
+        if (const int64_t n = item * wide + tid % wide; mine && n < a.N) {
+            my_sum = __ldg(a.row_sums + n);
+            if (a.bias) my_bias = __ldg(a.bias + n);
+        }
         for (int chunk = 0; chunk < chunks; ++chunk) {
             const int kt0 = chunk * a.chunk, kt1 = min(a.ktiles, kt0 + a.chunk);
-            Tile next;
-            load(next, kt0 + seg, kt1);
             if (chunks > 1 || item == blockIdx.x) {
                 if (chunk > 0 || item != blockIdx.x) __syncthreads();  // all warps are done with what was there
-                // A's codes, 16 a step; past K, 128, which counts 0
-                const int blocks = (kt1 - kt0) * (kTileCols / 16);
-                for (int i = tid; i < rows * blocks; i += kMmThreads) {
-                    const int m = i / blocks, k = kt0 * kTileCols + 16 * (i % blocks);
-                    const uint8_t *p = a.A + (m0 + m) * a.lda + k;
-                    uint32_t v[4];
-                    if (a.align == 16 && k + 16 <= a.K) {
-                        const uint4 x = __ldg(reinterpret_cast<const uint4 *>(p));
-                        v[0] = x.x, v[1] = x.y, v[2] = x.z, v[3] = x.w;
-                    } else {
+                // A's codes, 16 a thread (past K: 128, which counts 0), and their sums by groups, over 2 to 8 lanes
+                const int blocks = (kt1 - kt0) * (kTileCols / 16), total = rows * blocks;
+                for (int i0 = 0; i0 < total; i0 += kMmThreads) {
+                    const int i = i0 + tid, m = i / blocks, blk = i % blocks, k = kt0 * kTileCols + 16 * blk;
+                    uint32_t v[4] = {0x80808080u, 0x80808080u, 0x80808080u, 0x80808080u};
+                    if (i < total) {
+                        const uint8_t *p = a.A + (m0 + m) * a.lda + k;
+                        if (a.align == 16 && k + 16 <= a.K) {
+                            const uint4 x = __ldg(reinterpret_cast<const uint4 *>(p));
+                            v[0] = x.x, v[1] = x.y, v[2] = x.z, v[3] = x.w;
+                        } else {
 #pragma unroll
-                        for (int j = 0; j < 4; ++j) {
-                            if (a.align >= 4 && k + 4 * j + 4 <= a.K) {
-                                v[j] = __ldg(reinterpret_cast<const uint32_t *>(p + 4 * j));
-                            } else {
-                                v[j] = 0;
+                            for (int j = 0; j < 4; ++j) {
+                                if (a.align >= 4 && k + 4 * j + 4 <= a.K) {
+                                    v[j] = __ldg(reinterpret_cast<const uint32_t *>(p + 4 * j));
+                                } else if (k + 4 * j < a.K) {
+                                    v[j] = 0;
 #pragma unroll
-                                for (int e = 0; e < 4; ++e) v[j] |= (uint32_t)(k + 4 * j + e < a.K ? __ldg(p + 4 * j + e) : 128) << (8 * e);
+                                    for (int e = 0; e < 4; ++e) v[j] |= (uint32_t)(k + 4 * j + e < a.K ? __ldg(p + 4 * j + e) : 128) << (8 * e);
+                                }
                             }
                         }
-                    }
-                    *reinterpret_cast<uint4 *>(sA + m * a.stride + 16 * (i % blocks)) = make_uint4(v[0], v[1], v[2], v[3]);
-                }
-                __syncthreads();
-                const int groups = (kt1 - kt0) * kGroups;
-                for (int i = tid; i < kRows * groups; i += kMmThreads) {
-                    const int m = i / groups, q = i % groups;
-                    int sum = 0;
-                    if (m < rows) {
-                        const uint4 *p = reinterpret_cast<const uint4 *>(sA + m * a.stride + q * GROUP);
-#pragma unroll
-                        for (int j = 0; j < GROUP / 16; ++j) {
-                            const uint4 v = p[j];
-                            sum = (int)__dp4a(v.x, 0x01010101u, (uint32_t)sum), sum = (int)__dp4a(v.y, 0x01010101u, (uint32_t)sum);
-                            sum = (int)__dp4a(v.z, 0x01010101u, (uint32_t)sum), sum = (int)__dp4a(v.w, 0x01010101u, (uint32_t)sum);
+                        if constexpr (F16) {
+                            uint4 *to = reinterpret_cast<uint4 *>(sA + m * a.stride + 32 * blk);
+                            to[0] = make_uint4(codes_x16(v[0], 0x4140), codes_x1(v[0], 0x4342), codes_x16(v[1], 0x4140), codes_x1(v[1], 0x4342));
+                            to[1] = make_uint4(codes_x16(v[2], 0x4140), codes_x1(v[2], 0x4342), codes_x16(v[3], 0x4140), codes_x1(v[3], 0x4342));
+                        } else {
+                            *reinterpret_cast<uint4 *>(sA + m * a.stride + 16 * blk) = make_uint4(v[0], v[1], v[2], v[3]);
                         }
-                        sum -= 128 * GROUP;
                     }
-                    sR[q * kRows + m] = (float)sum * kUnit;
+                    uint32_t sum = 0;
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) sum = __dp4a(v[j], 0x01010101u, sum);
+#pragma unroll
+                    for (int o = 1; o < GROUP / 16; o *= 2) sum += __shfl_xor_sync(0xffffffffu, sum, o);
+                    if (i < total && blk % (GROUP / 16) == 0) sR[blk / (GROUP / 16) * kRows + m] = (float)((int)sum - 128 * GROUP) * kUnit;
                 }
                 __syncthreads();
             }
-            const uint8_t *pa = sA + g * a.stride + 8 * t;
+            const uint8_t *pa = sA + g * a.stride + (F16 ? 16 : 8) * t;
             for (int kt = kt0 + seg; kt < kt1; kt += a.segments) {
-                const Tile now = next;
-                load(next, kt + a.segments, kt1);
-                float sum[RT][NT][4];
+                copies_wait<P::kStages - 1>();
+                __syncwarp();
+                const uint8_t *at = ring + slot * P::kSlot;
+                const uint4 w0v = *reinterpret_cast<const uint4 *>(at + 16 * lane), w1v = *reinterpret_cast<const uint4 *>(at + 512 + 16 * lane);
+                Units<GROUP> u0, u1;
+                u0.load(reinterpret_cast<const uint32_t *>(at + kTileBytes) + g * kGroups);
+                u1.load(reinterpret_cast<const uint32_t *>(at + kTileBytes) + (g + 8) * kGroups);
+                __syncwarp();
+                issue(slot);
+                slot = slot + 1 == P::kStages ? 0 : slot + 1;
+                const uint32_t w0[4] = {w0v.x, w0v.y, w0v.z, w0v.w}, w1[4] = {w1v.x, w1v.y, w1v.z, w1v.w};
+                float sum[NT][4];
 #pragma unroll
                 for (int j = 0; j < 4; ++j) {
+                    const int q = j * 32 / GROUP;
                     if (j * 32 % GROUP == 0) {  // a group begins: offset x (sum of its b - 128)
-                        const float2 *R = reinterpret_cast<const float2 *>(sR + ((kt - kt0) * kGroups + j * 32 / GROUP) * kRows) + t;
+                        const float2 *R = reinterpret_cast<const float2 *>(sR + ((kt - kt0) * kGroups + q) * kRows) + t;
+                        const float z0 = unit_offset(u0.u[q]), z1 = unit_offset(u1.u[q]);
 #pragma unroll
                         for (int c = 0; c < NT; ++c) {
                             const float2 v = R[4 * c];
-#pragma unroll
-                            for (int r = 0; r < RT; ++r) {
-                                const float z0 = unit_offset(now.u[r][0].u[j * 32 / GROUP]), z1 = unit_offset(now.u[r][1].u[j * 32 / GROUP]);
-                                sum[r][c][0] = __fmul_rn(z0, v.x), sum[r][c][1] = __fmul_rn(z0, v.y);
-                                sum[r][c][2] = __fmul_rn(z1, v.x), sum[r][c][3] = __fmul_rn(z1, v.y);
-                            }
+                            sum[c][0] = __fmul_rn(z0, v.x), sum[c][1] = __fmul_rn(z0, v.y);
+                            sum[c][2] = __fmul_rn(z1, v.x), sum[c][3] = __fmul_rn(z1, v.y);
                         }
                     }
-                    uint32_t wa[RT][4], wb[RT][4];
-#pragma unroll
-                    for (int r = 0; r < RT; ++r) {
-                        const uint32_t *w0 = &now.w[r][0].x, *w1 = &now.w[r][1].x;
-                        const uint32_t x = w0[j], y = w1[j], x8 = x >> 8, y8 = y >> 8;
-                        wa[r][0] = x & 0x000f000fu, wa[r][1] = y & 0x000f000fu, wa[r][2] = x & 0x00f000f0u, wa[r][3] = y & 0x00f000f0u;
-                        wb[r][0] = x8 & 0x000f000fu, wb[r][1] = y8 & 0x000f000fu, wb[r][2] = x8 & 0x00f000f0u, wb[r][3] = y8 & 0x00f000f0u;
-                    }
+                    const uint32_t x = w0[j], y = w1[j], x8 = x >> 8, y8 = y >> 8;
+                    const uint32_t wa[4] = {x & 0x000f000fu, y & 0x000f000fu, x & 0x00f000f0u, y & 0x00f000f0u};
+                    const uint32_t wb[4] = {x8 & 0x000f000fu, y8 & 0x000f000fu, x8 & 0x00f000f0u, y8 & 0x00f000f0u};
 #pragma unroll
                     for (int c = 0; c < NT; ++c) {
-                        uint2 v = make_uint2(0x80808080u, 0x80808080u);
-                        if (8 * c + g < rows)
-                            v = *reinterpret_cast<const uint2 *>(pa + 8 * c * a.stride + (kt - kt0) * kTileCols + 32 * j);
-                        const uint32_t one = both(1.0f), six = both(16.0f), cone = both(-1152.0f), csix = both(-18432.0f);
-                        const uint32_t b0 = hfma2_bits(__byte_perm(v.x, 0x64646464u, 0x4140), six, csix);
-                        const uint32_t b1 = hfma2_bits(__byte_perm(v.x, 0x64646464u, 0x4342), one, cone);
-                        const uint32_t b2 = hfma2_bits(__byte_perm(v.y, 0x64646464u, 0x4140), six, csix);
-                        const uint32_t b3 = hfma2_bits(__byte_perm(v.y, 0x64646464u, 0x4342), one, cone);
-#pragma unroll
-                        for (int r = 0; r < RT; ++r) {
-                            mma_f16(sum[r][c], wa[r], b0, b1);
-                            mma_f16(sum[r][c], wb[r], b2, b3);
+                        if constexpr (F16) {
+                            uint4 v = make_uint4(0, 0, 0, 0);
+                            if (8 * c + g < rows)
+                                v = *reinterpret_cast<const uint4 *>(pa + 8 * c * a.stride + 2 * ((kt - kt0) * kTileCols + 32 * j));
+                            mma_f16(sum[c], wa, v.x, v.y);
+                            mma_f16(sum[c], wb, v.z, v.w);
+                        } else {
+                            uint2 v = make_uint2(0x80808080u, 0x80808080u);
+                            if (8 * c + g < rows)
+                                v = *reinterpret_cast<const uint2 *>(pa + 8 * c * a.stride + (kt - kt0) * kTileCols + 32 * j);
+                            mma_f16(sum[c], wa, codes_x16(v.x, 0x4140), codes_x1(v.x, 0x4342));
+                            mma_f16(sum[c], wb, codes_x16(v.y, 0x4140), codes_x1(v.y, 0x4342));
                         }
                     }
                     if ((j + 1) * 32 % GROUP == 0) {  // and ends
+                        const float s0 = unit_scale(u0.u[q]), s1 = unit_scale(u1.u[q]);
 #pragma unroll
-                        for (int r = 0; r < RT; ++r) {
-                            const float s0 = unit_scale(now.u[r][0].u[j * 32 / GROUP]), s1 = unit_scale(now.u[r][1].u[j * 32 / GROUP]);
-#pragma unroll
-                            for (int c = 0; c < NT; ++c) {
-                                acc[r][c][0] = __fmaf_rn(s0, sum[r][c][0], acc[r][c][0]);
-                                acc[r][c][1] = __fmaf_rn(s0, sum[r][c][1], acc[r][c][1]);
-                                acc[r][c][2] = __fmaf_rn(s1, sum[r][c][2], acc[r][c][2]);
-                                acc[r][c][3] = __fmaf_rn(s1, sum[r][c][3], acc[r][c][3]);
-                            }
+                        for (int c = 0; c < NT; ++c) {
+                            acc[c][0] = __fmaf_rn(s0, sum[c][0], acc[c][0]), acc[c][1] = __fmaf_rn(s0, sum[c][1], acc[c][1]);
+                            acc[c][2] = __fmaf_rn(s1, sum[c][2], acc[c][2]), acc[c][3] = __fmaf_rn(s1, sum[c][3], acc[c][3]);
                         }
                     }
                 }
             }
         }
         // the segments' sums, in order
-        if (item != blockIdx.x) __syncthreads();  // the item before is out
+        float *red = reds + red_at * (P::kRed / 4);
+        if (P::kReds == 1 && item != blockIdx.x) __syncthreads();  // the item before is out
+        if (P::kReds == 2) red_at ^= 1;
 #pragma unroll
-        for (int r = 0; r < RT; ++r)
-#pragma unroll
-            for (int c = 0; c < NT; ++c) {
-                float *p = red + ((warp * RT + r) * kRows + 8 * c + 2 * t) * kRedStride + g;
-                p[0] = acc[r][c][0], p[kRedStride] = acc[r][c][1];
-                p[8] = acc[r][c][2], p[kRedStride + 8] = acc[r][c][3];
-            }
+        for (int c = 0; c < NT; ++c) {
+            float *p = red + (warp * kRows + 8 * c + 2 * t) * kRedStride + g;
+            p[0] = acc[c][0], p[kRedStride] = acc[c][1];
+            p[8] = acc[c][2], p[kRedStride + 8] = acc[c][3];
+        }
         __syncthreads();
-        const int wide = tile_groups * RT * kTileRows;
         for (int i = tid; i < wide * rows; i += kMmThreads) {
-            const int m = i / wide, col = i % wide, tg = col / (RT * kTileRows), r = col / kTileRows % RT, row = col % kTileRows;
+            const int m = i / wide, col = i % wide, tg = col / kTileRows, row = col % kTileRows;
             const int64_t n = item * wide + col;
             if (n >= a.N) continue;
-            const qnn_qparams p = a.pa[a.per_row ? m0 + m : 0];
-            const float row_sum = __ldg(a.row_sums + n), bias = a.bias ? __ldg(a.bias + n) : 0.0f;
+            qnn_qparams p = my_unit;
+            float row_sum = my_sum, bias = my_bias;
+            if (i != tid) {
+                p = a.pa[a.per_row ? m0 + m : 0];
+                row_sum = __ldg(a.row_sums + n), bias = a.bias ? __ldg(a.bias + n) : 0.0f;
+            }
             float sum = 0.0f;
             for (int k = 0; k < a.segments; ++k)
-                sum = __fadd_rn(sum, red[(((tg * a.segments + k) * RT + r) * kRows + m) * kRedStride + row]);
+                sum = __fadd_rn(sum, red[((tg * a.segments + k) * kRows + m) * kRedStride + row]);
             a.Y[(m0 + m) * a.ldy + n] = recover4(__fmul_rn(sum, kPerUnit), p.Q, (float)p.z, row_sum, bias);
         }
     }
+    copies_wait<0>();
 }
 
-template <int GROUP, int NT, int RT>
+template <int GROUP, int NT>
 qnn_status launch_mm4(Mm4Args a, cudaStream_t st) {
-    constexpr int kRows = 8 * NT;
+    using P = Mm4Plan<GROUP, NT>;
     const int64_t ntiles = (a.N + kTileRows - 1) / kTileRows;
-    a.segments = 1;
-    while (a.segments < kMmWarps && a.segments < a.ktiles) a.segments *= 2;
-    const int64_t per_item = (int64_t)kMmWarps / a.segments * RT;
+    // as many warps on a row tile as leave every SM a block, and as have a column tile each
+    a.segments = kMmWarps;
+    while (a.segments > 1 && (a.segments >= 2 * a.ktiles || ntiles * a.segments > (int64_t)kMmWarps * sm_count())) a.segments /= 2;
+    const int64_t per_item = (int64_t)kMmWarps / a.segments;
     a.items = (ntiles + per_item - 1) / per_item;
-    // shared memory: the sums of all warps, and as many column tiles of A (codes and group sums) as fit beside them
-    constexpr size_t kMost = 220 * 1024, kRed = (size_t)kMmWarps * RT * kRows * kRedStride * 4;
-    const int rows = (int)std::min<int64_t>(kRows, a.M);
-    const size_t per_tile = (size_t)rows * kTileCols + (size_t)(kTileCols / GROUP) * kRows * 4;
-    a.chunk = (int)std::min<int64_t>(a.ktiles, (int64_t)((kMost - kRed - (size_t)rows * 32) / per_tile));
-    a.stride = a.chunk * kTileCols + 32;
-    const size_t bytes = kRed + (size_t)rows * a.stride + (size_t)a.chunk * (kTileCols / GROUP) * kRows * 4;
-    const auto kern = qmatmul4_kernel<GROUP, NT, RT>;
+    // A in shared memory beside the slots and sums: as fp16 values where all of it fits, else as codes that are converted as
+    // they are used, as many column tiles as fit, a part of them in whole rounds
+    constexpr size_t kMost = 227 * 1024 - 64, kFixed = P::kRing + P::kReds * P::kRed;
+    const int rows = (int)std::min<int64_t>(P::kRows, a.M);
+    const size_t sums = (size_t)P::kGroups * P::kRows * 4;  // a column tile's group sums
+    const bool f16 = kFixed + (size_t)rows * 64 + (size_t)a.ktiles * ((size_t)rows * 2 * kTileCols + sums) <= kMost;
+    a.chunk = a.ktiles;
+    if (!f16) {
+        a.chunk = (int)std::min<int64_t>(a.ktiles, (int64_t)((kMost - kFixed - (size_t)rows * 32) / ((size_t)rows * kTileCols + sums)));
+        if (a.chunk < a.ktiles) a.chunk = a.chunk / a.segments * a.segments;
+    }
+    a.stride = f16 ? a.chunk * 2 * kTileCols + 64 : a.chunk * kTileCols + 32;  // (rows 2 or 4 apart in the banks of a load)
+    const size_t bytes = kFixed + (size_t)rows * a.stride + (size_t)a.chunk * sums;
+    const auto kern = f16 ? qmatmul4_kernel<GROUP, NT, true> : qmatmul4_kernel<GROUP, NT, false>;
     if (bytes > 48 * 1024) QNN_CUDA_TRY(cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)bytes));
-    const int64_t mblocks = (a.M + kRows - 1) / kRows;
+    const int64_t mblocks = (a.M + P::kRows - 1) / P::kRows;
     if (mblocks > 65535) return QNN_FAIL(QNN_ERR_INVALID_ARG);
     kern<<<dim3((unsigned)std::min<int64_t>(a.items, sm_count()), (unsigned)mblocks), kMmThreads, bytes, st>>>(a);
     QNN_CUDA_TRY(cudaGetLastError());
@@ -335,11 +391,9 @@ qnn_status launch_mm4(Mm4Args a, cudaStream_t st) {
 
 template <int GROUP>
 qnn_status launch_mm4(const Mm4Args &a, cudaStream_t st) {
-    const int64_t ntiles = (a.N + kTileRows - 1) / kTileRows;
-    const bool two = ntiles > sm_count();
-    if (a.M <= 8) return two ? launch_mm4<GROUP, 1, 2>(a, st) : launch_mm4<GROUP, 1, 1>(a, st);
-    if (a.M <= 16) return two ? launch_mm4<GROUP, 2, 2>(a, st) : launch_mm4<GROUP, 2, 1>(a, st);
-    return launch_mm4<GROUP, 4, 1>(a, st);  // (two row tiles a warp do not fit its registers)
+    if (a.M <= 8) return launch_mm4<GROUP, 1>(a, st);
+    if (a.M <= 16) return launch_mm4<GROUP, 2>(a, st);
+    return launch_mm4<GROUP, 4>(a, st);
 }
 
 bool aligned16(const void *p) { return (reinterpret_cast<uintptr_t>(p) & 15) == 0; }
