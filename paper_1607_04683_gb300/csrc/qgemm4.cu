@@ -109,12 +109,12 @@ __device__ __forceinline__ uint32_t hfma2_bits(uint32_t x, uint32_t m, uint32_t 
 }
 __device__ __forceinline__ uint32_t both(float v) { return __half_as_ushort(__float2half_rn(v)) * 0x10001u; }
 
-// Two 8-bit codes b (the bytes of v that sel picks, 4: the byte 0x64) as 16 (b - 128) and as b - 128.
-__device__ __forceinline__ uint32_t codes_x16(uint32_t v, uint32_t sel) {
-    return hfma2_bits(__byte_perm(v, 0x64646464u, sel), both(16.0f), both(-18432.0f));
+// The first two and the last two of four 8-bit codes b as 16 (b - 128) and as b - 128.
+__device__ __forceinline__ uint32_t codes_x16(uint32_t v) {
+    return hfma2_bits(__byte_perm(v, 0x64646464u, 0x4140), both(16.0f), both(-18432.0f));
 }
-__device__ __forceinline__ uint32_t codes_x1(uint32_t v, uint32_t sel) {
-    return hfma2_bits(__byte_perm(v, 0x64646464u, sel), both(1.0f), both(-1152.0f));
+__device__ __forceinline__ uint32_t codes_x1(uint32_t v) {
+    return hfma2_bits(__byte_perm(v, 0x64646464u, 0x4342), both(1.0f), both(-1152.0f));
 }
 
 // The products run on the fp16 tensor-core instruction, exactly, on codes that cost next to nothing to convert:
@@ -162,14 +162,14 @@ struct Units {  // of a row's 128 columns
 template <int GROUP, int NT>
 struct Mm4Plan {
     static constexpr int kRows = 8 * NT, kGroups = kTileCols / GROUP;
-    static constexpr int kStages = NT == 1 ? 3 : 2;
+    static constexpr int kStages = NT <= 2 ? 3 : 2;
     static constexpr int kUnitBytes = kTileRows * kGroups * 4, kSlot = kTileBytes + kUnitBytes;
     static constexpr int kRing = kMmWarps * kStages * kSlot;
     static constexpr int kReds = NT == 1 ? 2 : 1, kRed = kMmWarps * kRows * kRedStride * 4;  // two: one barrier a row tile
     // shared memory: the slots, the warps' sums, A's codes, their group sums
 };
 
-template <int GROUP, int NT, bool F16>
+template <int GROUP, int NT>
 __global__ void __launch_bounds__(kMmThreads, 1) qmatmul4_kernel(const Mm4Args a) {
     using P = Mm4Plan<GROUP, NT>;
     constexpr int kRows = P::kRows, kGroups = P::kGroups;
@@ -232,46 +232,52 @@ __global__ void __launch_bounds__(kMmThreads, 1) qmatmul4_kernel(const Mm4Args a
             const int kt0 = chunk * a.chunk, kt1 = min(a.ktiles, kt0 + a.chunk);
             if (chunks > 1 || item == blockIdx.x) {
                 if (chunk > 0 || item != blockIdx.x) __syncthreads();  // all warps are done with what was there
-                // A's codes, 16 a thread (past K: 128, which counts 0), and their sums by groups, over 2 to 8 lanes
+                // A's codes, 16 a thread and step (past K: 128, which counts 0), as fp16 values, and their sums by groups, over
+                // 2 to 8 lanes; kAtOnce steps' loads in flight
+                constexpr int kAtOnce = NT == 1 ? 2 : 4;
                 const int blocks = (kt1 - kt0) * (kTileCols / 16), total = rows * blocks;
-                for (int i0 = 0; i0 < total; i0 += kMmThreads) {
-                    const int i = i0 + tid, m = i / blocks, blk = i % blocks, k = kt0 * kTileCols + 16 * blk;
-                    uint32_t v[4] = {0x80808080u, 0x80808080u, 0x80808080u, 0x80808080u};
-                    if (i < total) {
+                for (int i0 = 0; i0 < total; i0 += kAtOnce * kMmThreads) {
+                    uint32_t v[kAtOnce][4];
+#pragma unroll
+                    for (int s = 0; s < kAtOnce; ++s) {
+                        const int i = i0 + s * kMmThreads + tid, m = i / blocks, k = kt0 * kTileCols + 16 * (i % blocks);
+                        v[s][0] = v[s][1] = v[s][2] = v[s][3] = 0x80808080u;
+                        if (i >= total) continue;
                         const uint8_t *p = a.A + (m0 + m) * a.lda + k;
                         if (a.align == 16 && k + 16 <= a.K) {
                             const uint4 x = __ldg(reinterpret_cast<const uint4 *>(p));
-                            v[0] = x.x, v[1] = x.y, v[2] = x.z, v[3] = x.w;
+                            v[s][0] = x.x, v[s][1] = x.y, v[s][2] = x.z, v[s][3] = x.w;
                         } else {
 #pragma unroll
                             for (int j = 0; j < 4; ++j) {
                                 if (a.align >= 4 && k + 4 * j + 4 <= a.K) {
-                                    v[j] = __ldg(reinterpret_cast<const uint32_t *>(p + 4 * j));
+                                    v[s][j] = __ldg(reinterpret_cast<const uint32_t *>(p + 4 * j));
                                 } else if (k + 4 * j < a.K) {
-                                    v[j] = 0;
+                                    v[s][j] = 0;
 #pragma unroll
-                                    for (int e = 0; e < 4; ++e) v[j] |= (uint32_t)(k + 4 * j + e < a.K ? __ldg(p + 4 * j + e) : 128) << (8 * e);
+                                    for (int e = 0; e < 4; ++e) v[s][j] |= (uint32_t)(k + 4 * j + e < a.K ? __ldg(p + 4 * j + e) : 128) << (8 * e);
                                 }
                             }
                         }
-                        if constexpr (F16) {
-                            uint4 *to = reinterpret_cast<uint4 *>(sA + m * a.stride + 32 * blk);
-                            to[0] = make_uint4(codes_x16(v[0], 0x4140), codes_x1(v[0], 0x4342), codes_x16(v[1], 0x4140), codes_x1(v[1], 0x4342));
-                            to[1] = make_uint4(codes_x16(v[2], 0x4140), codes_x1(v[2], 0x4342), codes_x16(v[3], 0x4140), codes_x1(v[3], 0x4342));
-                        } else {
-                            *reinterpret_cast<uint4 *>(sA + m * a.stride + 16 * blk) = make_uint4(v[0], v[1], v[2], v[3]);
-                        }
                     }
-                    uint32_t sum = 0;
 #pragma unroll
-                    for (int j = 0; j < 4; ++j) sum = __dp4a(v[j], 0x01010101u, sum);
+                    for (int s = 0; s < kAtOnce; ++s) {
+                        const int i = i0 + s * kMmThreads + tid, m = i / blocks, blk = i % blocks;
+                        uint32_t sum = 0;
 #pragma unroll
-                    for (int o = 1; o < GROUP / 16; o *= 2) sum += __shfl_xor_sync(0xffffffffu, sum, o);
-                    if (i < total && blk % (GROUP / 16) == 0) sR[blk / (GROUP / 16) * kRows + m] = (float)((int)sum - 128 * GROUP) * kUnit;
+                        for (int j = 0; j < 4; ++j) sum = __dp4a(v[s][j], 0x01010101u, sum);
+#pragma unroll
+                        for (int o = 1; o < GROUP / 16; o *= 2) sum += __shfl_xor_sync(0xffffffffu, sum, o);
+                        if (i >= total) continue;
+                        uint4 *to = reinterpret_cast<uint4 *>(sA + m * a.stride + 32 * blk);
+                        to[0] = make_uint4(codes_x16(v[s][0]), codes_x1(v[s][0]), codes_x16(v[s][1]), codes_x1(v[s][1]));
+                        to[1] = make_uint4(codes_x16(v[s][2]), codes_x1(v[s][2]), codes_x16(v[s][3]), codes_x1(v[s][3]));
+                        if (blk % (GROUP / 16) == 0) sR[blk / (GROUP / 16) * kRows + m] = (float)((int)sum - 128 * GROUP) * kUnit;
+                    }
                 }
                 __syncthreads();
             }
-            const uint8_t *pa = sA + g * a.stride + (F16 ? 16 : 8) * t;
+            const uint8_t *pa = sA + g * a.stride + 16 * t;
             for (int kt = kt0 + seg; kt < kt1; kt += a.segments) {
                 copies_wait<P::kStages - 1>();
                 __syncwarp();
@@ -303,19 +309,11 @@ __global__ void __launch_bounds__(kMmThreads, 1) qmatmul4_kernel(const Mm4Args a
                     const uint32_t wb[4] = {x8 & 0x000f000fu, y8 & 0x000f000fu, x8 & 0x00f000f0u, y8 & 0x00f000f0u};
 #pragma unroll
                     for (int c = 0; c < NT; ++c) {
-                        if constexpr (F16) {
-                            uint4 v = make_uint4(0, 0, 0, 0);
-                            if (8 * c + g < rows)
-                                v = *reinterpret_cast<const uint4 *>(pa + 8 * c * a.stride + 2 * ((kt - kt0) * kTileCols + 32 * j));
-                            mma_f16(sum[c], wa, v.x, v.y);
-                            mma_f16(sum[c], wb, v.z, v.w);
-                        } else {
-                            uint2 v = make_uint2(0x80808080u, 0x80808080u);
-                            if (8 * c + g < rows)
-                                v = *reinterpret_cast<const uint2 *>(pa + 8 * c * a.stride + (kt - kt0) * kTileCols + 32 * j);
-                            mma_f16(sum[c], wa, codes_x16(v.x, 0x4140), codes_x1(v.x, 0x4342));
-                            mma_f16(sum[c], wb, codes_x16(v.y, 0x4140), codes_x1(v.y, 0x4342));
-                        }
+                        uint4 v = make_uint4(0, 0, 0, 0);
+                        if (8 * c + g < rows)
+                            v = *reinterpret_cast<const uint4 *>(pa + 8 * c * a.stride + 2 * ((kt - kt0) * kTileCols + 32 * j));
+                        mma_f16(sum[c], wa, v.x, v.y);
+                        mma_f16(sum[c], wb, v.z, v.w);
                     }
                     if ((j + 1) * 32 % GROUP == 0) {  // and ends
                         const float s0 = unit_scale(u0.u[q]), s1 = unit_scale(u1.u[q]);
@@ -367,20 +365,19 @@ qnn_status launch_mm4(Mm4Args a, cudaStream_t st) {
     while (a.segments > 1 && (a.segments >= 2 * a.ktiles || ntiles * a.segments > (int64_t)kMmWarps * sm_count())) a.segments /= 2;
     const int64_t per_item = (int64_t)kMmWarps / a.segments;
     a.items = (ntiles + per_item - 1) / per_item;
-    // A in shared memory beside the slots and sums: as fp16 values where all of it fits, else as codes that are converted as
-    // they are used, as many column tiles as fit, a part of them in whole rounds
+    // as many column tiles of A as fit in shared memory beside the slots and sums, the parts of them even and in whole rounds
     constexpr size_t kMost = 227 * 1024 - 64, kFixed = P::kRing + P::kReds * P::kRed;
     const int rows = (int)std::min<int64_t>(P::kRows, a.M);
     const size_t sums = (size_t)P::kGroups * P::kRows * 4;  // a column tile's group sums
-    const bool f16 = kFixed + (size_t)rows * 64 + (size_t)a.ktiles * ((size_t)rows * 2 * kTileCols + sums) <= kMost;
+    const int fit = (int)std::min<int64_t>(a.ktiles, (int64_t)((kMost - kFixed - (size_t)rows * 64) / ((size_t)rows * 2 * kTileCols + sums)));
     a.chunk = a.ktiles;
-    if (!f16) {
-        a.chunk = (int)std::min<int64_t>(a.ktiles, (int64_t)((kMost - kFixed - (size_t)rows * 32) / ((size_t)rows * kTileCols + sums)));
-        if (a.chunk < a.ktiles) a.chunk = a.chunk / a.segments * a.segments;
+    if (fit < a.ktiles) {
+        const int whole = fit / a.segments * a.segments, parts = (a.ktiles + whole - 1) / whole;
+        a.chunk = ((a.ktiles + parts - 1) / parts + a.segments - 1) / a.segments * a.segments;
     }
-    a.stride = f16 ? a.chunk * 2 * kTileCols + 64 : a.chunk * kTileCols + 32;  // (rows 2 or 4 apart in the banks of a load)
+    a.stride = a.chunk * 2 * kTileCols + 64;  // (so that the two rows of a quarter of a load lie in different banks)
     const size_t bytes = kFixed + (size_t)rows * a.stride + (size_t)a.chunk * sums;
-    const auto kern = f16 ? qmatmul4_kernel<GROUP, NT, true> : qmatmul4_kernel<GROUP, NT, false>;
+    const auto kern = qmatmul4_kernel<GROUP, NT>;
     if (bytes > 48 * 1024) QNN_CUDA_TRY(cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)bytes));
     const int64_t mblocks = (a.M + P::kRows - 1) / P::kRows;
     if (mblocks > 65535) return QNN_FAIL(QNN_ERR_INVALID_ARG);
