@@ -277,7 +277,9 @@ __global__ void __launch_bounds__(kMmThreads, 1) qmatmul4_kernel(const Mm4Args a
                 }
                 __syncthreads();
             }
-            const uint8_t *pa = sA + g * a.stride + 16 * t;
+            const uint8_t *pa[NT];  // (columns past the rows there are repeat the last: their sums go nowhere)
+#pragma unroll
+            for (int c = 0; c < NT; ++c) pa[c] = sA + min(8 * c + g, rows - 1) * a.stride + 16 * t;
             for (int kt = kt0 + seg; kt < kt1; kt += a.segments) {
                 copies_wait<P::kStages - 1>();
                 __syncwarp();
@@ -309,9 +311,7 @@ __global__ void __launch_bounds__(kMmThreads, 1) qmatmul4_kernel(const Mm4Args a
                     const uint32_t wb[4] = {x8 & 0x000f000fu, y8 & 0x000f000fu, x8 & 0x00f000f0u, y8 & 0x00f000f0u};
 #pragma unroll
                     for (int c = 0; c < NT; ++c) {
-                        uint4 v = make_uint4(0, 0, 0, 0);
-                        if (8 * c + g < rows)
-                            v = *reinterpret_cast<const uint4 *>(pa + 8 * c * a.stride + 2 * ((kt - kt0) * kTileCols + 32 * j));
+                        const uint4 v = *reinterpret_cast<const uint4 *>(pa[c] + 2 * ((kt - kt0) * kTileCols + 32 * j));
                         mma_f16(sum[c], wa, v.x, v.y);
                         mma_f16(sum[c], wb, v.z, v.w);
                     }
