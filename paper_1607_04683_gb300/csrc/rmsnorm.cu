@@ -79,36 +79,197 @@ struct NormArgs {
     int *status;
 };
 
-// A row a block, three passes over it (sum of squares, range, codes), h formed again in each: every element is read and
-// written by one thread, so h may take the place of x or r.
-constexpr int kThreads = 256, kWarps = kThreads / 32;
+// The row's scale: s, or s found again at a smaller scale where squares overflow. total(f): the sum of the squares of f h.
+template <typename F>
+__device__ __forceinline__ float row_scale(const NormArgs &a, F total) {
+    const Pair sum = total(1.0f);
+    if (sum.hi <= 0x1p126f) return inverse_rms(sum, (float)a.cols, a.eps_hi, a.eps_lo);
+    return __fmul_rn(inverse_rms(total(kDown), (float)a.cols, a.eps_down_hi, 0.0f), kDown);
+}
+
+// Sums, ranges and counts over the warps of a block, by every warp from shared memory. (Each on arrays of its own: between
+// two uses of one lie two barriers.)
+struct BlockShare {
+    float2 sum[32];
+    float mn[32], mx[32];
+    int ok[32], count[32];
+};
+__device__ __forceinline__ Pair block_sum(Pair p, BlockShare &sh, int warps) {
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    p = warp_sum_pair(p);
+    __syncthreads();
+    if (lane == 0) sh.sum[warp] = make_float2(p.hi, p.lo);
+    __syncthreads();
+    Pair q;
+    if (lane < warps) q.hi = sh.sum[lane].x, q.lo = sh.sum[lane].y;
+    return warp_sum_pair(q);
+}
+// The range over the block; false if a value was not finite.
+__device__ __forceinline__ bool block_range(float &mn, float &mx, bool ok, BlockShare &sh, int warps) {
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    mn = warp_min(mn);
+    mx = warp_max(mx);
+    ok = __all_sync(0xffffffffu, ok);
+    if (lane == 0) sh.mn[warp] = mn, sh.mx[warp] = mx, sh.ok[warp] = ok;
+    __syncthreads();
+    const int w = lane < warps ? lane : 0;
+    mn = warp_min(sh.mn[w]);
+    mx = warp_max(sh.mx[w]);
+    return __all_sync(0xffffffffu, sh.ok[w] != 0);
+}
+
+// Rows held in registers: R runs of V neighbouring values a thread (16 bytes of x each), a warp a row (ROWWARP, several
+// rows a block) or a block a row. Every value is read once; the row's two reductions lie between the loads and the stores.
+// VEC: all of the call's rows begin on whole runs.
+constexpr int kNormWarps = 4;  // rows a block, ROWWARP
+template <typename T, int R, bool ROWWARP, bool VEC>
+__global__ void __launch_bounds__(ROWWARP ? 32 * kNormWarps : 1024) rmsnorm_rows_kernel(const NormArgs a) {
+    constexpr int V = 16 / (int)sizeof(T);
+    __shared__ BlockShare sh;
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, warps = ROWWARP ? 1 : blockDim.x >> 5;
+    const int64_t row = ROWWARP ? (int64_t)blockIdx.x * kNormWarps + warp : blockIdx.x;
+    if (row >= a.rows) return;
+    const int first = V * (ROWWARP ? lane : (int)threadIdx.x), step = V * 32 * warps;
+    auto left = [&](int j) { return a.cols - (first + j * step); };
+    float h[R][V], w[R][V];
+    {
+        const T *x = static_cast<const T *>(a.x) + row * a.ldx + first;
+        const T *r = static_cast<const T *>(a.r) + (a.r ? row * a.ldr + first : 0);
+        Run<T, V> rx[R], rr[R];
+        Run<float, V> rw[R];
+#pragma unroll
+        for (int j = 0; j < R; ++j) {
+            if (VEC && left(j) >= V) {
+                rx[j].load(x + j * step);
+                if (a.r) rr[j].load(r + j * step);
+                rw[j].load(a.w + first + j * step);
+            } else {
+                rx[j].load_some(x + j * step, left(j));
+                if (a.r) rr[j].load_some(r + j * step, left(j));
+                rw[j].load_some(a.w + first + j * step, left(j));
+            }
+        }
+#pragma unroll
+        for (int j = 0; j < R; ++j)
+#pragma unroll
+            for (int v = 0; v < V; ++v) {
+                h[j][v] = rx[j].get(v);
+                if (a.r) h[j][v] = __fadd_rn(h[j][v], rr[j].get(v));
+                w[j][v] = rw[j].get(v);
+            }
+    }
+    if (a.h) {
+        T *out = static_cast<T *>(a.h) + row * a.ldh + first;
+#pragma unroll
+        for (int j = 0; j < R; ++j) {
+            Run<T, V> o;
+            o.set(h[j]);
+            if (VEC && left(j) >= V)
+                o.store(out + j * step);
+            else
+                o.store_some(out + j * step, left(j));
+        }
+    }
+    const float s = row_scale(a, [&](float scale) {
+        Pair p;  // (values past the row's end are 0)
+#pragma unroll
+        for (int j = 0; j < R; ++j)
+#pragma unroll
+            for (int v = 0; v < V; ++v) p.add_square(__fmul_rn(h[j][v], scale));
+        return ROWWARP ? warp_sum_pair(p) : block_sum(p, sh, warps);
+    });
+    float mn = FLT_MAX, mx = -FLT_MAX, bad = 0.0f;
+#pragma unroll
+    for (int j = 0; j < R; ++j)
+#pragma unroll
+        for (int v = 0; v < V; ++v) {
+            h[j][v] = __fmul_rn(__fmul_rn(h[j][v], s), w[j][v]);
+            if (v < left(j)) {
+                mn = fminf(mn, h[j][v]);
+                mx = fmaxf(mx, h[j][v]);
+                bad = __fmaf_rn(h[j][v], 0.0f, bad);
+            }
+        }
+    bool ok = bad == 0.0f;
+    if (ROWWARP)
+        mn = warp_min(mn), mx = warp_max(mx), ok = __all_sync(0xffffffffu, ok);
+    else
+        ok = block_range(mn, mx, ok, sh, warps);
+    if (!ok) {
+        if (first == 0) record_status(a.status, QNN_ERR_NONFINITE);
+        mn = mx = 0.0f;
+    }
+    const qnn_qparams p = params_from_range(mn, mx);
+    const UnitCoder unit(p.Q, p.z);
+    const bool quick = p.Q >= 0x1p-60f && p.Q <= 0x1p60f;  // quotients by the reciprocal, correctly rounded all the same
+    const float inv = quick ? rcp_rn(p.Q) : 0.0f;
+    int count = 0;
+    uint8_t *codes = a.codes + row * a.ldc + first;
+    float *values = a.values + (a.values ? row * a.ldv + first : 0);
+#pragma unroll
+    for (int j = 0; j < R; ++j) {
+        uint32_t c[V];
+        float q[V];
+#pragma unroll
+        for (int v = 0; v < V; ++v) {
+            c[v] = unit.code(h[j][v]);
+            if (v < left(j)) count += (int)c[v];
+        }
+        if (VEC && left(j) >= V) {
+            uint32_t word[V / 4];
+#pragma unroll
+            for (int k = 0; k < V / 4; ++k) word[k] = c[4 * k] | (c[4 * k + 1] << 8) | (c[4 * k + 2] << 16) | (c[4 * k + 3] << 24);
+            if constexpr (V == 8)
+                *reinterpret_cast<uint2 *>(codes + j * step) = make_uint2(word[0], word[1]);
+            else
+                *reinterpret_cast<uint32_t *>(codes + j * step) = word[0];
+        } else {
+#pragma unroll
+            for (int v = 0; v < V; ++v)
+                if (v < left(j)) codes[j * step + v] = (uint8_t)c[v];
+        }
+        if (a.values) {
+#pragma unroll
+            for (int v = 0; v < V; ++v) {
+                const float k = (float)((int)c[v] + p.z);
+                q[v] = quick ? div_by_recip(k, p.Q, inv) : __fdiv_rn(k, p.Q);
+            }
+            Run<float, V> o;
+            o.set(q);
+            if (VEC && left(j) >= V)
+                o.store(values + j * step);
+            else
+                o.store_some(values + j * step, left(j));
+        }
+    }
+    count = warp_sum(count);
+    if (!ROWWARP) {
+        if (lane == 0) sh.count[warp] = count;
+        __syncthreads();
+        if (warp == 0) count = warp_sum(lane < warps ? sh.count[lane] : 0);
+    }
+    if (first == 0) {
+        a.params[row] = p;
+        if (a.sums) a.sums[row] = count;
+    }
+}
+
+// Rows too long for registers: a row a block, three passes over it (sum of squares, range, codes), h formed again in each.
+// Every element is read and written by one thread, and h only in the last pass, so it may take the place of x or r.
+constexpr int kThreads = 1024;
 template <typename T>
 __global__ void __launch_bounds__(kThreads) rmsnorm_long_rows_kernel(const NormArgs a) {
-    __shared__ Pair s_sum[kWarps];
-    __shared__ float s_mn[kWarps], s_mx[kWarps];
-    __shared__ int s_bad[kWarps], s_cnt[kWarps];
+    __shared__ BlockShare sh;
     const int64_t row = blockIdx.x;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const T *x = static_cast<const T *>(a.x) + row * a.ldx;
     const T *r = a.r ? static_cast<const T *>(a.r) + row * a.ldr : nullptr;
     auto h_at = [&](int k) { return r ? __fadd_rn(to_f32(x[k]), to_f32(r[k])) : to_f32(x[k]); };
-    auto total = [&](float scale) {
+    const float s = row_scale(a, [&](float scale) {
         Pair p;
         for (int k = threadIdx.x; k < a.cols; k += kThreads) p.add_square(__fmul_rn(h_at(k), scale));
-        p = warp_sum_pair(p);
-        __syncthreads();
-        if (lane == 0) s_sum[warp] = p;
-        __syncthreads();
-        p = s_sum[0];
-        for (int w = 1; w < kWarps; ++w) p.add(s_sum[w]);
-        return p;
-    };
-    Pair sum = total(1.0f);
-    float s;
-    if (sum.hi <= 0x1p126f)
-        s = inverse_rms(sum, (float)a.cols, a.eps_hi, a.eps_lo);
-    else
-        s = __fmul_rn(inverse_rms(total(kDown), (float)a.cols, a.eps_down_hi, 0.0f), kDown);
+        return block_sum(p, sh, kThreads / 32);
+    });
     float mn = FLT_MAX, mx = -FLT_MAX, bad = 0.0f;
     auto v_at = [&](float h, int k) { return __fmul_rn(__fmul_rn(h, s), __ldg(a.w + k)); };
     for (int k = threadIdx.x; k < a.cols; k += kThreads) {
@@ -117,35 +278,63 @@ __global__ void __launch_bounds__(kThreads) rmsnorm_long_rows_kernel(const NormA
         mx = fmaxf(mx, v);
         bad = __fmaf_rn(v, 0.0f, bad);
     }
-    mn = warp_min(mn);
-    mx = warp_max(mx);
-    const int ok = __all_sync(0xffffffffu, bad == 0.0f);
-    if (lane == 0) s_mn[warp] = mn, s_mx[warp] = mx, s_bad[warp] = !ok;
-    __syncthreads();
-    int any = 0;
-    for (int w = 0; w < kWarps; ++w) mn = fminf(mn, s_mn[w]), mx = fmaxf(mx, s_mx[w]), any |= s_bad[w];
-    if (any) {
+    if (!block_range(mn, mx, bad == 0.0f, sh, kThreads / 32)) {
         if (threadIdx.x == 0) record_status(a.status, QNN_ERR_NONFINITE);
         mn = mx = 0.0f;
     }
     const qnn_qparams p = params_from_range(mn, mx);
     const UnitCoder unit(p.Q, p.z);
-    int cnt = 0;
+    int count = 0;
     for (int k = threadIdx.x; k < a.cols; k += kThreads) {
         const float h = h_at(k);
         const uint32_t c = unit.code(v_at(h, k));
-        cnt += (int)c;
+        count += (int)c;
         a.codes[row * a.ldc + k] = (uint8_t)c;
         if (a.h) static_cast<T *>(a.h)[row * a.ldh + k] = from_f32<T>(h);
         if (a.values) a.values[row * a.ldv + k] = __fdiv_rn((float)((int)c + p.z), p.Q);
     }
-    cnt = warp_sum(cnt);
-    if (lane == 0) s_cnt[warp] = cnt;
+    count = warp_sum(count);
+    if (lane == 0) sh.count[warp] = count;
     __syncthreads();
+    if (warp == 0) count = warp_sum(sh.count[lane]);
     if (threadIdx.x == 0) {
-        for (int w = 1; w < kWarps; ++w) cnt += s_cnt[w];
         a.params[row] = p;
-        if (a.sums) a.sums[row] = cnt;
+        if (a.sums) a.sums[row] = count;
+    }
+}
+
+template <typename T, int R, bool ROWWARP>
+void launch_rows(const NormArgs &a, bool vec, unsigned blocks, int threads, cudaStream_t st) {
+    if (vec)
+        rmsnorm_rows_kernel<T, R, ROWWARP, true><<<blocks, threads, 0, st>>>(a);
+    else
+        rmsnorm_rows_kernel<T, R, ROWWARP, false><<<blocks, threads, 0, st>>>(a);
+}
+
+template <typename T>
+void launch_norm(const NormArgs &a, cudaStream_t st) {
+    constexpr int V = 16 / (int)sizeof(T), kMost = 16 / V;  // runs a thread: 16 values
+    auto whole = [](const void *p, int64_t ld, int64_t size, uintptr_t bytes) {
+        return !p || (reinterpret_cast<uintptr_t>(p) % bytes == 0 && ld * size % (int64_t)bytes == 0);
+    };
+    const int64_t one = a.rows == 1 ? 0 : 1;  // (a single row has no next one)
+    const bool vec = whole(a.x, one * a.ldx, sizeof(T), 16) && whole(a.r, one * a.ldr, sizeof(T), 16) && whole(a.h, one * a.ldh, sizeof(T), 16) &&
+                     whole(a.w, 0, 4, 16) && whole(a.codes, one * a.ldc, 1, V) && whole(a.values, one * a.ldv, 4, 16);
+    const int runs = (a.cols + V - 1) / V;
+    if (runs <= 32 * kMost && a.rows > sm_count() / 2) {
+        const unsigned blocks = (unsigned)((a.rows + kNormWarps - 1) / kNormWarps);
+        if (runs <= 32)
+            launch_rows<T, 1, true>(a, vec, blocks, 32 * kNormWarps, st);
+        else if (runs <= 64)
+            launch_rows<T, 2, true>(a, vec, blocks, 32 * kNormWarps, st);
+        else
+            launch_rows<T, kMost, true>(a, vec, blocks, 32 * kNormWarps, st);
+    } else if (runs <= 1024 && a.rows <= sm_count()) {  // few rows: as many threads as runs
+        launch_rows<T, 1, false>(a, vec, (unsigned)a.rows, (runs + 31) / 32 * 32, st);
+    } else if (runs <= 1024 * kMost) {
+        launch_rows<T, kMost, false>(a, vec, (unsigned)a.rows, ((runs + kMost - 1) / kMost + 31) / 32 * 32, st);
+    } else {
+        rmsnorm_long_rows_kernel<T><<<(unsigned)a.rows, kThreads, 0, st>>>(a);
     }
 }
 
@@ -193,9 +382,7 @@ extern "C" qnn_status qnn_rmsnorm_quantize(const void *x, int64_t ldx, const voi
     QNN_TRY(status_word(&a.status));
     cudaStream_t st = as_stream(stream);
     ProfScope prof("rmsnorm_quantize", st);
-    with_type(dtype, [&](auto t) {
-        rmsnorm_long_rows_kernel<decltype(t)><<<(unsigned)rows, kThreads, 0, st>>>(a);
-    });
+    with_type(dtype, [&](auto t) { launch_norm<decltype(t)>(a, st); });
     QNN_CUDA_TRY(cudaGetLastError());
     return QNN_OK;
 }
