@@ -120,11 +120,11 @@ __device__ __forceinline__ bool block_range(float &mn, float &mx, bool ok, Block
 
 // Rows held in registers: R runs of V neighbouring values a thread (16 bytes of x each), a warp a row (ROWWARP, several
 // rows a block) or a block a row. Every value is read once; the row's two reductions lie between the loads and the stores.
-// VEC: all of the call's rows begin on whole runs.
+// VEC: all of the call's rows begin on whole runs; otherwise the runs are single values, as many.
 constexpr int kNormWarps = 4;  // rows a block, ROWWARP
-template <typename T, int R, bool ROWWARP, bool VEC>
+template <typename T, int RUNS, bool ROWWARP, bool VEC>
 __global__ void __launch_bounds__(ROWWARP ? 32 * kNormWarps : 1024) rmsnorm_rows_kernel(const NormArgs a) {
-    constexpr int V = 16 / (int)sizeof(T);
+    constexpr int V = VEC ? 16 / (int)sizeof(T) : 1, R = VEC ? RUNS : RUNS * 16 / (int)sizeof(T);
     __shared__ BlockShare sh;
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, warps = ROWWARP ? 1 : blockDim.x >> 5;
     const int64_t row = ROWWARP ? (int64_t)blockIdx.x * kNormWarps + warp : blockIdx.x;
@@ -216,7 +216,7 @@ __global__ void __launch_bounds__(ROWWARP ? 32 * kNormWarps : 1024) rmsnorm_rows
             if (v < left(j)) count += (int)c[v];
         }
         if (VEC && left(j) >= V) {
-            uint32_t word[V / 4];
+            uint32_t word[(V + 3) / 4];
 #pragma unroll
             for (int k = 0; k < V / 4; ++k) word[k] = c[4 * k] | (c[4 * k + 1] << 8) | (c[4 * k + 2] << 16) | (c[4 * k + 3] << 24);
             if constexpr (V == 8)
