@@ -87,17 +87,17 @@ __device__ __forceinline__ float row_scale(const NormArgs &a, F total) {
     return __fmul_rn(inverse_rms(total(kDown), (float)a.cols, a.eps_down_hi, 0.0f), kDown);
 }
 
-// Sums, ranges and counts over the warps of a block, by every warp from shared memory. (Each on arrays of its own: between
-// two uses of one lie two barriers.)
+// Sums, ranges and counts over the warps of a block, by every warp from shared memory, each on arrays of its own (again: the
+// sum's are used for a second time).
 struct BlockShare {
     float2 sum[32];
     float mn[32], mx[32];
     int ok[32], count[32];
 };
-__device__ __forceinline__ Pair block_sum(Pair p, BlockShare &sh, int warps) {
+__device__ __forceinline__ Pair block_sum(Pair p, BlockShare &sh, int warps, bool again) {
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     p = warp_sum_pair(p);
-    __syncthreads();
+    if (again) __syncthreads();
     if (lane == 0) sh.sum[warp] = make_float2(p.hi, p.lo);
     __syncthreads();
     Pair q;
@@ -176,7 +176,7 @@ __global__ void __launch_bounds__(ROWWARP ? 32 * kNormWarps : 1024) rmsnorm_rows
         for (int j = 0; j < R; ++j)
 #pragma unroll
             for (int v = 0; v < V; ++v) p.add_square(__fmul_rn(h[j][v], scale));
-        return ROWWARP ? warp_sum_pair(p) : block_sum(p, sh, warps);
+        return ROWWARP ? warp_sum_pair(p) : block_sum(p, sh, warps, scale != 1.0f);
     });
     float mn = FLT_MAX, mx = -FLT_MAX, bad = 0.0f;
 #pragma unroll
@@ -268,7 +268,7 @@ __global__ void __launch_bounds__(kThreads) rmsnorm_long_rows_kernel(const NormA
     const float s = row_scale(a, [&](float scale) {
         Pair p;
         for (int k = threadIdx.x; k < a.cols; k += kThreads) p.add_square(__fmul_rn(h_at(k), scale));
-        return block_sum(p, sh, kThreads / 32);
+        return block_sum(p, sh, kThreads / 32, scale != 1.0f);
     });
     float mn = FLT_MAX, mx = -FLT_MAX, bad = 0.0f;
     auto v_at = [&](float h, int k) { return __fmul_rn(__fmul_rn(h, s), __ldg(a.w + k)); };

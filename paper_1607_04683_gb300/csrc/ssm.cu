@@ -46,26 +46,27 @@ __global__ void __launch_bounds__(kConvThreads) causal_conv_kernel(const ConvArg
     T *y = static_cast<T *>(a.y) + b * a.y_seq + d;
     const T *s_in = static_cast<const T *>(a.state_in) + b * (W - 1) * a.D + d;
     T *s_out = static_cast<T *>(a.state_out) + b * (W - 1) * a.D + d;
-    Run<T, V> taps[WT];  // taps[j]: the input WT - 1 - j frames back
+    auto unpack = [](const Run<T, V> &r, float (&to)[V]) {
 #pragma unroll
-    for (int j = 0; j < WT; ++j) taps[j].clear();
+        for (int v = 0; v < V; ++v) to[v] = r.get(v);
+    };
+    float in[WT - 1 + kAhead][V];  // the WT - 1 inputs before a round of kAhead frames, and the round's
+    {
+        Run<T, V> r[WT];
 #pragma unroll
-    for (int j = 0; j < WT - 1; ++j) {  // before the chunk: WT - 1 - j frames back of t0
-        const int t = t0 - (WT - 1) + j;
-        if (j < WT - W) continue;
-        if (chunk > 0)
-            taps[j].load(x + t * a.x_frame);
-        else if (a.state_in)
-            taps[j].load(s_in + (t + W - 1) * a.D);
+        for (int j = 0; j < WT - 1; ++j) {  // before the chunk: WT - 1 - j frames back of t0
+            const int t = t0 - (WT - 1) + j;
+            r[j].clear();
+            if (j < WT - W) continue;
+            if (chunk > 0)
+                r[j].load(x + t * a.x_frame);
+            else if (a.state_in)
+                r[j].load(s_in + (t + W - 1) * a.D);
+        }
+#pragma unroll
+        for (int j = 0; j < WT - 1; ++j) unpack(r[j], in[j]);
     }
     if (t0 < t1) {
-        float w[WT][V], bias[V];
-#pragma unroll
-        for (int v = 0; v < V; ++v) {
-            bias[v] = a.bias ? __ldg(a.bias + d + v) : 0.0f;
-#pragma unroll
-            for (int j = 0; j < WT; ++j) w[j][v] = j >= WT - W ? __ldg(a.w + (d + v) * W + j - (WT - W)) : 0.0f;
-        }
         Run<T, V> next[kAhead];
         auto fetch = [&](int t) {
 #pragma unroll
@@ -73,37 +74,65 @@ __global__ void __launch_bounds__(kConvThreads) causal_conv_kernel(const ConvArg
                 if (t + i < t1) next[i].load(x + (int64_t)(t + i) * a.x_frame);
         };
         fetch(t0);
-        for (int t = t0; t < t1; t += kAhead) {
-            Run<T, V> now[kAhead];
+        float w[WT][V], bias[V];
 #pragma unroll
-            for (int i = 0; i < kAhead; ++i) now[i] = next[i];
+        for (int v = 0; v < V; ++v) {
+            bias[v] = a.bias ? __ldg(a.bias + d + v) : 0.0f;
+            if (WT == 4 && W == 4 && V > 1) {  // (V channels' taps lie side by side: whole loads; one by one, a load's 32 lanes
+                                               // touch as many lines)
+                const float4 q = __ldg(reinterpret_cast<const float4 *>(a.w + (d + v) * 4));
+                w[0][v] = q.x, w[1][v] = q.y, w[2][v] = q.z, w[3][v] = q.w;
+            } else {
+#pragma unroll
+                for (int j = 0; j < WT; ++j) w[j][v] = j >= WT - W ? __ldg(a.w + (d + v) * W + j - (WT - W)) : 0.0f;
+            }
+        }
+        auto frame = [&](int t, int i) {  // frame t, the i-th of the round
+            float o[V];
+#pragma unroll
+            for (int v = 0; v < V; ++v) {
+                o[v] = bias[v];
+#pragma unroll
+                for (int j = 0; j < WT; ++j) o[v] = __fmaf_rn(w[j][v], in[i + j][v], o[v]);
+                if (a.silu) o[v] = silu(o[v]);
+            }
+            Run<T, V> out;
+            out.set(o);
+            out.store(y + (int64_t)t * a.y_frame);
+        };
+        int t = t0;
+        for (; t + kAhead <= t1; t += kAhead) {
+#pragma unroll
+            for (int i = 0; i < kAhead; ++i) unpack(next[i], in[WT - 1 + i]);
             fetch(t + kAhead);
 #pragma unroll
-            for (int i = 0; i < kAhead; ++i) {
-                if (t + i >= t1) break;
-                taps[WT - 1] = now[i];
-                float o[V];
+            for (int i = 0; i < kAhead; ++i) frame(t + i, i);
 #pragma unroll
-                for (int v = 0; v < V; ++v) {
-                    o[v] = bias[v];
+            for (int j = 0; j < WT - 1; ++j)
 #pragma unroll
-                    for (int j = 0; j < WT; ++j) o[v] = __fmaf_rn(w[j][v], taps[j].get(v), o[v]);
-                    if (a.silu) o[v] = silu(o[v]);
-                }
-                Run<T, V> out;
-                out.set(o);
-                out.store(y + (int64_t)(t + i) * a.y_frame);
+                for (int v = 0; v < V; ++v) in[j][v] = in[j + kAhead][v];
+        }
 #pragma unroll
-                for (int j = 0; j < WT - 1; ++j) taps[j] = taps[j + 1];
-            }
+        for (int i = 0; i < kAhead - 1; ++i) {  // the frames of a last, shorter round
+            if (t + i >= t1) break;
+            unpack(next[i], in[WT - 1]);
+            frame(t + i, 0);
+#pragma unroll
+            for (int j = 0; j < WT - 1; ++j)
+#pragma unroll
+                for (int v = 0; v < V; ++v) in[j][v] = in[j + 1][v];
         }
     }
     if (chunk > 0 || !a.state_out) return;
-    // the last W - 1 of old state and n frames. Where the chunk holds all frames they are the taps (shifted once a frame)
+    // the last W - 1 of old state and n frames. Where the chunk holds all frames they are at hand
     if (n <= a.chunk) {
 #pragma unroll
         for (int j = 0; j < WT - 1; ++j)
-            if (j >= WT - W) taps[j].store(s_out + (j - (WT - W)) * a.D);
+            if (j >= WT - W) {
+                Run<T, V> last;
+                last.set(in[j]);
+                last.store(s_out + (j - (WT - W)) * a.D);
+            }
     } else {
         for (int j = 0; j < W - 1; ++j) {
             Run<T, V> last;
@@ -585,13 +614,14 @@ qnn_status launch_scan(ScanArgs &a, cudaStream_t st) {
 
 template <typename T, int WT>
 qnn_status launch_conv(ConvArgs a, cudaStream_t st) {
-    constexpr int V = 16 / (int)sizeof(T);
+    constexpr int V = 4;  // (eight 16-bit values a thread: 26 us where four take 22)
     const int e = sizeof(T);
-    auto at16 = [](const void *p) { return reinterpret_cast<uintptr_t>(p) % 16 == 0; };
-    const bool vec = a.D % V == 0 && (a.T == 0 || (aligned_to(a.x, a.x_seq, a.x_frame, e, 16) && aligned_to(a.y, a.y_seq, a.y_frame, e, 16))) &&
-                     at16(a.state_in) && at16(a.state_out);
+    auto whole = [](const void *p, uintptr_t bytes) { return reinterpret_cast<uintptr_t>(p) % bytes == 0; };
+    const bool vec = a.D % V == 0 && whole(a.state_in, V * e) && whole(a.state_out, V * e) && whole(a.w, 16) &&
+                     (a.T == 0 || (aligned_to(a.x, a.x_seq, a.x_frame, e, V * e) && aligned_to(a.y, a.y_seq, a.y_frame, e, V * e)));
     a.runs = vec ? a.D / V : a.D;
-    a.chunk = 32;
+    // frames a thread: 32, or 16 while that leaves the SMs less than two waves of blocks (1 x 300 x 2048 bf16 5.8 and 4.3 us)
+    a.chunk = a.B * a.runs * ((a.T + 31) / 32) < 16 * kConvThreads * (int64_t)sm_count() ? 16 : 32;
     a.chunks = std::max<int64_t>(1, (a.T + a.chunk - 1) / a.chunk);
     const int64_t blocks = (a.B * a.runs * a.chunks + kConvThreads - 1) / kConvThreads;
     if (blocks > INT32_MAX) return QNN_FAIL(QNN_ERR_INVALID_ARG);
