@@ -16,6 +16,18 @@ __device__ __forceinline__ int frames_of(const int32_t *lengths, int64_t b, int6
     return n < 0 ? 0 : n > T ? (int)T : n;
 }
 
+// i / n and i % n. 64-bit divisions take a hundred instructions; most indices need 32.
+struct Split {
+    int64_t quot, rem;
+};
+__device__ __forceinline__ Split split(int64_t i, int64_t n) {
+    if (((i | n) >> 32) == 0) {
+        const uint32_t q = (uint32_t)i / (uint32_t)n;
+        return {(int64_t)q, (int64_t)((uint32_t)i - q * (uint32_t)n)};
+    }
+    return {i / n, i % n};
+}
+
 // ------------------------------------------------------------------------------------------------
 // Convolution
 // ------------------------------------------------------------------------------------------------
@@ -29,15 +41,16 @@ struct ConvArgs {
     int W, silu, chunk;
 };
 
-// A thread takes V neighbouring channels of a sequence over a chunk of its frames, the last WT - 1 inputs in registers and
-// kAhead frames' loads in flight. The first chunk's thread alone reads and writes the channels' state: it has read the old
+// A thread takes V neighbouring channels of a sequence over a chunk of its frames in rounds of kAhead, the last WT - 1 inputs
+// in registers and the next round's loads in flight. The first chunk's thread alone reads and writes the channels' state: it has read the old
 // state before it writes the new one, and later chunks (at least WT - 1 frames on) never look at it. W < WT taps stand at
 // the end of WT, the others are not loaded and count 0.
-constexpr int kMostTaps = 8, kConvThreads = 128, kAhead = 4;
-template <typename T, int WT, int V>
+constexpr int kMostTaps = 8, kConvThreads = 128;
+template <typename T, int WT, int V, int kAhead>
 __global__ void __launch_bounds__(kConvThreads) causal_conv_kernel(const ConvArgs a) {
     const int64_t at = (int64_t)blockIdx.x * kConvThreads + threadIdx.x;
-    const int64_t run = at % a.runs, rest = at / a.runs, chunk = rest % a.chunks, b = rest / a.chunks;
+    const Split of_runs = split(at, a.runs), of_chunks = split(of_runs.quot, a.chunks);
+    const int64_t run = of_runs.rem, chunk = of_chunks.rem, b = of_chunks.quot;
     if (b >= a.B) return;
     const int n = frames_of(a.lengths, b, a.T), t0 = (int)chunk * a.chunk, t1 = min(n, t0 + a.chunk), W = a.W;
     if (chunk > 0 && t0 >= n) return;
@@ -68,12 +81,16 @@ __global__ void __launch_bounds__(kConvThreads) causal_conv_kernel(const ConvArg
     }
     if (t0 < t1) {
         Run<T, V> next[kAhead];
-        auto fetch = [&](int t) {
+        const T *from = x + t0 * a.x_frame;
+        T *to = y + t0 * a.y_frame;
+        auto fetch = [&](int left) {  // the next round's frames, of `left` there are
 #pragma unroll
-            for (int i = 0; i < kAhead; ++i)
-                if (t + i < t1) next[i].load(x + (int64_t)(t + i) * a.x_frame);
+            for (int i = 0; i < kAhead; ++i) {
+                if (i < left) next[i].load(from);
+                from += a.x_frame;
+            }
         };
-        fetch(t0);
+        fetch(t1 - t0);
         float w[WT][V], bias[V];
 #pragma unroll
         for (int v = 0; v < V; ++v) {
@@ -87,26 +104,35 @@ __global__ void __launch_bounds__(kConvThreads) causal_conv_kernel(const ConvArg
                 for (int j = 0; j < WT; ++j) w[j][v] = j >= WT - W ? __ldg(a.w + (d + v) * W + j - (WT - W)) : 0.0f;
             }
         }
-        auto frame = [&](int t, int i) {  // frame t, the i-th of the round
+        auto frame = [&](int i) {  // the i-th of the round
             float o[V];
+            if constexpr (V > 1) {
 #pragma unroll
-            for (int v = 0; v < V; ++v) {
-                o[v] = bias[v];
+                for (int v = 0; v < V; v += 2) {
+                    float2 f = make_float2(bias[v], bias[v + 1]);
 #pragma unroll
-                for (int j = 0; j < WT; ++j) o[v] = __fmaf_rn(w[j][v], in[i + j][v], o[v]);
-                if (a.silu) o[v] = silu(o[v]);
+                    for (int j = 0; j < WT; ++j) f = ffma2_rn(make_float2(w[j][v], w[j][v + 1]), make_float2(in[i + j][v], in[i + j][v + 1]), f);
+                    if (a.silu) f = silu2(f);
+                    o[v] = f.x, o[v + 1] = f.y;
+                }
+            } else {
+                o[0] = bias[0];
+#pragma unroll
+                for (int j = 0; j < WT; ++j) o[0] = __fmaf_rn(w[j][0], in[i + j][0], o[0]);
+                if (a.silu) o[0] = silu(o[0]);
             }
             Run<T, V> out;
             out.set(o);
-            out.store(y + (int64_t)t * a.y_frame);
+            out.store(to);
+            to += a.y_frame;
         };
         int t = t0;
         for (; t + kAhead <= t1; t += kAhead) {
 #pragma unroll
             for (int i = 0; i < kAhead; ++i) unpack(next[i], in[WT - 1 + i]);
-            fetch(t + kAhead);
+            fetch(t1 - t - kAhead);
 #pragma unroll
-            for (int i = 0; i < kAhead; ++i) frame(t + i, i);
+            for (int i = 0; i < kAhead; ++i) frame(i);
 #pragma unroll
             for (int j = 0; j < WT - 1; ++j)
 #pragma unroll
@@ -116,7 +142,7 @@ __global__ void __launch_bounds__(kConvThreads) causal_conv_kernel(const ConvArg
         for (int i = 0; i < kAhead - 1; ++i) {  // the frames of a last, shorter round
             if (t + i >= t1) break;
             unpack(next[i], in[WT - 1]);
-            frame(t + i, 0);
+            frame(0);
 #pragma unroll
             for (int j = 0; j < WT - 1; ++j)
 #pragma unroll
@@ -161,11 +187,12 @@ enum { kVecStates = 1, kVecBC = 2 };
 // A lane holds four states of a channel, 1 .. 32 lanes a channel; each step's sum over the states by shuffles.
 constexpr int kStepFrames = 4, kStepThreads = 128;
 template <typename T>
-__global__ void __launch_bounds__(kStepThreads) ssm_step_kernel(const ScanArgs a, int lanes) {
-    const int64_t at = (int64_t)blockIdx.x * kStepThreads + threadIdx.x, chan = at / lanes;
-    const int n0 = 4 * (int)(at % lanes);
+__global__ void __launch_bounds__(kStepThreads) ssm_step_kernel(const ScanArgs a, int shift) {
+    const int64_t at = (int64_t)blockIdx.x * kStepThreads + threadIdx.x, chan = at >> shift;
+    const int lanes = 1 << shift, n0 = 4 * (int)(at & (lanes - 1));
     const bool there = chan < a.B * a.D;
-    const int64_t b = there ? chan / a.D : a.B - 1, d = there ? chan % a.D : a.D - 1, g = d / a.group_chans;
+    const Split of_chans = split(there ? chan : a.B * a.D - 1, a.D);
+    const int64_t b = of_chans.quot, d = of_chans.rem, g = a.groups == 1 ? 0 : split(d, a.group_chans).quot;
     const int count = there ? max(min(a.N - n0, 4), 0) : 0;
     const int frames = frames_of(a.lengths, b, a.T);
     float h[4] = {}, A[4] = {};
@@ -310,12 +337,13 @@ __global__ void __launch_bounds__(32 * ScanWarp<NS, L>::kBlockWarps, 3) ssm_scan
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     Sh &sh = all[warp];
     const int64_t at = (int64_t)blockIdx.x * W + warp;
-    const int rank = (int)(at % a.parts);
-    int64_t unit = at / a.parts;
+    const int rank = (int)at & (a.parts - 1);  // (parts is a power of two)
+    int64_t unit = at >> (31 - __clz(a.parts));
     const bool there = unit < a.units;  // (a warp without work still takes part in the barriers)
     if (!there) unit = 0;
-    const int blk = (int)(unit % a.group_blocks), g = (int)(unit / a.group_blocks % a.groups);
-    const int64_t b = unit / a.group_blocks / a.groups, d0 = g * a.group_chans + (int64_t)blk * Sh::kChans;
+    const Split of_blocks = split(unit, a.group_blocks), of_groups = split(of_blocks.quot, a.groups);
+    const int blk = (int)of_blocks.rem, g = (int)of_groups.rem;
+    const int64_t b = of_groups.quot, d0 = g * a.group_chans + (int64_t)blk * Sh::kChans;
     const int chans = (int)min((int64_t)Sh::kChans, (g + 1) * a.group_chans - d0);
     const int n = there ? frames_of(a.lengths, b, a.T) : 0;
     const int tiles = (n + kTile - 1) / kTile, each = (tiles + a.parts - 1) / a.parts * kTile;
@@ -546,11 +574,11 @@ bool aligned_to(const void *p, int64_t seq, int64_t frame, int e, int bytes) {
 
 template <typename T>
 qnn_status launch_step(const ScanArgs &a, cudaStream_t st) {
-    int lanes = 1;
-    while (4 * lanes < a.N) lanes *= 2;
-    const int64_t blocks = (a.B * a.D * lanes + kStepThreads - 1) / kStepThreads;
+    int shift = 0;
+    while (4 << shift < a.N) ++shift;
+    const int64_t blocks = ((a.B * a.D << shift) + kStepThreads - 1) / kStepThreads;
     if (blocks > INT32_MAX) return QNN_FAIL(QNN_ERR_INVALID_ARG);
-    ssm_step_kernel<T><<<(unsigned)blocks, kStepThreads, 0, st>>>(a, lanes);
+    ssm_step_kernel<T><<<(unsigned)blocks, kStepThreads, 0, st>>>(a, shift);
     return QNN_OK;
 }
 
@@ -620,15 +648,16 @@ qnn_status launch_conv(ConvArgs a, cudaStream_t st) {
     const bool vec = a.D % V == 0 && whole(a.state_in, V * e) && whole(a.state_out, V * e) && whole(a.w, 16) &&
                      (a.T == 0 || (aligned_to(a.x, a.x_seq, a.x_frame, e, V * e) && aligned_to(a.y, a.y_seq, a.y_frame, e, V * e)));
     a.runs = vec ? a.D / V : a.D;
-    // frames a thread: 32, or 16 while that leaves the SMs less than two waves of blocks (1 x 300 x 2048 bf16 5.8 and 4.3 us)
-    a.chunk = a.B * a.runs * ((a.T + 31) / 32) < 16 * kConvThreads * (int64_t)sm_count() ? 16 : 32;
+    // Frames a thread: 40, or 16 while that leaves the SMs less than two waves of blocks (1 x 300 x 2048 bf16 5.8 us with 32 and
+    // 4.3 so). A few frames take a round of one (a kernel of half the registers: 256 x 1 x 2048 fp32 6.3 us with eight).
+    const bool few = a.T <= 4;
+    a.chunk = few || a.B * a.runs * ((a.T + 39) / 40) < 8 * kConvThreads * (int64_t)sm_count() ? 16 : 40;
     a.chunks = std::max<int64_t>(1, (a.T + a.chunk - 1) / a.chunk);
     const int64_t blocks = (a.B * a.runs * a.chunks + kConvThreads - 1) / kConvThreads;
     if (blocks > INT32_MAX) return QNN_FAIL(QNN_ERR_INVALID_ARG);
-    if (vec)
-        causal_conv_kernel<T, WT, V><<<(unsigned)blocks, kConvThreads, 0, st>>>(a);
-    else
-        causal_conv_kernel<T, WT, 1><<<(unsigned)blocks, kConvThreads, 0, st>>>(a);
+    const auto kern = vec ? (few ? causal_conv_kernel<T, WT, V, 1> : causal_conv_kernel<T, WT, V, 8>)
+                          : (few ? causal_conv_kernel<T, WT, 1, 1> : causal_conv_kernel<T, WT, 1, 8>);
+    kern<<<(unsigned)blocks, kConvThreads, 0, st>>>(a);
     return QNN_OK;
 }
 
