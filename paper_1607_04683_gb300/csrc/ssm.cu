@@ -175,83 +175,153 @@ __global__ void __launch_bounds__(kConvThreads) causal_conv_kernel(const ConvArg
 constexpr int kMostStates = 128;
 
 struct ScanArgs : qnn_ssm_args {
-    int vec;              // (few frames) kVec*: arrays whose runs of four states may be loaded or stored whole
+    bool vec;             // (few frames) runs of four states are loaded and stored whole
     int64_t group_chans;  // D / groups
     int64_t units;        // warps' shares of channels, of all sequences
     int group_blocks;     // of them a group
     int parts;            // warps that share a unit's frames
 };
-enum { kVecStates = 1, kVecBC = 2 };
 
-// Few frames: no frame waits for another for long, and states are most of the traffic (8 N bytes a channel, in and out).
-// A lane holds four states of a channel, 1 .. 32 lanes a channel; each step's sum over the states by shuffles.
+// Few frames: states are most of the traffic (8 N bytes a channel, in and out). A lane holds four states of a channel, L lanes a
+// channel, and takes NB sequences at a time: lane q forms the steps and gates of sequence q of them and passes them on by
+// shuffles, so that each is formed once. It goes on to further sequences of its channel, whose states and inputs are loaded
+// one round ahead; what depends on the channel alone is read once. (256 x 1 x 2048 x 16 fp32: a sequence a thread 29 us, 350
+// instructions each; four, once, 22 us.)
 constexpr int kStepFrames = 4, kStepThreads = 128;
-template <typename T>
-__global__ void __launch_bounds__(kStepThreads) ssm_step_kernel(const ScanArgs a, int shift) {
-    const int64_t at = (int64_t)blockIdx.x * kStepThreads + threadIdx.x, chan = at >> shift;
-    const int lanes = 1 << shift, n0 = 4 * (int)(at & (lanes - 1));
-    const bool there = chan < a.B * a.D;
-    const Split of_chans = split(there ? chan : a.B * a.D - 1, a.D);
-    const int64_t b = of_chans.quot, d = of_chans.rem, g = a.groups == 1 ? 0 : split(d, a.group_chans).quot;
-    const int count = there ? max(min(a.N - n0, 4), 0) : 0;
-    const int frames = frames_of(a.lengths, b, a.T);
-    float h[4] = {}, A[4] = {};
-    const int64_t state = (b * a.D + d) * a.N + n0;
-    if (a.vec & kVecStates) {
-        if (count) {
-            Run<float, 4> r;
+template <typename T, int L, bool VEC>
+__global__ void __launch_bounds__(kStepThreads, 4) ssm_step_kernel(const ScanArgs a) {
+    constexpr int NB = L < 4 ? L : 4;
+    const int64_t at = (int64_t)blockIdx.x * kStepThreads + threadIdx.x;
+    const int q = (int)(at % L), n0 = 4 * q, lane = threadIdx.x & 31, mine = q % NB;  // mine: this lane's sequence
+    const bool chan = at / L < a.D;
+    const int64_t d = chan ? at / L : a.D - 1, g = a.groups == 1 ? 0 : split(d, a.group_chans).quot;
+    const int count = chan ? max(min(a.N - n0, 4), 0) : 0;  // states
+    float A[4];
+    {
+        Run<float, 4> r;
+        r.clear();
+        if (!VEC)
+            r.load_some(a.A + d * a.N + n0, count);
+        else if (count)
             r.load(a.A + d * a.N + n0);
 #pragma unroll
-            for (int i = 0; i < 4; ++i) A[i] = r.get(i);
-            if (a.state_in) {
-                r.load(a.state_in + state);
-#pragma unroll
-                for (int i = 0; i < 4; ++i) h[i] = r.get(i);
-            }
-        }
-    } else {
-#pragma unroll
-        for (int i = 0; i < 4; ++i)
-            if (i < count) {
-                A[i] = __ldg(a.A + d * a.N + n0 + i);
-                if (a.state_in) h[i] = a.state_in[state + i];
-            }
+        for (int k = 0; k < 4; ++k) A[k] = __fmul_rn(r.get(k), kLog2e);
     }
     const float skip = a.skip ? __ldg(a.skip + d) : 0.0f, bias = a.dt_bias ? __ldg(a.dt_bias + d) : 0.0f;
-    for (int t = 0; t < a.T; ++t) {  // (frames differ within a warp: all lanes take part in the shuffles)
-        const bool on = t < frames;
-        float y = 0.0f, u = 0.0f, gate = 1.0f;
-        if (on && count) {
-            u = to_f32(static_cast<const T *>(a.u)[b * a.u_seq + t * a.u_frame + d]);
-            float s = __fadd_rn(to_f32(static_cast<const T *>(a.dt)[b * a.dt_seq + t * a.dt_frame + d]), bias);
-            const T *pB = static_cast<const T *>(a.Bm) + b * a.Bm_seq + t * a.Bm_frame + g * a.N + n0;
-            const T *pC = static_cast<const T *>(a.Cm) + b * a.Cm_seq + t * a.Cm_frame + g * a.N + n0;
-            Run<T, 4> rB, rC;
-            if (a.vec & kVecBC)
-                rB.load(pB), rC.load(pC);
-            else
-                rB.load_some(pB, count), rC.load_some(pC, count);
-            if (a.z) gate = silu(to_f32(static_cast<const T *>(a.z)[b * a.z_seq + t * a.z_frame + d]));
-            if (a.softplus) s = softplus(s);
-            const float su = __fmul_rn(s, u), s2 = __fmul_rn(s, kLog2e);
+
+    const int64_t step = (int64_t)gridDim.y * NB, row = a.D * a.N;  // sequences from a round to the next, states of one
+    int64_t b0 = (int64_t)blockIdx.y * NB;
+    const float *p_in = a.state_in + (a.state_in ? b0 * row + d * a.N + n0 : 0);
+    float *p_out = a.state_out + (a.state_out ? b0 * row + d * a.N + n0 : 0);
+    const T *pu = static_cast<const T *>(a.u) + (b0 + mine) * a.u_seq + d, *pd = static_cast<const T *>(a.dt) + (b0 + mine) * a.dt_seq + d;
+    const T *pz = static_cast<const T *>(a.z) + (b0 + mine) * a.z_seq + d;
+    T *py = static_cast<T *>(a.y) + (b0 + mine) * a.y_seq + d;
+    const T *pB = static_cast<const T *>(a.Bm) + b0 * a.Bm_seq + g * a.N + n0, *pC = static_cast<const T *>(a.Cm) + b0 * a.Cm_seq + g * a.N + n0;
+
+    Run<float, 4> next[NB];
+    Run<T, 1> nu, nd, nz;
+    int n_frames = 0;
+    auto fetch = [&](int64_t b) {  // the states of the round from sequence b on, and their first frame's inputs
 #pragma unroll
-            for (int i = 0; i < 4; ++i)
-                if (i < count) {
-                    h[i] = __fmaf_rn(exp2_hw(__fmul_rn(s2, A[i])), h[i], __fmul_rn(su, rB.get(i)));
-                    y = __fmaf_rn(rC.get(i), h[i], y);
-                }
+        for (int i = 0; i < NB; ++i) {
+            next[i].clear();
+            if (a.state_in && b + i < a.B) {
+                if (!VEC)
+                    next[i].load_some(p_in + i * row, count);
+                else if (count)
+                    next[i].load(p_in + i * row);
+            }
         }
-        for (int o = lanes >> 1; o > 0; o >>= 1) y = __fadd_rn(y, __shfl_xor_sync(0xffffffffu, y, o));
-        if (on && there && n0 == 0)
-            static_cast<T *>(a.y)[b * a.y_seq + t * a.y_frame + d] = from_f32<T>(__fmul_rn(__fmaf_rn(skip, u, y), gate));
-    }
-    if (!a.state_out) return;
-    if (a.vec & kVecStates) {
-        if (count) *reinterpret_cast<float4 *>(a.state_out + state) = make_float4(h[0], h[1], h[2], h[3]);
-    } else {
+        p_in += step * row;
+        n_frames = chan && b + mine < a.B ? frames_of(a.lengths, b + mine, a.T) : 0;
+        nu.clear(), nd.clear(), nz.clear();
+        if (n_frames > 0) {
+            nu.load(pu), nd.load(pd);
+            if (a.z) nz.load(pz);
+        }
+    };
+    fetch(b0);
+    for (; b0 < a.B; b0 += step) {
+        float h[NB][4];
 #pragma unroll
-        for (int i = 0; i < 4; ++i)
-            if (i < count) a.state_out[state + i] = h[i];
+        for (int i = 0; i < NB; ++i)
+#pragma unroll
+            for (int k = 0; k < 4; ++k) h[i][k] = next[i].get(k);
+        float u = nu.get(0), s = nd.get(0), gate = nz.get(0);
+        const int frames = n_frames;
+        const T *qu = pu, *qd = pd, *qz = pz;  // (further frames)
+        pu += step * a.u_seq, pd += step * a.dt_seq, pz += step * a.z_seq;
+        fetch(b0 + step);
+        T *qy = py;
+        const T *qB = pB, *qC = pC;
+        for (int t = 0; t < a.T; ++t) {  // (sequences differ in frames: all lanes take part in the shuffles)
+            const bool on = t < frames;
+            if (t > 0 && on) {
+                qu += a.u_frame, qd += a.dt_frame, qz += a.z_frame;
+                u = to_f32(*qu), s = to_f32(*qd);
+                if (a.z) gate = to_f32(*qz);
+            }
+            const unsigned group_on = __ballot_sync(0xffffffffu, on) >> (lane - q);  // bit i: sequence i has this frame
+            Run<T, 4> rB[NB], rC[NB];
+#pragma unroll
+            for (int i = 0; i < NB; ++i) {
+                const int some = group_on >> i & 1 ? count : 0;
+                if (!VEC) {
+                    rB[i].load_some(qB + i * a.Bm_seq, some), rC[i].load_some(qC + i * a.Cm_seq, some);
+                } else {
+                    rB[i].clear(), rC[i].clear();
+                    if (some) rB[i].load(qB + i * a.Bm_seq), rC[i].load(qC + i * a.Cm_seq);
+                }
+            }
+            qB += a.Bm_frame, qC += a.Cm_frame;
+            s = __fadd_rn(s, bias);
+            if (a.softplus) s = softplus(s);
+            if (!on) s = 0.0f;  // (a frame that is not there has a step of 0 and no Bm: the state stays as it is)
+            const float su = on ? __fmul_rn(s, u) : 0.0f;
+            float y[NB];
+#pragma unroll
+            for (int i = 0; i < NB; ++i) {
+                const float si = __shfl_sync(0xffffffffu, s, lane - q + i), sui = __shfl_sync(0xffffffffu, su, lane - q + i);
+                y[i] = 0.0f;
+#pragma unroll
+                for (int k = 0; k < 4; ++k) {
+                    h[i][k] = __fmaf_rn(exp2_hw(__fmul_rn(si, A[k])), h[i][k], __fmul_rn(sui, rB[i].get(k)));
+                    y[i] = __fmaf_rn(rC[i].get(k), h[i][k], y[i]);
+                }
+            }
+            // NB sums over L lanes: whole sums where there are more lanes than sequences, then halved, until lane q has its own
+#pragma unroll
+            for (int o = L / 2; o >= NB && o > 0; o >>= 1)
+#pragma unroll
+                for (int i = 0; i < NB; ++i) y[i] = __fadd_rn(y[i], __shfl_xor_sync(0xffffffffu, y[i], o));
+#pragma unroll
+            for (int o = NB / 2; o > 0; o >>= 1)
+#pragma unroll
+                for (int i = 0; i < o; ++i) {
+                    const float send = q & o ? y[i] : y[i + o], keep = q & o ? y[i + o] : y[i];
+                    y[i] = __fadd_rn(keep, __shfl_xor_sync(0xffffffffu, send, o));
+                }
+            if (on && q < NB) {
+                float o = __fmaf_rn(skip, u, y[0]);
+                if (a.z) o = __fmul_rn(o, silu(gate));
+                *qy = from_f32<T>(o);
+            }
+            qy += a.y_frame;
+        }
+        if (a.state_out) {
+#pragma unroll
+            for (int i = 0; i < NB; ++i) {
+                if (b0 + i >= a.B) continue;
+                Run<float, 4> o;
+                o.set(h[i]);
+                if (!VEC)
+                    o.store_some(p_out + i * row, count);
+                else if (count)
+                    o.store(p_out + i * row);
+            }
+            p_out += step * row;
+        }
+        py += step * a.y_seq, pB += step * a.Bm_seq, pC += step * a.Cm_seq;
     }
 }
 
@@ -572,13 +642,18 @@ bool aligned_to(const void *p, int64_t seq, int64_t frame, int e, int bytes) {
     return reinterpret_cast<uintptr_t>(p) % bytes == 0 && seq * e % bytes == 0 && frame * e % bytes == 0;
 }
 
-template <typename T>
+template <typename T, int L>
 qnn_status launch_step(const ScanArgs &a, cudaStream_t st) {
-    int shift = 0;
-    while (4 << shift < a.N) ++shift;
-    const int64_t blocks = ((a.B * a.D << shift) + kStepThreads - 1) / kStepThreads;
-    if (blocks > INT32_MAX) return QNN_FAIL(QNN_ERR_INVALID_ARG);
-    ssm_step_kernel<T><<<(unsigned)blocks, kStepThreads, 0, st>>>(a, shift);
+    constexpr int NB = L < 4 ? L : 4;
+    // two waves of blocks, each on a part of the channels and every so many of the sequences
+    const int64_t chans = (a.D * L + kStepThreads - 1) / kStepThreads, rounds = (a.B + NB - 1) / NB;
+    if (chans > INT32_MAX) return QNN_FAIL(QNN_ERR_INVALID_ARG);
+    const int64_t shares = std::min<int64_t>({rounds, std::max<int64_t>(1, 8 * (int64_t)sm_count() / chans), 65535});
+    const dim3 grid((unsigned)chans, (unsigned)shares);
+    if (a.vec)
+        ssm_step_kernel<T, L, true><<<grid, kStepThreads, 0, st>>>(a);
+    else
+        ssm_step_kernel<T, L, false><<<grid, kStepThreads, 0, st>>>(a);
     return QNN_OK;
 }
 
@@ -624,13 +699,17 @@ qnn_status launch_scan(ScanArgs &a, cudaStream_t st) {
     const int e = sizeof(T);
     a.group_chans = a.D / a.groups;
     a.parts = 1;
-    a.vec = 0;
+    a.vec = false;
     if (a.T <= kStepFrames) {
         auto at16 = [](const void *p) { return reinterpret_cast<uintptr_t>(p) % 16 == 0; };
-        if (a.N % 4 == 0 && at16(a.A) && at16(a.state_in) && at16(a.state_out)) a.vec |= kVecStates;
-        if (a.N % 4 == 0 && aligned_to(a.Bm, a.Bm_seq, a.Bm_frame, e, 4 * e) && aligned_to(a.Cm, a.Cm_seq, a.Cm_frame, e, 4 * e))
-            a.vec |= kVecBC;
-        return launch_step<T>(a, st);
+        a.vec = a.N % 4 == 0 && at16(a.A) && at16(a.state_in) && at16(a.state_out) &&
+                (a.T == 0 || (aligned_to(a.Bm, a.Bm_seq, a.Bm_frame, e, 4 * e) && aligned_to(a.Cm, a.Cm_seq, a.Cm_frame, e, 4 * e)));
+        if (a.N <= 4) return launch_step<T, 1>(a, st);
+        if (a.N <= 8) return launch_step<T, 2>(a, st);
+        if (a.N <= 16) return launch_step<T, 4>(a, st);
+        if (a.N <= 32) return launch_step<T, 8>(a, st);
+        if (a.N <= 64) return launch_step<T, 16>(a, st);
+        return launch_step<T, 32>(a, st);
     }
     if (a.N <= 4) return launch_tiles<T, 4, 1>(a, st);
     if (a.N <= 8) return launch_tiles<T, 8, 1>(a, st);
