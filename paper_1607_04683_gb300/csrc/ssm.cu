@@ -325,11 +325,6 @@ __global__ void __launch_bounds__(kStepThreads, 4) ssm_step_kernel(const ScanArg
     }
 }
 
-__device__ __forceinline__ uint32_t cluster_rank() {
-    uint32_t r;
-    asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(r));
-    return r;
-}
 __device__ __forceinline__ void cluster_arrive() { asm volatile("barrier.cluster.arrive.release;" ::: "memory"); }
 __device__ __forceinline__ void cluster_wait() { asm volatile("barrier.cluster.wait.acquire;" ::: "memory"); }
 // The address of a shared variable in another block of the cluster, and a load from it.
@@ -364,27 +359,35 @@ struct ScanWarp {
     static constexpr int kRowLanes = kChans / V, kRows = 32 / kRowLanes;  // lanes a frame, frames a load
     static constexpr int kBCEach = (kTile * kStates / 4 + 31) / 32;       // runs of four a lane loads of Bm and Cm
     static constexpr bool kBCAhead = kBCEach <= 4;       // a tile ahead, while registers allow it
-    static constexpr int kBlockWarps = kStates <= 64 ? 4 : 2;
+    static constexpr int kBlockWarps = 4;
 
     alignas(16) float2 s[kTile][kChans];  // steps s and s u
-    alignas(16) float y[kTile][kChans];   // sums over the states
     alignas(16) float B[kTile][kStates], C[kTile][kStates];
-    float part[NS][32], sum[32];          // r and S
+    struct Part {
+        float part[NS][32], sum[32];      // r and S
+    };
+    float part[NS][32], sum[32];          // of this warp's part
     float2 start[NS / 2][32];             // the states that a part starts from, where it is the first
 };
 
-// h <- exp2(s A) h + su B for NS states, y += C h, in pairs: one instruction issues for two results (a state costs 2.5
-// issue slots and the hardware's exponential instead of 4.5).
+// A frame's factors exp2(s A), its inputs su B and the sum of C h, for NS states in pairs: one instruction for two results.
 template <int NS>
-__device__ __forceinline__ void advance(float2 (&h)[NS / 2], const float2 (&A)[NS / 2], float s, float su, const float *B) {
-    const float2 s2 = make_float2(s, s), su2 = make_float2(su, su);
+__device__ __forceinline__ void factors(float2 (&f)[NS / 2], const float2 (&A)[NS / 2], float s) {
+    const float2 s2 = make_float2(s, s);
+#pragma unroll
+    for (int i = 0; i < NS / 2; ++i) {
+        const float2 x = fmul2_rn(s2, A[i]);
+        f[i] = make_float2(exp2_hw(x.x), exp2_hw(x.y));
+    }
+}
+template <int NS>
+__device__ __forceinline__ void inputs(float2 (&bu)[NS / 2], float su, const float *B) {
+    const float2 su2 = make_float2(su, su);
 #pragma unroll
     for (int i = 0; i < NS / 2; i += 2) {
         const float4 b = *reinterpret_cast<const float4 *>(B + 2 * i);
-        float2 x = fmul2_rn(s2, A[i]), x1 = fmul2_rn(s2, A[i + 1]);
-        x.x = exp2_hw(x.x), x.y = exp2_hw(x.y), x1.x = exp2_hw(x1.x), x1.y = exp2_hw(x1.y);
-        h[i] = ffma2_rn(x, h[i], fmul2_rn(su2, make_float2(b.x, b.y)));
-        h[i + 1] = ffma2_rn(x1, h[i + 1], fmul2_rn(su2, make_float2(b.z, b.w)));
+        bu[i] = fmul2_rn(su2, make_float2(b.x, b.y));
+        bu[i + 1] = fmul2_rn(su2, make_float2(b.z, b.w));
     }
 }
 template <int NS>
@@ -400,12 +403,15 @@ __device__ __forceinline__ float dot(const float2 (&h)[NS / 2], const float *C) 
 }
 
 template <typename T, int NS, int L, bool VEC>
-__global__ void __launch_bounds__(32 * ScanWarp<NS, L>::kBlockWarps, 3) ssm_scan_kernel(const ScanArgs a) {
+__global__ void __launch_bounds__(32 * ScanWarp<NS, L>::kBlockWarps, sizeof(T) == 4 ? 2 : 3) ssm_scan_kernel(const ScanArgs a) {
     using Sh = ScanWarp<NS, L>;
     constexpr int V = Sh::V, R = Sh::kRuns, W = Sh::kBlockWarps, BC = Sh::kBCEach;
     __shared__ Sh all[W];
+    __shared__ typename Sh::Part whole;  // of the block's parts together
+    __shared__ __align__(16) float all_y[W][kTile][Sh::kChans];  // sums over the states (apart: nothing else may be waited for with them)
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     Sh &sh = all[warp];
+    float(&yw)[kTile][Sh::kChans] = all_y[warp];
     const int64_t at = (int64_t)blockIdx.x * W + warp;
     const int rank = (int)at & (a.parts - 1);  // (parts is a power of two)
     int64_t unit = at >> (31 - __clz(a.parts));
@@ -426,20 +432,6 @@ __global__ void __launch_bounds__(32 * ScanWarp<NS, L>::kBlockWarps, 3) ssm_scan
     for (int v = 0; v < V; ++v) {
         bias[v] = a.dt_bias && v < left ? __ldg(a.dt_bias + d0 + run + v) : 0.0f;
         skip[v] = a.skip && v < left ? __ldg(a.skip + d0 + run + v) : 0.0f;
-    }
-    // and in the recurrence: channel c, states n0 .. n0 + NS
-    const int c = lane / L, q = lane % L, n0 = q * NS;
-    float2 A[NS / 2], h[NS / 2];
-    const bool start = there && rank == 0 && a.state_in;
-#pragma unroll
-    for (int i = 0; i < NS; ++i) {
-        const bool ok = c < chans && n0 + i < a.N;
-        const float v = ok ? __fmul_rn(__ldg(a.A + (d0 + c) * a.N + n0 + i), kLog2e) : 0.0f;
-        const float s = ok && start ? a.state_in[(b * a.D + d0 + c) * a.N + n0 + i] : 0.0f;
-        if (i & 1)
-            A[i / 2].y = v, h[i / 2].y = s;
-        else
-            A[i / 2].x = v, h[i / 2].x = s;
     }
     // the next tile's values, and where they lie
     Run<T, V> ru[R], rd[R], rz[R];
@@ -491,6 +483,22 @@ __global__ void __launch_bounds__(32 * ScanWarp<NS, L>::kBlockWarps, 3) ssm_scan
             if (final) fetch_bc(t0, rC, pC, a.Cm_frame);
         }
     };
+    seek(first);
+    fetch(first, a.parts == 1);
+    // and in the recurrence: channel c, states n0 .. n0 + NS
+    const int c = lane / L, q = lane % L, n0 = q * NS;
+    float2 A[NS / 2], h[NS / 2];
+    const bool start = there && rank == 0 && a.state_in;
+#pragma unroll
+    for (int i = 0; i < NS; ++i) {
+        const bool ok = c < chans && n0 + i < a.N;
+        const float v = ok ? __fmul_rn(__ldg(a.A + (d0 + c) * a.N + n0 + i), kLog2e) : 0.0f;
+        const float s = ok && start ? a.state_in[(b * a.D + d0 + c) * a.N + n0 + i] : 0.0f;
+        if (i & 1)
+            A[i / 2].y = v, h[i / 2].y = s;
+        else
+            A[i / 2].x = v, h[i / 2].x = s;
+    }
     auto stage = [&](int t0, bool final) {  // a frame that is not there has a step of 0, which leaves the states as they are
         if constexpr (!Sh::kBCAhead) {
             fetch_bc(t0, rB, pB, a.Bm_frame);
@@ -529,8 +537,6 @@ __global__ void __launch_bounds__(32 * ScanWarp<NS, L>::kBlockWarps, 3) ssm_scan
 #pragma unroll
         for (int i = 0; i < NS / 2; ++i) sh.start[i][lane] = h[i];
         float sum = 0.0f;
-        seek(first);
-        fetch(first, false);
         for (int t0 = first; t0 < last; t0 += kTile) {
             stage(t0, false);
             __syncwarp();
@@ -539,40 +545,80 @@ __global__ void __launch_bounds__(32 * ScanWarp<NS, L>::kBlockWarps, 3) ssm_scan
             for (int t = 0; t < kTile; ++t) {
                 const float2 s = sh.s[t][c];
                 sum = __fadd_rn(sum, s.x);
-                advance<NS>(h, A, s.x, s.y, &sh.B[t][n0]);
+                float2 f[NS / 2], bu[NS / 2];
+                factors<NS>(f, A, s.x);
+                inputs<NS>(bu, s.y, &sh.B[t][n0]);
+#pragma unroll
+                for (int k = 0; k < NS / 2; ++k) h[k] = ffma2_rn(f[k], h[k], bu[k]);
             }
             __syncwarp();
         }
 #pragma unroll
         for (int i = 0; i < NS; ++i) sh.part[i][lane] = i & 1 ? h[i / 2].y : h[i / 2].x;
         sh.sum[lane] = sum;
+        seek(first);  // the second pass's first loads are in flight meanwhile
+        fetch(first, true);
+        // the parts of a block, then those of the blocks before it, which the last warp of each has put together. `first_part`
+        // takes r as it is: nothing lies before it
         const bool cluster = a.parts > W;
+        const int w0 = cluster ? 0 : warp - rank;  // the first part's warp in this block
+        auto compose = [&](float2 (&to)[NS / 2], float s, const float (&r)[NS], bool first_part) {
+#pragma unroll
+            for (int k = 0; k < NS / 2; ++k) {
+                to[k].x = first_part ? r[2 * k] : __fmaf_rn(exp2_hw(__fmul_rn(s, A[k].x)), to[k].x, r[2 * k]);
+                to[k].y = first_part ? r[2 * k + 1] : __fmaf_rn(exp2_hw(__fmul_rn(s, A[k].y)), to[k].y, r[2 * k + 1]);
+            }
+        };
+        auto compose_warps = [&](float2 (&to)[NS / 2], int end, bool first_part) {  // and the sum of their steps
+            float total = 0.0f;
+            for (int w = w0; w < end; ++w) {
+                float r[NS];
+#pragma unroll
+                for (int k = 0; k < NS; ++k) r[k] = all[w].part[k][lane];
+                compose(to, all[w].sum[lane], r, first_part && w == w0);
+                total = __fadd_rn(total, all[w].sum[lane]);
+            }
+            return total;
+        };
+        __syncthreads();
         if (cluster) {
+            const int block = rank / W;
+            if (warp == W - 1) {
+                const float total = compose_warps(h, W, true);
+#pragma unroll
+                for (int k = 0; k < NS; ++k) whole.part[k][lane] = k & 1 ? h[k / 2].y : h[k / 2].x;
+                whole.sum[lane] = total;
+            }
             cluster_arrive();
             cluster_wait();
-        } else {
-            __syncthreads();
-        }
 #pragma unroll
-        for (int i = 0; i < NS / 2; ++i) h[i] = sh.start[i][lane];
-        const int w0 = warp - rank;  // (in one block) the first part's warp
-        for (int p = 0; p < rank; ++p) {
-            const Sh &its = all[cluster ? p % W : w0 + p];
-            auto get = [&](const float &v) { return cluster ? peer_load(peer_address(&v, p / W)) : v; };
-            const float s = get(its.sum[lane]);
+            for (int i = 0; i < NS / 2; ++i) h[i] = sh.start[i][lane];
+            constexpr int kAtOnce = 4;  // blocks whose values are loaded together
+            for (int p0 = 0; p0 < block; p0 += kAtOnce) {
+                float s[kAtOnce], r[kAtOnce][NS];
 #pragma unroll
-            for (int i = 0; i < NS / 2; ++i) {
-                const float x = get(its.part[2 * i][lane]), y = get(its.part[2 * i + 1][lane]);
-                h[i].x = p ? __fmaf_rn(exp2_hw(__fmul_rn(s, A[i].x)), h[i].x, x) : x;
-                h[i].y = p ? __fmaf_rn(exp2_hw(__fmul_rn(s, A[i].y)), h[i].y, y) : y;
+                for (int i = 0; i < kAtOnce; ++i) {
+                    if (p0 + i >= block) break;
+                    s[i] = peer_load(peer_address(&whole.sum[lane], p0 + i));
+#pragma unroll
+                    for (int k = 0; k < NS; ++k) r[i][k] = peer_load(peer_address(&whole.part[k][lane], p0 + i));
+                }
+#pragma unroll
+                for (int i = 0; i < kAtOnce; ++i) {
+                    if (p0 + i >= block) break;
+                    compose(h, s[i], r[i], p0 + i == 0);
+                }
             }
+            cluster_arrive();  // waited for at the end: the others may still read this block's
+            compose_warps(h, warp, block == 0);
+        } else {
+#pragma unroll
+            for (int i = 0; i < NS / 2; ++i) h[i] = sh.start[i][lane];
+            compose_warps(h, warp, true);
         }
-        if (cluster) cluster_arrive();  // waited for at the end: the others may still read this block's parts
     }
 
     constexpr int kSteps = L > 8 ? L : 8;  // frames between stores: their loads and products overlap
-    seek(first);
-    fetch(first, true);
     T *py = static_cast<T *>(a.y) + b * a.y_seq + (first + row) * a.y_frame + d0 + run;
     for (int t0 = first; t0 < last; t0 += kTile) {
         stage(t0, true);
@@ -584,24 +630,37 @@ __global__ void __launch_bounds__(32 * ScanWarp<NS, L>::kBlockWarps, 3) ssm_scan
 #pragma unroll 1
         for (int tb = 0; tb < kTile; tb += kSteps) {
             float y[kSteps];
+            float2 f[NS / 2];  // a frame's factors are formed beside the products of the one before
+            float su = sh.s[tb][c].y;
+            factors<NS>(f, A, sh.s[tb][c].x);
 #pragma unroll
             for (int i = 0; i < kSteps; ++i) {
-                const float2 s = sh.s[tb + i][c];
-                advance<NS>(h, A, s.x, s.y, &sh.B[tb + i][n0]);
+                const int next = i + 1 < kSteps ? tb + i + 1 : tb;
+                float2 bu[NS / 2], f1[NS / 2];
+                inputs<NS>(bu, su, &sh.B[tb + i][n0]);
+                const float2 s = sh.s[next][c];
+                if (i + 1 < kSteps) factors<NS>(f1, A, s.x);
+#pragma unroll
+                for (int k = 0; k < NS / 2; ++k) h[k] = ffma2_rn(f[k], h[k], bu[k]);
                 y[i] = dot<NS>(h, &sh.C[tb + i][n0]);
+                if (i + 1 < kSteps) {
+                    su = s.y;
+#pragma unroll
+                    for (int k = 0; k < NS / 2; ++k) f[k] = f1[k];
+                }
             }
             // the sums of L frames at a time over L lanes: each exchange halves the frames a lane holds, until lane q has
             // frame q of them
 #pragma unroll
-            for (int f = 0; f < kSteps; f += L) {
+            for (int r = 0; r < kSteps; r += L) {
 #pragma unroll
                 for (int o = L / 2; o > 0; o >>= 1)
 #pragma unroll
                     for (int i = 0; i < o; ++i) {
-                        const float send = q & o ? y[f + i] : y[f + i + o], keep = q & o ? y[f + i + o] : y[f + i];
-                        y[f + i] = __fadd_rn(keep, __shfl_xor_sync(0xffffffffu, send, o));
+                        const float send = q & o ? y[r + i] : y[r + i + o], keep = q & o ? y[r + i + o] : y[r + i];
+                        y[r + i] = __fadd_rn(keep, __shfl_xor_sync(0xffffffffu, send, o));
                     }
-                sh.y[tb + f + q][c] = y[f];
+                yw[tb + r + q][c] = y[r];
             }
         }
         __syncwarp();
@@ -614,7 +673,7 @@ __global__ void __launch_bounds__(32 * ScanWarp<NS, L>::kBlockWarps, 3) ssm_scan
                 for (int v = 0; v < V; v += 2) {
                     const int w = v + 1 < V ? v + 1 : v;
                     float2 y = ffma2_rn(make_float2(skip[v], skip[w]), make_float2(cu[j].get(v), cu[j].get(w)),
-                                        make_float2(sh.y[r][run + v], sh.y[r][run + w]));
+                                        make_float2(yw[r][run + v], yw[r][run + w]));
                     if (a.z) y = fmul2_rn(y, silu2(make_float2(rz[j].get(v), rz[j].get(w))));
                     o[v] = y.x;
                     if (w > v) o[w] = y.y;
