@@ -359,7 +359,7 @@ struct ScanWarp {
     static constexpr int kRowLanes = kChans / V, kRows = 32 / kRowLanes;  // lanes a frame, frames a load
     static constexpr int kBCEach = (kTile * kStates / 4 + 31) / 32;       // runs of four a lane loads of Bm and Cm
     static constexpr bool kBCAhead = kBCEach <= 4;       // a tile ahead, while registers allow it
-    static constexpr int kBlockWarps = 4;
+    static constexpr int kBlockWarps = kStates <= 64 ? 4 : 2;  // (48 KB of shared memory a block)
 
     alignas(16) float2 s[kTile][kChans];  // steps s and s u
     alignas(16) float B[kTile][kStates], C[kTile][kStates];
