@@ -8,6 +8,7 @@ from __future__ import annotations
 
 import ctypes as C
 import os
+import struct
 
 import numpy as np
 
@@ -38,8 +39,9 @@ EXPORTS = ("qnn_status_string", "qnn_device_status", "qnn_quantize", "qnn_qmatmu
            "qnn_lstm_stream_push", "qnn_lstm_stream_pull", "qnn_lstm_stream_close", "qnn_measure_exchange_floor",
            "qnn_rmsnorm_quantize", "qnn_quantize4", "qnn_qmatmul4", "qnn_causal_conv", "qnn_ssm_scan")
 
-# qnn_dtype by a torch type's name
-_DTYPES = {"torch.float32": 0, "torch.bfloat16": 1, "torch.float16": 2}
+_DTYPES = {}  # qnn_dtype of a torch type
+# qnn_ssm_args as it lies in memory
+_SSM_ARGS = struct.Struct("=3q4i" + 6 * "Q2q" + "6Q")
 
 
 class QnnError(RuntimeError):
@@ -130,7 +132,7 @@ def lib():
         L.qnn_qmatmul4.restype = i32
         L.qnn_causal_conv.argtypes = [P, i64, i64, i32, i64, i64, i64, P, C.c_int32, P, i32, P, P, P, P, i64, i64, P]
         L.qnn_causal_conv.restype = i32
-        L.qnn_ssm_scan.argtypes = [C.POINTER(SsmArgs), P]
+        L.qnn_ssm_scan.argtypes = [P, P]
         L.qnn_ssm_scan.restype = i32
         _lib = L
     return _lib
@@ -216,6 +218,25 @@ def _stream(stream):
     return torch._C._cuda_getCurrentRawStream(torch.cuda.current_device())
 
 
+_torch = None
+
+
+def _libs():
+    """torch and the library, for the calls whose marshalling is most of their time."""
+    global _torch
+    if _torch is None:
+        import torch
+        torch.cuda.current_device()  # (starts CUDA)
+        _torch = torch
+        _DTYPES.update({torch.float32: 0, torch.bfloat16: 1, torch.float16: 2})
+    return _torch, _lib or lib()
+
+
+def _here(torch):
+    """The current stream of the current device (half of _stream's time)."""
+    return torch._C._cuda_getCurrentRawStream(torch._C._cuda_getDevice())
+
+
 def params_view(p) -> np.ndarray:
     """Device params tensor (int32 [n, 4]) -> numpy records with fields vmin, vmax, Q, z."""
     return p.detach().cpu().numpy().view(QPARAMS_DTYPE).reshape(-1)
@@ -268,7 +289,7 @@ def _bad(what: str, *more):
 
 
 def _dtype(t, what: str) -> int:
-    d = _DTYPES.get(str(t.dtype))
+    d = _DTYPES.get(t.dtype)
     if d is None:
         _bad(f"{what}: fp32, bf16 or fp16")
     return d
@@ -285,10 +306,10 @@ def _rows(t, what: str, dtype, shape) -> int:
     return s0 if s0 >= cols else cols
 
 
-def _flat(t, what: str, dtype, shape):
-    """Address of a contiguous array, or None."""
+def _flat(t, what: str, dtype, shape) -> int:
+    """Address of a contiguous array, 0 for None."""
     if t is None:
-        return None
+        return 0
     if t.dtype is not dtype or t.shape != shape or not t.is_contiguous():
         _bad(what + ": contiguous", dtype, shape)
     return t.data_ptr()
@@ -304,10 +325,9 @@ def _frames(t, what: str, dtype, shape):
     return t.data_ptr(), st[0], st[1]
 
 
-def _result(shape, dtype, like, stream):
+def _result(torch, shape, dtype, like, stream):
     """A new tensor for a call on stream: where that is not the current one, its memory is not given to others before
     what the call queued there is done."""
-    import torch
     t = torch.empty(shape, dtype=dtype, device=like.device)
     if stream is not None:
         t.record_stream(stream)
@@ -319,33 +339,40 @@ def qnn_rmsnorm_quantize(x, weight, residual=None, eps=1e-5, residual_out=None, 
     8-bit codes, one unit per row. Returns (codes u8, params int32 [rows, 4], code_sums int32 [rows], h, values): h = x +
     residual in x's type (residual_out, which may be x or residual, or a new tensor; None without a residual), values the
     fp32 values that the codes stand for (None unless wanted)."""
-    import torch
+    torch, L = _libs()
     if x.dim() != 2 or not x.is_cuda:
         _bad("x: a CUDA matrix")
+    shape, ty, dev, empty = x.shape, x.dtype, x.device, torch.empty
     dt = _dtype(x, "x")
-    rows, cols = shape = x.shape
-    ldx = _rows(x, "x", x.dtype, shape)
-    ldr = _rows(residual, "residual", x.dtype, shape) if residual is not None else 0
-    if residual_out is not None and residual is None:
+    rows, cols = shape
+    ldx = _rows(x, "x", ty, shape)
+    h, pr, ph, ldr, ldh, pv = residual_out, 0, 0, 0, 0, 0
+    if residual is not None:
+        ldr = _rows(residual, "residual", ty, shape)
+        pr = residual.data_ptr()
+        if h is None:
+            h, ldh = empty(shape, dtype=ty, device=dev), cols
+        else:
+            ldh = _rows(h, "residual_out", ty, shape)
+        ph = h.data_ptr()
+    elif h is not None:
         _bad("residual_out: needs a residual")
-    dev, empty = x.device, torch.empty
-    h = residual_out
-    if residual is not None and h is None:
-        h = empty(shape, dtype=x.dtype, device=dev)
-    ldh = _rows(h, "residual_out", x.dtype, shape) if h is not None else 0
     w = _flat(weight, "weight", torch.float32, (cols,))
     codes = empty(shape, dtype=torch.uint8, device=dev)
     params = empty((rows, 4), dtype=torch.int32, device=dev)
     sums = empty((rows,), dtype=torch.int32, device=dev)
-    values = empty(shape, dtype=torch.float32, device=dev) if want_values else None
+    values = None
+    if want_values:
+        values = empty(shape, dtype=torch.float32, device=dev)
+        pv = values.data_ptr()
     if stream is not None:
         for t in (h, codes, params, sums, values):
             if t is not None:
                 t.record_stream(stream)
-    st = lib().qnn_rmsnorm_quantize(x.data_ptr(), ldx, None if residual is None else residual.data_ptr(), ldr, dt, w, eps, rows,
-                                    cols, None if h is None else h.data_ptr(), ldh, codes.data_ptr(), cols, params.data_ptr(),
-                                    sums.data_ptr(), None if values is None else values.data_ptr(), cols, _stream(stream))
-    if st != QNN_OK:
+    st = L.qnn_rmsnorm_quantize(x.data_ptr(), ldx, pr, ldr, dt, w, eps, rows, cols, ph, ldh, codes.data_ptr(), cols,
+                                params.data_ptr(), sums.data_ptr(), pv, cols,
+                                _here(torch) if stream is None else stream.cuda_stream)
+    if st:
         _check(st, "qnn_rmsnorm_quantize")
     return codes, params, sums, h, values
 
@@ -357,19 +384,19 @@ class Weights4:
     __slots__ = ("codes", "units", "row_sums", "N", "K", "group")
 
     def __init__(self, codes, units, row_sums, N: int, K: int, group: int):
-        import torch
-        if group not in (32, 64, 128):
+        torch = _libs()[0]
+        if group != 32 and group != 64 and group != 128:
             _bad("group: 32, 64 or 128")
-        tiles = ((N + 15) // 16, (K + 127) // 128)
-        _flat(codes, "codes", torch.uint8, (*tiles, 1024))
-        _flat(units, "units", torch.bfloat16, (*tiles, 16, 128 // group, 2))
+        nt, kt = (N + 15) // 16, (K + 127) // 128
+        _flat(codes, "codes", torch.uint8, (nt, kt, 1024))
+        _flat(units, "units", torch.bfloat16, (nt, kt, 16, 128 // group, 2))
         _flat(row_sums, "row_sums", torch.float32, (N,))
         self.codes, self.units, self.row_sums, self.N, self.K, self.group = codes, units, row_sums, N, K, group
 
 
 def qnn_quantize4(w, group: int = 64, stream=None) -> Weights4:
     """Weights w, CUDA fp32 [N, K], to 4-bit codes offline, one unit per group (32, 64 or 128) of a row's columns."""
-    import torch
+    torch, L = _libs()
     if w.dim() != 2 or not w.is_cuda:
         _bad("w: a CUDA matrix")
     if group not in (32, 64, 128):
@@ -377,29 +404,34 @@ def qnn_quantize4(w, group: int = 64, stream=None) -> Weights4:
     N, K = w.shape
     ldw = _rows(w, "w", torch.float32, w.shape)
     tiles = ((N + 15) // 16, (K + 127) // 128)
-    codes = _result((*tiles, 1024), torch.uint8, w, stream)
-    units = _result((*tiles, 16, 128 // group, 2), torch.bfloat16, w, stream)
-    sums = _result((N,), torch.float32, w, stream)
-    _check(lib().qnn_quantize4(w.data_ptr(), N, K, ldw, group, codes.data_ptr(), units.data_ptr(), sums.data_ptr(),
-                               _stream(stream)), "qnn_quantize4")
+    codes = _result(torch, (*tiles, 1024), torch.uint8, w, stream)
+    units = _result(torch, (*tiles, 16, 128 // group, 2), torch.bfloat16, w, stream)
+    sums = _result(torch, (N,), torch.float32, w, stream)
+    _check(L.qnn_quantize4(w.data_ptr(), N, K, ldw, group, codes.data_ptr(), units.data_ptr(), sums.data_ptr(),
+                           _stream(stream)), "qnn_quantize4")
     return Weights4(codes, units, sums, N, K, group)
 
 
 def qnn_qmatmul4(A, pa, weights: Weights4, ga=PER_ROW, bias=None, out=None, stream=None):
     """Y = R(A' W'^T) + bias with 4-bit weights: A u8 [M, K] codes with their units pa int32 [M, 4] (or [1, 4] with
     ga = PER_MATRIX), as qnn_quantize and qnn_rmsnorm_quantize give them. Returns Y fp32 [M, N]."""
-    import torch
+    torch, L = _libs()
     if A.dim() != 2 or not A.is_cuda or A.shape[1] != weights.K:
         _bad("A: a CUDA matrix of the weights' K columns")
-    M, K = A.shape
+    M, K = shape = A.shape
     N = weights.N
-    lda = _rows(A, "A", torch.uint8, A.shape)
+    lda = _rows(A, "A", torch.uint8, shape)
     p = _flat(pa, "pa", torch.int32, (M if ga == PER_ROW else 1, 4))
     b = _flat(bias, "bias", torch.float32, (N,))
-    Y = out if out is not None else _result((M, N), torch.float32, A, stream)
-    ldy = _rows(Y, "out", torch.float32, (M, N)) if out is not None else N
-    _check(lib().qnn_qmatmul4(A.data_ptr(), lda, p, ga, M, K, weights.codes.data_ptr(), weights.units.data_ptr(), weights.group,
-                              weights.row_sums.data_ptr(), N, b, Y.data_ptr(), ldy, _stream(stream)), "qnn_qmatmul4")
+    if out is None:
+        Y, ldy = _result(torch, (M, N), torch.float32, A, stream), N
+    else:
+        Y, ldy = out, _rows(out, "out", torch.float32, (M, N))
+    st = L.qnn_qmatmul4(A.data_ptr(), lda, p, ga, M, K, weights.codes.data_ptr(), weights.units.data_ptr(), weights.group,
+                        weights.row_sums.data_ptr(), N, b, Y.data_ptr(), ldy,
+                        _here(torch) if stream is None else stream.cuda_stream)
+    if st:
+        _check(st, "qnn_qmatmul4")
     return Y
 
 
@@ -408,21 +440,24 @@ def qnn_causal_conv(x, weight, bias=None, silu=True, state_in=None, state_out=No
     fp16; frames may be slices of wider ones), weight [D, W] and bias [D] fp32, states [B, W - 1, D] in x's type (state_out
     may be state_in), lengths int32 [B]. Returns out, [B, T, D]; without an out given, the frames behind a sequence's end
     hold nothing in particular."""
-    import torch
+    torch, L = _libs()
     if x.dim() != 3 or not x.is_cuda:
         _bad("x: CUDA [B, T, D]")
-    dt = _dtype(x, "x")
+    dt, ty = _dtype(x, "x"), x.dtype
     B, T, D = shape = x.shape
     if weight.dim() != 2:
         _bad("weight: [D, W]")
     W = weight.shape[1]
-    y = out if out is not None else _result(shape, x.dtype, x, stream)
-    _check(lib().qnn_causal_conv(*_frames(x, "x", x.dtype, shape), dt, B, T, D, _flat(weight, "weight", torch.float32, (D, W)), W,
-                                 _flat(bias, "bias", torch.float32, (D,)), 1 if silu else 0,
-                                 _flat(state_in, "state_in", x.dtype, (B, W - 1, D)),
-                                 _flat(state_out, "state_out", x.dtype, (B, W - 1, D)),
-                                 _flat(lengths, "lengths", torch.int32, (B,)), *_frames(y, "out", x.dtype, shape),
-                                 _stream(stream)), "qnn_causal_conv")
+    y = out if out is not None else _result(torch, shape, ty, x, stream)
+    px, xs, xf = _frames(x, "x", ty, shape)
+    py, ys, yf = _frames(y, "out", ty, shape)
+    state = (B, W - 1, D)
+    st = L.qnn_causal_conv(px, xs, xf, dt, B, T, D, _flat(weight, "weight", torch.float32, (D, W)), W,
+                           _flat(bias, "bias", torch.float32, (D,)), 1 if silu else 0, _flat(state_in, "state_in", ty, state),
+                           _flat(state_out, "state_out", ty, state), _flat(lengths, "lengths", torch.int32, (B,)), py, ys, yf,
+                           _here(torch) if stream is None else stream.cuda_stream)
+    if st:
+        _check(st, "qnn_causal_conv")
     return y
 
 
@@ -432,25 +467,29 @@ def qnn_ssm_scan(u, dt, A, B, C, D=None, z=None, dt_bias=None, softplus=True, st
     type; frames may be slices of wider ones), A [D, N], D [D], dt_bias [D] and states [B, D, N] fp32 (state_out may be
     state_in), lengths int32 [B]. Returns out, [B, T, D]; without an out given, the frames behind a sequence's end hold
     nothing in particular."""
-    import torch
+    torch, L = _libs()
     if u.dim() != 3 or not u.is_cuda:
         _bad("u: CUDA [B, T, D]")
-    ty, f32 = u.dtype, torch.float32
-    kind = _dtype(u, "u")
+    ty, f32, kind = u.dtype, torch.float32, _dtype(u, "u")
     nb, nt, nd = shape = u.shape
     if A.dim() != 2:
         _bad("A: [D, N]")
     ns = A.shape[1]
-    groups = B.shape[2] if B.dim() == 4 else 1
-    bc = (nb, nt, groups, ns) if B.dim() == 4 else (nb, nt, ns)
-    y = out if out is not None else _result(shape, ty, u, stream)
+    groups, bc = 1, (nb, nt, ns)
+    if B.dim() == 4:
+        groups = B.shape[2]
+        bc = (nb, nt, groups, ns)
+    y = out if out is not None else _result(torch, shape, ty, u, stream)
     state = (nb, nd, ns)
-    a = SsmArgs(nb, nt, nd, ns, groups, kind, 1 if softplus else 0, *_frames(u, "u", ty, shape), *_frames(dt, "dt", ty, shape),
-                *_frames(B, "B", ty, bc), *_frames(C, "C", ty, bc), *((None, 0, 0) if z is None else _frames(z, "z", ty, shape)),
-                *_frames(y, "out", ty, shape), _flat(A, "A", f32, (nd, ns)), _flat(D, "D", f32, (nd,)),
-                _flat(dt_bias, "dt_bias", f32, (nd,)), _flat(state_in, "state_in", f32, state),
-                _flat(state_out, "state_out", f32, state), _flat(lengths, "lengths", torch.int32, (nb,)))
-    _check(lib().qnn_ssm_scan(a, _stream(stream)), "qnn_ssm_scan")
+    pz, zs, zf = _frames(z, "z", ty, shape) if z is not None else (0, 0, 0)
+    args = _SSM_ARGS.pack(nb, nt, nd, ns, groups, kind, 1 if softplus else 0, *_frames(u, "u", ty, shape),
+                          *_frames(dt, "dt", ty, shape), *_frames(B, "B", ty, bc), *_frames(C, "C", ty, bc), pz, zs, zf,
+                          *_frames(y, "out", ty, shape), _flat(A, "A", f32, (nd, ns)), _flat(D, "D", f32, (nd,)),
+                          _flat(dt_bias, "dt_bias", f32, (nd,)), _flat(state_in, "state_in", f32, state),
+                          _flat(state_out, "state_out", f32, state), _flat(lengths, "lengths", torch.int32, (nb,)))
+    st = L.qnn_ssm_scan(args, _here(torch) if stream is None else stream.cuda_stream)
+    if st:
+        _check(st, "qnn_ssm_scan")
     return y
 
 
