@@ -1,6 +1,7 @@
 // qgemm4.cu — 4-bit weights in units of `group` columns of a row (Sec. 3.1's sub-matrices, eq. 2 with S = 15) and their
 // product with rows of 8-bit activation codes, recovered to fp32 (eq. 1, eq. 3) on sm_103a.
 #include <algorithm>
+#include <atomic>
 
 #include <cuda_fp16.h>
 
@@ -85,9 +86,11 @@ struct Mm4Args {
     float *Y;
     int64_t lda, ldy, M, N;
     int K, ktiles, per_row;
-    int segments;     // warps that share a row tile's columns; the block's other warps take other row tiles
-    int64_t items;    // blocks' shares of row tiles
-    int chunk, stride;  // column tiles of A in shared memory at once, bytes of a row of them
+    int seg_shift;    // 2^seg_shift warps share a row tile's columns; the block's other warps take other row tiles
+    int blocks, span; // of a cluster, which share the columns of its row tiles, and the column tiles of one
+    int64_t items;    // clusters' shares of row tiles
+    int chunks, chunk, stride;  // column tiles of A in shared memory at once, how often, and bytes of a row of them
+    uint32_t per_row_magic;     // ceil(2^32 / (8 chunk)): divides by the steps of a row of a whole chunk
     int align;        // of A's rows, 16, 4 or 1
 };
 
@@ -130,7 +133,7 @@ __device__ __forceinline__ uint32_t codes_x1(uint32_t v) {
 // contiguous stretches) and add up through shared memory at the end, in a fixed order. Bound: the weights' bytes. Each
 // warp streams its own column tiles through kStages slots of shared memory by asynchronous copies, across row tiles, so that
 // 16 kStages KB a block are in flight at any time; a slot is read into registers and filled again before its products.
-constexpr int kMmThreads = 512, kMmWarps = kMmThreads / 32, kRedStride = 20;
+constexpr int kMmThreads = 512, kMmWarps = kMmThreads / 32, kRedStride = 20, kMostBlocks = 4;
 constexpr float kUnit = 0x1p-20f, kPerUnit = 0x1p20f;
 
 __device__ __forceinline__ void copy16_async(uint32_t to, const void *from) {
@@ -159,6 +162,22 @@ struct Units {  // of a row's 128 columns
     }
 };
 
+// All threads of the block, or of the cluster, and what they wrote to shared memory.
+__device__ __forceinline__ void all_here(bool cluster) {
+    if (cluster)
+        asm volatile("barrier.cluster.arrive.release;\n barrier.cluster.wait.acquire;" ::: "memory");
+    else
+        __syncthreads();
+}
+// A shared variable of another block of the cluster.
+__device__ __forceinline__ float peer_load(const float *p, int rank) {
+    uint32_t at;
+    float v;
+    asm("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(at) : "r"((uint32_t)__cvta_generic_to_shared(p)), "r"(rank));
+    asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v) : "r"(at) : "memory");
+    return v;
+}
+
 template <int GROUP, int NT>
 struct Mm4Plan {
     static constexpr int kRows = 8 * NT, kGroups = kTileCols / GROUP;
@@ -181,18 +200,21 @@ __global__ void __launch_bounds__(kMmThreads, 1) qmatmul4_kernel(const Mm4Args a
     float *reds = reinterpret_cast<float *>(smem + P::kRing);        // [kReds][warps][kRows][kRedStride]
     uint8_t *sA = smem + P::kRing + P::kReds * P::kRed;              // [rows][stride]
     float *sR = reinterpret_cast<float *>(sA + rows * a.stride);     // [chunk groups][kRows]: group sums of b - 128
-    const int seg = warp % a.segments, tile_group = warp / a.segments, tile_groups = kMmWarps / a.segments;
+    const int segments = 1 << a.seg_shift, seg = warp & (segments - 1), tile_group = warp >> a.seg_shift;
+    const int tile_groups = kMmWarps >> a.seg_shift;
+    const int rank = a.blocks > 1 ? (int)(blockIdx.x & (a.blocks - 1)) : 0;  // (of the cluster: its size divides the grid)
+    const int64_t first_item = blockIdx.x / a.blocks, item_step = gridDim.x / a.blocks;
+    const int kt_begin = rank * a.span, kt_end = min(a.ktiles, kt_begin + a.span);
     const int64_t ntiles = (a.N + kTileRows - 1) / kTileRows;
-    const int chunks = (a.ktiles + a.chunk - 1) / a.chunk;
 
     // the copies' place: the next of `left` column tiles of this warp's row tile of item_next
     const uint32_t ring_at = (uint32_t)__cvta_generic_to_shared(ring) + 16 * lane;
-    const int steps = seg < a.ktiles ? (a.ktiles - 1 - seg) / a.segments + 1 : 0;
-    int64_t item_next = blockIdx.x;
+    const int steps = (max(kt_end - kt_begin - seg, 0) + segments - 1) >> a.seg_shift;
+    int64_t item_next = first_item;
     int left = 0;
     const uint8_t *code_next = nullptr, *unit_next = nullptr;
     auto seek = [&]() {
-        const int64_t tile = item_next * tile_groups + tile_group, at = tile * a.ktiles + seg;
+        const int64_t tile = item_next * tile_groups + tile_group, at = tile * a.ktiles + kt_begin + seg;
         left = item_next < a.items && tile < ntiles ? steps : 0;
         code_next = a.codes + at * kTileBytes + 16 * lane;
         unit_next = reinterpret_cast<const uint8_t *>(a.units) + at * P::kUnitBytes + 16 * lane;
@@ -204,10 +226,10 @@ __global__ void __launch_bounds__(kMmThreads, 1) qmatmul4_kernel(const Mm4Args a
             copy16_async(to, code_next);
             copy16_async(to + 512, code_next + 512);
             if (16 * lane < P::kUnitBytes) copy16_async(to + kTileBytes, unit_next);
-            code_next += a.segments * kTileBytes;
-            unit_next += a.segments * P::kUnitBytes;
+            code_next += kTileBytes << a.seg_shift;
+            unit_next += P::kUnitBytes << a.seg_shift;
             if (--left == 0) {
-                item_next += gridDim.x;
+                item_next += item_step;
                 seek();
             }
         }
@@ -217,32 +239,33 @@ __global__ void __launch_bounds__(kMmThreads, 1) qmatmul4_kernel(const Mm4Args a
     for (int i = 0; i < P::kStages; ++i) issue(i);
     int slot = 0, red_at = 0;
     // what this thread's first output of a row tile needs is loaded ahead
-    const int wide = tile_groups * kTileRows;
-    const bool mine = tid < wide * rows;
+    const int wide_shift = 8 - a.seg_shift, wide = 1 << wide_shift;  // columns of an item: 16 a tile group
+    const int share = wide * rows / a.blocks, first_out = rank * share;  // this block's outputs of them
+    const bool mine = tid < share;
     qnn_qparams my_unit = {};
-    if (mine) my_unit = a.pa[a.per_row ? m0 + tid / wide : 0];
+    if (mine) my_unit = a.pa[a.per_row ? m0 + ((first_out + tid) >> wide_shift) : 0];
 
-    for (int64_t item = blockIdx.x; item < a.items; item += gridDim.x) {
+    for (int64_t item = first_item; item < a.items; item += item_step) {
         float acc[NT][4] = {}, my_sum = 0.0f, my_bias = 0.0f;
-        if (const int64_t n = item * wide + tid % wide; mine && n < a.N) {
+        if (const int64_t n = item * wide + ((first_out + tid) & (wide - 1)); mine && n < a.N) {
             my_sum = __ldg(a.row_sums + n);
             if (a.bias) my_bias = __ldg(a.bias + n);
         }
-        for (int chunk = 0; chunk < chunks; ++chunk) {
-            const int kt0 = chunk * a.chunk, kt1 = min(a.ktiles, kt0 + a.chunk);
-            if (chunks > 1 || item == blockIdx.x) {
-                if (chunk > 0 || item != blockIdx.x) __syncthreads();  // all warps are done with what was there
+        for (int chunk = 0; chunk < a.chunks; ++chunk) {
+            const int kt0 = min(kt_end, kt_begin + chunk * a.chunk), kt1 = min(kt_end, kt0 + a.chunk);
+            if (a.chunks > 1 || item == first_item) {
+                if (chunk > 0 || item != first_item) __syncthreads();  // all warps are done with what was there
                 // A's codes, 16 a thread and step (past K: 128, which counts 0), as fp16 values, and their sums by groups, over
                 // 2 to 8 lanes; kAtOnce steps' loads in flight
                 constexpr int kAtOnce = NT == 1 ? 2 : 4;
-                const int blocks = (kt1 - kt0) * (kTileCols / 16), total = rows * blocks;
+                const int blocks = a.chunk * (kTileCols / 16), there = (kt1 - kt0) * (kTileCols / 16), total = rows * blocks;
                 for (int i0 = 0; i0 < total; i0 += kAtOnce * kMmThreads) {
                     uint32_t v[kAtOnce][4];
 #pragma unroll
                     for (int s = 0; s < kAtOnce; ++s) {
-                        const int i = i0 + s * kMmThreads + tid, m = i / blocks, k = kt0 * kTileCols + 16 * (i % blocks);
+                        const int i = i0 + s * kMmThreads + tid, m = (int)__umulhi((uint32_t)i, a.per_row_magic), k = kt0 * kTileCols + 16 * (i - m * blocks);
                         v[s][0] = v[s][1] = v[s][2] = v[s][3] = 0x80808080u;
-                        if (i >= total) continue;
+                        if (i >= total || k >= a.K) continue;
                         const uint8_t *p = a.A + (m0 + m) * a.lda + k;
                         if (a.align == 16 && k + 16 <= a.K) {
                             const uint4 x = __ldg(reinterpret_cast<const uint4 *>(p));
@@ -262,13 +285,13 @@ __global__ void __launch_bounds__(kMmThreads, 1) qmatmul4_kernel(const Mm4Args a
                     }
 #pragma unroll
                     for (int s = 0; s < kAtOnce; ++s) {
-                        const int i = i0 + s * kMmThreads + tid, m = i / blocks, blk = i % blocks;
+                        const int i = i0 + s * kMmThreads + tid, m = (int)__umulhi((uint32_t)i, a.per_row_magic), blk = i - m * blocks;
                         uint32_t sum = 0;
 #pragma unroll
                         for (int j = 0; j < 4; ++j) sum = __dp4a(v[s][j], 0x01010101u, sum);
 #pragma unroll
                         for (int o = 1; o < GROUP / 16; o *= 2) sum += __shfl_xor_sync(0xffffffffu, sum, o);
-                        if (i >= total) continue;
+                        if (i >= total || blk >= there) continue;
                         uint4 *to = reinterpret_cast<uint4 *>(sA + m * a.stride + 32 * blk);
                         to[0] = make_uint4(codes_x16(v[s][0]), codes_x1(v[s][0]), codes_x16(v[s][1]), codes_x1(v[s][1]));
                         to[1] = make_uint4(codes_x16(v[s][2]), codes_x1(v[s][2]), codes_x16(v[s][3]), codes_x1(v[s][3]));
@@ -280,7 +303,7 @@ __global__ void __launch_bounds__(kMmThreads, 1) qmatmul4_kernel(const Mm4Args a
             const uint8_t *pa[NT];  // (columns past the rows there are repeat the last: their sums go nowhere)
 #pragma unroll
             for (int c = 0; c < NT; ++c) pa[c] = sA + min(8 * c + g, rows - 1) * a.stride + 16 * t;
-            for (int kt = kt0 + seg; kt < kt1; kt += a.segments) {
+            for (int kt = kt0 + seg; kt < kt1; kt += segments) {
                 copies_wait<P::kStages - 1>();
                 __syncwarp();
                 const uint8_t *at = ring + slot * P::kSlot;
@@ -326,9 +349,9 @@ __global__ void __launch_bounds__(kMmThreads, 1) qmatmul4_kernel(const Mm4Args a
                 }
             }
         }
-        // the segments' sums, in order
+        // the segments' sums, in order, and those of the cluster's blocks
         float *red = reds + red_at * (P::kRed / 4);
-        if (P::kReds == 1 && item != blockIdx.x) __syncthreads();  // the item before is out
+        if (P::kReds == 1 && item != first_item) all_here(a.blocks > 1);  // the item before is out
         if (P::kReds == 2) red_at ^= 1;
 #pragma unroll
         for (int c = 0; c < NT; ++c) {
@@ -336,9 +359,9 @@ __global__ void __launch_bounds__(kMmThreads, 1) qmatmul4_kernel(const Mm4Args a
             p[0] = acc[c][0], p[kRedStride] = acc[c][1];
             p[8] = acc[c][2], p[kRedStride + 8] = acc[c][3];
         }
-        __syncthreads();
-        for (int i = tid; i < wide * rows; i += kMmThreads) {
-            const int m = i / wide, col = i % wide, tg = col / kTileRows, row = col % kTileRows;
+        all_here(a.blocks > 1);
+        for (int i = tid; i < share; i += kMmThreads) {
+            const int o = first_out + i, m = o >> wide_shift, col = o & (wide - 1), tg = col / kTileRows, row = col % kTileRows;
             const int64_t n = item * wide + col;
             if (n >= a.N) continue;
             qnn_qparams p = my_unit;
@@ -348,11 +371,15 @@ __global__ void __launch_bounds__(kMmThreads, 1) qmatmul4_kernel(const Mm4Args a
                 row_sum = __ldg(a.row_sums + n), bias = a.bias ? __ldg(a.bias + n) : 0.0f;
             }
             float sum = 0.0f;
-            for (int k = 0; k < a.segments; ++k)
-                sum = __fadd_rn(sum, red[((tg * a.segments + k) * kRows + m) * kRedStride + row]);
+            for (int b = 0; b < a.blocks; ++b)
+                for (int k = 0; k < segments; ++k) {
+                    const float *at = red + (((tg << a.seg_shift) + k) * kRows + m) * kRedStride + row;
+                    sum = __fadd_rn(sum, b == rank ? *at : peer_load(at, b));
+                }
             a.Y[(m0 + m) * a.ldy + n] = recover4(__fmul_rn(sum, kPerUnit), p.Q, (float)p.z, row_sum, bias);
         }
     }
+    if (a.blocks > 1) all_here(true);  // the others may still read this block's sums
     copies_wait<0>();
 }
 
@@ -360,29 +387,55 @@ template <int GROUP, int NT>
 qnn_status launch_mm4(Mm4Args a, cudaStream_t st) {
     using P = Mm4Plan<GROUP, NT>;
     const int64_t ntiles = (a.N + kTileRows - 1) / kTileRows;
-    // as many warps on a row tile as leave every SM a block, and as have a column tile each
-    a.segments = kMmWarps;
-    while (a.segments > 1 && (a.segments >= 2 * a.ktiles || ntiles * a.segments > (int64_t)kMmWarps * sm_count())) a.segments /= 2;
-    const int64_t per_item = (int64_t)kMmWarps / a.segments;
-    a.items = (ntiles + per_item - 1) / per_item;
-    // as many column tiles of A as fit in shared memory beside the slots and sums, the parts of them even and in whole rounds
+    // A in shared memory: as many column tiles (fp16 values and group sums) as fit beside the slots and sums
     constexpr size_t kMost = 227 * 1024 - 64, kFixed = P::kRing + P::kReds * P::kRed;
-    const int rows = (int)std::min<int64_t>(P::kRows, a.M);
+    const int rows = (int)std::min<int64_t>(P::kRows, a.M), sms = sm_count();
     const size_t sums = (size_t)P::kGroups * P::kRows * 4;  // a column tile's group sums
-    const int fit = (int)std::min<int64_t>(a.ktiles, (int64_t)((kMost - kFixed - (size_t)rows * 64) / ((size_t)rows * 2 * kTileCols + sums)));
-    a.chunk = a.ktiles;
-    if (fit < a.ktiles) {
-        const int whole = fit / a.segments * a.segments, parts = (a.ktiles + whole - 1) / whole;
-        a.chunk = ((a.ktiles + parts - 1) / parts + a.segments - 1) / a.segments * a.segments;
+    const int fit = (int)((kMost - kFixed - (size_t)rows * 64) / ((size_t)rows * 2 * kTileCols + sums));
+    // Blocks that share a row tile's columns: as many as hold all of A between them, and, where row tiles are few, as many as
+    // give half of the SMs one (a column tile each at least). (16 x 8192 x 8192: A twice through one block 18.9 us, two blocks MM4A.)
+    a.blocks = 1;
+    while (a.blocks < kMostBlocks && (a.blocks * fit < a.ktiles || (2 * ntiles * a.blocks <= sms && 2 * a.blocks <= a.ktiles))) a.blocks *= 2;
+    a.span = (a.ktiles + a.blocks - 1) / a.blocks;
+    // as many warps on a row tile as leave every SM a block, and as have a column tile each
+    a.seg_shift = 4;
+    while (a.seg_shift > 0 && ((1 << a.seg_shift) >= 2 * a.span || (ntiles * a.blocks << a.seg_shift) > (int64_t)kMmWarps * sms)) --a.seg_shift;
+    const int segments = 1 << a.seg_shift;
+    a.items = (ntiles * segments + kMmWarps - 1) / kMmWarps;
+    // parts of A that do not fit at once are even, and whole rounds of the warps
+    a.chunk = a.span, a.chunks = 1;
+    if (fit < a.span) {
+        const int whole = fit / segments * segments;
+        a.chunks = (a.span + whole - 1) / whole;
+        a.chunk = ((a.span + a.chunks - 1) / a.chunks + segments - 1) / segments * segments;
     }
     a.stride = a.chunk * 2 * kTileCols + 64;  // (so that the two rows of a quarter of a load lie in different banks)
+    const uint32_t steps = (uint32_t)a.chunk * (kTileCols / 16);
+    a.per_row_magic = (uint32_t)((((uint64_t)1 << 32) + steps - 1) / steps);  // (exact: at most 32 rows of 2072 steps)
     const size_t bytes = kFixed + (size_t)rows * a.stride + (size_t)a.chunk * sums;
     const auto kern = qmatmul4_kernel<GROUP, NT>;
-    if (bytes > 48 * 1024) QNN_CUDA_TRY(cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)bytes));
+    static std::atomic<bool> allowed[64];  // by device: the attribute costs a microsecond a call
+    int dev = 0;
+    QNN_CUDA_TRY(cudaGetDevice(&dev));
+    if (dev < 0 || dev >= 64) return QNN_FAIL(QNN_ERR_CUDA);
+    if (!allowed[dev].load(std::memory_order_acquire)) {
+        QNN_CUDA_TRY(cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kMost));
+        allowed[dev].store(true, std::memory_order_release);
+    }
     const int64_t mblocks = (a.M + P::kRows - 1) / P::kRows;
     if (mblocks > 65535) return QNN_FAIL(QNN_ERR_INVALID_ARG);
-    kern<<<dim3((unsigned)std::min<int64_t>(a.items, sm_count()), (unsigned)mblocks), kMmThreads, bytes, st>>>(a);
-    QNN_CUDA_TRY(cudaGetLastError());
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3((unsigned)(std::min<int64_t>(a.items, std::max(1, a.blocks > 1 ? sms * 7 / 8 / a.blocks : sms)) * a.blocks), (unsigned)mblocks);
+    cfg.blockDim = dim3(kMmThreads);
+    cfg.dynamicSmemBytes = bytes;
+    cfg.stream = st;
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeClusterDimension;
+    attr[0].val.clusterDim.x = (unsigned)a.blocks;
+    attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = a.blocks > 1 ? 1 : 0;
+    QNN_CUDA_TRY(cudaLaunchKernelEx(&cfg, kern, a));
     return QNN_OK;
 }
 
