@@ -392,10 +392,15 @@ qnn_status launch_mm4(Mm4Args a, cudaStream_t st) {
     const int rows = (int)std::min<int64_t>(P::kRows, a.M), sms = sm_count();
     const size_t sums = (size_t)P::kGroups * P::kRows * 4;  // a column tile's group sums
     const int fit = (int)((kMost - kFixed - (size_t)rows * 64) / ((size_t)rows * 2 * kTileCols + sums));
-    // Blocks that share a row tile's columns: as many as hold all of A between them, and, where row tiles are few, as many as
-    // give half of the SMs one (a column tile each at least). (16 x 8192 x 8192: A twice through one block 18.9 us, two blocks MM4A.)
+    // Blocks that share a row tile's columns: as many as hold all of A between them and convert at most kMostCells cells of it
+    // each (a row's column tile), and, where row tiles are few, as many as give half of the SMs one (a column tile each at
+    // least). (16 x 8192 x 8192: A in two parts through one block 18.9 us, two blocks 15.8, four 15.3; 8 x 8192 x 8192 one 14.4, two
+    // 13.8, 16 x 2048 x 8192 one 7.8, two 8.6.)
+    constexpr int kMostCells = 256;
     a.blocks = 1;
-    while (a.blocks < kMostBlocks && (a.blocks * fit < a.ktiles || (2 * ntiles * a.blocks <= sms && 2 * a.blocks <= a.ktiles))) a.blocks *= 2;
+    while (a.blocks < kMostBlocks && (a.blocks * fit < a.ktiles || rows * a.ktiles > kMostCells * a.blocks ||
+                                      (2 * ntiles * a.blocks <= sms && 2 * a.blocks <= a.ktiles)))
+        a.blocks *= 2;
     a.span = (a.ktiles + a.blocks - 1) / a.blocks;
     // as many warps on a row tile as leave every SM a block, and as have a column tile each
     a.seg_shift = 4;
