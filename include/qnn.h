@@ -292,8 +292,10 @@ qnn_status qnn_quantize_matrix_static(const float *x, int64_t rows, int64_t cols
  * layer whose state update is element-wise:
  *   qnn_rmsnorm_quantize -> qnn_qmatmul4 (or qnn_qmatmul) -> qnn_causal_conv -> qnn_ssm_scan -> qnn_quantize -> a product.
  * For these calls device pointers have to belong to the current device (or be managed memory), and an output may not
- * overlap an input unless a call allows it; QNN_ERR_INVALID_ARG otherwise, before anything runs. They allocate nothing and
- * may be captured into a graph.
+ * overlap an input unless a call allows it; QNN_ERR_INVALID_ARG otherwise, before anything runs. Overlap is judged by the
+ * range from an argument's first byte to its last. Rows (sequences, frames) times their stride may not pass 2^48 elements.
+ * The calls take no scratch, so any number may run at once, and may be captured into a graph after a first call on the device
+ * (which allocates the device status word).
  * ------------------------------------------------------------------------------------------- */
 
 /* Types of the values that pass between layers. All arithmetic is fp32 or wider, each output rounded once. */
@@ -341,7 +343,7 @@ qnn_status qnn_quantize4(const float *w, int64_t N, int64_t K, int64_t ldw, int3
 /*
  * qnn_qmatmul4 — the recovered product of Fig. 1 with 4-bit weights of qnn_quantize4, for few rows (each 32 of them read
  * the weights once).
- *   A, lda, pa, ga  [M x K] uint8 activation codes and their units, as for qnn_qmatmul.
+ *   A, lda, pa, ga  [M x K] uint8 activation codes and their units, as for qnn_qmatmul; M <= 524280.
  *   codes, units, group, row_sums  of a matrix [N x K].
  *   bias [N] fp32, nullable; Y [M x N] fp32 out (ldy >= N):
  *     Y[m,n] = (1 / Qa) sum_groups scale sum_{k in group} (A[m,k] + za)(code[n,k] + offset) + bias[n].
@@ -401,7 +403,8 @@ typedef struct {
  *   y[t][d] = (sum_n Cm[t][g][n] h[n] + skip[d] u[t][d]) * z / (1 + exp(-z)),  z = z[t][d],
  * with the last factor only where z is given and g = d / (D / groups). States and sums are fp32. lengths, frames behind a
  * sequence's end and T = 0 as for qnn_causal_conv; state_out is the state after each sequence's last frame, and
- * the states of a sequence do not depend on the others. One frame of many sequences is the serving form. Non-finite
+ * the states of a sequence do not depend on the others. Long sequences are taken in parts whose states are put together by
+ * their factors over a part (where states grow, A s > 0, that factor may overflow before a state does). One frame of many sequences is the serving form. Non-finite
  * inputs give non-finite outputs by the formulas, in their own channel and sequence (group, for Bm and Cm).
  */
 qnn_status qnn_ssm_scan(const qnn_ssm_args *args, void *stream);

@@ -428,7 +428,6 @@ qnn_status launch_mm4(Mm4Args a, cudaStream_t st) {
         allowed[dev].store(true, std::memory_order_release);
     }
     const int64_t mblocks = (a.M + P::kRows - 1) / P::kRows;
-    if (mblocks > 65535) return QNN_FAIL(QNN_ERR_INVALID_ARG);
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3((unsigned)(std::min<int64_t>(a.items, std::max(1, a.blocks > 1 ? sms * 7 / 8 / a.blocks : sms)) * a.blocks), (unsigned)mblocks);
     cfg.blockDim = dim3(kMmThreads);
@@ -455,7 +454,7 @@ bool aligned16(const void *p) { return (reinterpret_cast<uintptr_t>(p) & 15) == 
 bool aligned4(const void *p) { return (reinterpret_cast<uintptr_t>(p) & 3) == 0; }
 bool group_ok(int g) { return g == 32 || g == 64 || g == 128; }
 
-constexpr int64_t kMostN = INT32_MAX / 2, kMostLd = (int64_t)1 << 40;
+constexpr int64_t kMostN = INT32_MAX / 2, kMostM = 65535 * 8;  // (grid rows of 8 rows at least)
 int64_t tiles_of(int64_t N, int64_t K) { return (N + kTileRows - 1) / kTileRows * ((K + kTileCols - 1) / kTileCols); }
 
 }  // namespace
@@ -465,7 +464,7 @@ using namespace qnn;
 
 extern "C" qnn_status qnn_quantize4(const float *w, int64_t N, int64_t K, int64_t ldw, int32_t group, uint8_t *codes,
                                     uint32_t *units, float *row_sums, void *stream) {
-    if (N < 1 || N > kMostN || K < 1 || ldw < K || ldw > kMostLd || !group_ok(group)) return QNN_ERR_INVALID_ARG;
+    if (N < 1 || N > kMostN || K < 1 || ldw < K || !reach_ok(N, ldw) || !group_ok(group)) return QNN_ERR_INVALID_ARG;
     if (K > QNN_K_MAX) return QNN_ERR_K_TOO_LARGE;
     if (!is_local_ptr(w) || !is_local_ptr(codes) || !is_local_ptr(units) || !is_local_ptr(row_sums) || !aligned4(w) ||
         !aligned16(codes) || !aligned16(units) || !aligned16(row_sums))
@@ -493,7 +492,7 @@ extern "C" qnn_status qnn_quantize4(const float *w, int64_t N, int64_t K, int64_
 extern "C" qnn_status qnn_qmatmul4(const uint8_t *A, int64_t lda, const qnn_qparams *pa, int ga, int64_t M, int64_t K,
                                    const uint8_t *codes, const uint32_t *units, int32_t group, const float *row_sums,
                                    int64_t N, const float *bias, float *Y, int64_t ldy, void *stream) {
-    if (M < 0 || M > INT32_MAX || N < 1 || N > kMostN || K < 1 || lda < K || lda > kMostLd || ldy < N || ldy > kMostLd ||
+    if (M < 0 || M > kMostM || N < 1 || N > kMostN || K < 1 || lda < K || !reach_ok(M, lda) || ldy < N || !reach_ok(M, ldy) ||
         !group_ok(group) || (ga != QNN_PER_MATRIX && ga != QNN_PER_ROW))
         return QNN_ERR_INVALID_ARG;
     if (K > QNN_K_MAX) return QNN_ERR_K_TOO_LARGE;

@@ -53,6 +53,11 @@ struct Span {
     bool meets(const Span &o) const { return lo < o.hi && o.lo < hi; }
 };
 
+// count strides of `stride` elements stay within 2^48, so that byte offsets cannot overflow.
+inline bool reach_ok(int64_t count, int64_t stride) {
+    return stride >= 0 && (count <= 1 || stride <= ((int64_t)1 << 48) / count) && stride <= (int64_t)1 << 48;
+}
+
 inline int dtype_size(int dtype) { return dtype == QNN_F32 ? 4 : 2; }
 inline bool dtype_ok(int dtype) { return dtype == QNN_F32 || dtype == QNN_BF16 || dtype == QNN_F16; }
 

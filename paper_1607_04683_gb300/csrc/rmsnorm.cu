@@ -347,10 +347,10 @@ extern "C" qnn_status qnn_rmsnorm_quantize(const void *x, int64_t ldx, const voi
                                            const float *weight, double eps, int64_t rows, int64_t cols, void *residual_out,
                                            int64_t ldh, uint8_t *codes, int64_t ldc, qnn_qparams *params,
                                            int32_t *code_sums, float *values, int64_t ldv, void *stream) {
-    constexpr int64_t kMostCols = 1 << 24, kMostRows = INT32_MAX, kMostLd = (int64_t)1 << 40;
+    constexpr int64_t kMostCols = 1 << 24, kMostRows = INT32_MAX;
+    auto bad = [&](int64_t ld) { return ld < cols || !reach_ok(rows, ld); };
     if (!dtype_ok(dtype) || rows < 0 || rows > kMostRows || cols < 1 || cols > kMostCols || !(eps >= 1e-20 && eps <= 1e20) ||
-        ldx < cols || ldx > kMostLd || ldc < cols || ldc > kMostLd || (residual && (ldr < cols || ldr > kMostLd)) ||
-        (residual_out && (ldh < cols || ldh > kMostLd)) || (values && (ldv < cols || ldv > kMostLd)))
+        bad(ldx) || bad(ldc) || (residual && bad(ldr)) || (residual_out && bad(ldh)) || (values && bad(ldv)))
         return QNN_ERR_INVALID_ARG;
     if (rows == 0) return QNN_OK;
     if (!is_local_ptr(x) || !is_local_ptr(weight) || !is_local_ptr(codes) || !is_local_ptr(params) ||

@@ -805,11 +805,11 @@ qnn_status launch_conv(ConvArgs a, cudaStream_t st) {
     return QNN_OK;
 }
 
-constexpr int64_t kMostStride = (int64_t)1 << 40, kMostCount = (int64_t)1 << 40;
+constexpr int64_t kMostCount = (int64_t)1 << 40;
 
 // A [B][T][width] array: its strides are in range, its first element aligned to its type.
-bool frames_ok(const void *p, int64_t seq, int64_t frame, int e) {
-    return seq >= 0 && frame >= 0 && seq <= kMostStride && frame <= kMostStride && (reinterpret_cast<uintptr_t>(p) & (e - 1)) == 0;
+bool frames_ok(const void *p, int64_t B, int64_t T, int64_t seq, int64_t frame, int e) {
+    return reach_ok(B, seq) && reach_ok(T, frame) && (reinterpret_cast<uintptr_t>(p) & (e - 1)) == 0;
 }
 // No frame of an output overlaps another: sequences apart and frames apart within one, or the other way round.
 bool apart(int64_t B, int64_t T, int64_t width, int64_t seq, int64_t frame) {
@@ -820,7 +820,7 @@ Span frames_span(const void *p, int64_t B, int64_t T, int64_t width, int64_t seq
     return T > 0 ? Span(p, ((B - 1) * seq + (T - 1) * frame + width) * e) : Span();
 }
 bool sizes_ok(int64_t B, int64_t T, int64_t D) {
-    return B >= 0 && T >= 0 && D >= 1 && T <= INT32_MAX && D <= INT32_MAX && B <= INT32_MAX && B * D <= kMostCount;
+    return B >= 0 && T >= 0 && D >= 1 && T <= INT32_MAX && D <= INT32_MAX && B <= INT32_MAX && B * D <= kMostCount && reach_ok(T, B * D);
 }
 bool aligned4(const void *p) { return (reinterpret_cast<uintptr_t>(p) & 3) == 0; }
 bool local_or_null(const void *p) { return !p || is_local_ptr(p); }
@@ -836,8 +836,8 @@ extern "C" qnn_status qnn_causal_conv(const void *x, int64_t x_seq, int64_t x_fr
                                       void *stream) {
     if (!dtype_ok(dtype) || !sizes_ok(B, T, D) || W < 1 || W > kMostTaps) return QNN_ERR_INVALID_ARG;
     const int e = dtype_size(dtype);
-    if (!frames_ok(x, x_seq, x_frame, e) || !frames_ok(y, y_seq, y_frame, e) || !apart(B, T, D, y_seq, y_frame) ||
-        !frames_ok(state_in, 0, 0, e) || !frames_ok(state_out, 0, 0, e) || !aligned4(w) || !aligned4(bias) || !aligned4(lengths))
+    if (!frames_ok(x, B, T, x_seq, x_frame, e) || !frames_ok(y, B, T, y_seq, y_frame, e) || !apart(B, T, D, y_seq, y_frame) ||
+        !frames_ok(state_in, 0, 0, 0, 0, e) || !frames_ok(state_out, 0, 0, 0, 0, e) || !aligned4(w) || !aligned4(bias) || !aligned4(lengths))
         return QNN_ERR_INVALID_ARG;
     if (B == 0 || (T == 0 && !state_out)) return QNN_OK;
     if ((T > 0 && (!is_local_ptr(x) || !is_local_ptr(y))) || !is_local_ptr(w) || !local_or_null(bias) || !local_or_null(state_in) ||
@@ -869,9 +869,9 @@ extern "C" qnn_status qnn_ssm_scan(const qnn_ssm_args *args, void *stream) {
         return QNN_ERR_INVALID_ARG;
     const int e = dtype_size(a.dtype);
     const int64_t gn = (int64_t)a.groups * a.N;
-    if (!frames_ok(a.u, a.u_seq, a.u_frame, e) || !frames_ok(a.dt, a.dt_seq, a.dt_frame, e) ||
-        !frames_ok(a.Bm, a.Bm_seq, a.Bm_frame, e) || !frames_ok(a.Cm, a.Cm_seq, a.Cm_frame, e) ||
-        (a.z && !frames_ok(a.z, a.z_seq, a.z_frame, e)) || !frames_ok(a.y, a.y_seq, a.y_frame, e) ||
+    if (!frames_ok(a.u, a.B, a.T, a.u_seq, a.u_frame, e) || !frames_ok(a.dt, a.B, a.T, a.dt_seq, a.dt_frame, e) ||
+        !frames_ok(a.Bm, a.B, a.T, a.Bm_seq, a.Bm_frame, e) || !frames_ok(a.Cm, a.B, a.T, a.Cm_seq, a.Cm_frame, e) ||
+        (a.z && !frames_ok(a.z, a.B, a.T, a.z_seq, a.z_frame, e)) || !frames_ok(a.y, a.B, a.T, a.y_seq, a.y_frame, e) ||
         !apart(a.B, a.T, a.D, a.y_seq, a.y_frame) || !aligned4(a.A) || !aligned4(a.skip) || !aligned4(a.dt_bias) ||
         !aligned4(a.state_in) || !aligned4(a.state_out) || !aligned4(a.lengths))
         return QNN_ERR_INVALID_ARG;

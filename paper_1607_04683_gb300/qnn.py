@@ -326,12 +326,19 @@ def _frames(t, what: str, dtype, shape):
 
 
 def _result(torch, shape, dtype, like, stream):
-    """A new tensor for a call on stream: where that is not the current one, its memory is not given to others before
-    what the call queued there is done."""
-    t = torch.empty(shape, dtype=dtype, device=like.device)
-    if stream is not None:
-        t.record_stream(stream)
-    return t
+    """A new tensor for a call on stream, in memory of that stream: what the current one may still do with memory that was
+    given back to it is not waited for there."""
+    if stream is None:
+        return torch.empty(shape, dtype=dtype, device=like.device)
+    with torch.cuda.stream(stream):
+        return torch.empty(shape, dtype=dtype, device=like.device)
+
+
+def _used(stream, *tensors):
+    """Keeps the memory of a call's inputs from being given to others before what the call queued on stream is done."""
+    for t in tensors:
+        if t is not None:
+            t.record_stream(stream)
 
 
 def qnn_rmsnorm_quantize(x, weight, residual=None, eps=1e-5, residual_out=None, want_values=False, stream=None):
@@ -342,6 +349,10 @@ def qnn_rmsnorm_quantize(x, weight, residual=None, eps=1e-5, residual_out=None, 
     torch, L = _libs()
     if x.dim() != 2 or not x.is_cuda:
         _bad("x: a CUDA matrix")
+    if stream is not None:
+        _used(stream, x, weight, residual, residual_out)
+        with torch.cuda.stream(stream):  # (the results are memory of the call's stream)
+            return qnn_rmsnorm_quantize(x, weight, residual, eps, residual_out, want_values)
     shape, ty, dev, empty = x.shape, x.dtype, x.device, torch.empty
     dt = _dtype(x, "x")
     rows, cols = shape
@@ -365,13 +376,8 @@ def qnn_rmsnorm_quantize(x, weight, residual=None, eps=1e-5, residual_out=None, 
     if want_values:
         values = empty(shape, dtype=torch.float32, device=dev)
         pv = values.data_ptr()
-    if stream is not None:
-        for t in (h, codes, params, sums, values):
-            if t is not None:
-                t.record_stream(stream)
     st = L.qnn_rmsnorm_quantize(x.data_ptr(), ldx, pr, ldr, dt, w, eps, rows, cols, ph, ldh, codes.data_ptr(), cols,
-                                params.data_ptr(), sums.data_ptr(), pv, cols,
-                                _here(torch) if stream is None else stream.cuda_stream)
+                                params.data_ptr(), sums.data_ptr(), pv, cols, _here(torch))
     if st:
         _check(st, "qnn_rmsnorm_quantize")
     return codes, params, sums, h, values
@@ -407,6 +413,8 @@ def qnn_quantize4(w, group: int = 64, stream=None) -> Weights4:
     codes = _result(torch, (*tiles, 1024), torch.uint8, w, stream)
     units = _result(torch, (*tiles, 16, 128 // group, 2), torch.bfloat16, w, stream)
     sums = _result(torch, (N,), torch.float32, w, stream)
+    if stream is not None:
+        _used(stream, w)
     _check(L.qnn_quantize4(w.data_ptr(), N, K, ldw, group, codes.data_ptr(), units.data_ptr(), sums.data_ptr(),
                            _stream(stream)), "qnn_quantize4")
     return Weights4(codes, units, sums, N, K, group)
@@ -427,6 +435,8 @@ def qnn_qmatmul4(A, pa, weights: Weights4, ga=PER_ROW, bias=None, out=None, stre
         Y, ldy = _result(torch, (M, N), torch.float32, A, stream), N
     else:
         Y, ldy = out, _rows(out, "out", torch.float32, (M, N))
+    if stream is not None:
+        _used(stream, A, pa, weights.codes, weights.units, weights.row_sums, bias, out)
     st = L.qnn_qmatmul4(A.data_ptr(), lda, p, ga, M, K, weights.codes.data_ptr(), weights.units.data_ptr(), weights.group,
                         weights.row_sums.data_ptr(), N, b, Y.data_ptr(), ldy,
                         _here(torch) if stream is None else stream.cuda_stream)
@@ -452,6 +462,8 @@ def qnn_causal_conv(x, weight, bias=None, silu=True, state_in=None, state_out=No
     px, xs, xf = _frames(x, "x", ty, shape)
     py, ys, yf = _frames(y, "out", ty, shape)
     state = (B, W - 1, D)
+    if stream is not None:
+        _used(stream, x, weight, bias, state_in, state_out, lengths, out)
     st = L.qnn_causal_conv(px, xs, xf, dt, B, T, D, _flat(weight, "weight", torch.float32, (D, W)), W,
                            _flat(bias, "bias", torch.float32, (D,)), 1 if silu else 0, _flat(state_in, "state_in", ty, state),
                            _flat(state_out, "state_out", ty, state), _flat(lengths, "lengths", torch.int32, (B,)), py, ys, yf,
@@ -487,6 +499,8 @@ def qnn_ssm_scan(u, dt, A, B, C, D=None, z=None, dt_bias=None, softplus=True, st
                           *_frames(y, "out", ty, shape), _flat(A, "A", f32, (nd, ns)), _flat(D, "D", f32, (nd,)),
                           _flat(dt_bias, "dt_bias", f32, (nd,)), _flat(state_in, "state_in", f32, state),
                           _flat(state_out, "state_out", f32, state), _flat(lengths, "lengths", torch.int32, (nb,)))
+    if stream is not None:
+        _used(stream, u, dt, A, B, C, D, z, dt_bias, state_in, state_out, lengths, out)
     st = L.qnn_ssm_scan(args, _here(torch) if stream is None else stream.cuda_stream)
     if st:
         _check(st, "qnn_ssm_scan")

@@ -232,7 +232,8 @@ def activations(seed, M, K, spread=1.0, shift=0.0):
 @pytest.mark.parametrize("M,K,N", [(1, 1, 1), (1, 32, 16), (2, 31, 5), (3, 64, 17), (1, 128, 128), (4, 129, 33), (5, 100, 40),
                                    (8, 500, 500), (9, 1000, 70), (1, 2048, 130), (7, 2049, 31), (16, 512, 64), (17, 300, 129),
                                    (31, 640, 20), (32, 256, 48), (33, 127, 16), (64, 384, 33), (100, 96, 24), (1, 8192, 48),
-                                   (12, 8191, 17), (2, 33025, 18), (33, 4500, 20)])
+                                   (12, 8191, 17), (2, 33025, 18), (33, 4500, 20),
+                                   (32, 33025, 20), (16, 20000, 33), (9, 5000, 300), (1, 256, 40000), (3, 640, 41000)])
 def test_qmatmul4(qnn, M, K, N, group):
     A, params, _ = activations(M * 7 + K, M, K)
     bias = rng(K).normal(0, 1, N).astype(np.float32)
@@ -265,6 +266,27 @@ def test_qmatmul4_all_extreme_codes(qnn):
         w[:, 1::32] = 15.0
         for group in (32, 64, 128):
             check_product(qnn, A, params, w, group)
+
+
+def test_qmatmul4_more_row_tiles_than_blocks_and_rows_in_parts(qnn):
+    """Many row tiles on rows that shared memory holds in parts, against 64-bit products of the values on the GPU."""
+    M, N, K, G = 32, 8480, 8960, 64
+    A, params, _ = activations(7, M, K)
+    g = torch.Generator(device="cuda")
+    g.manual_seed(3)
+    w = qnn.qnn_quantize4(torch.randn((N, K), generator=g, device="cuda") * 0.05, G)
+    nt, kt = w.codes.shape[:2]
+    p = w.codes.view(nt, kt, 2, 8, 4, 4, 4)  # halves of rows, rows, eighths of 32 columns, parts of 32, bytes
+    half = torch.stack([p & 15, p >> 4], -1).view(nt, kt, 2, 8, 4, 4, 8)[..., [0, 4, 1, 5, 2, 6, 3, 7]]
+    codes = half.permute(0, 2, 3, 1, 5, 4, 6).reshape(nt * 16, kt * 128 // G, G).double()
+    u = w.units.permute(0, 2, 1, 3, 4).reshape(nt * 16, kt * 128 // G, 2).double()
+    W = ((codes + u[..., :1]) * u[..., 1:]).view(nt * 16, kt * 128)[:N, :K]
+    a = gpu(A).double()
+    z, Q = (torch.from_numpy(params[k].astype(np.float64)).cuda()[:, None] for k in ("z", "Q"))
+    want = (a + z) @ W.t() / Q
+    mass = ((a - 128).abs() @ W.abs().t() + (z + 128).abs() * W.abs().sum(1)) / Q
+    got = qnn.qnn_qmatmul4(gpu(A), qnn.params_tensor(params), w)
+    assert ((got.double() - want).abs() <= (K / 32 + 16) * ref.U * mass + 2 * ref.U * want.abs()).all()
 
 
 def test_qmatmul4_one_unit_for_the_matrix(qnn):
@@ -710,6 +732,25 @@ def test_captured_calls_replay(qnn):
 
 def some_calls_captured(calls):
     return calls[:4]
+
+
+def test_results_of_a_side_stream_are_not_memory_of_the_current_one(qnn):
+    """A call on a side stream while the current stream still writes to memory that was given back to it."""
+    calls = some_calls(qnn)
+    want = [[t.clone() for t in c()] for c in calls[:4]]
+    side = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    for _ in range(5):
+        for c, w in zip(calls[:4], want):
+            for t in w:  # long fills of blocks that the next allocations of their sizes would take
+                junk = torch.empty_like(t)
+                for _ in range(20):
+                    junk.fill_(1)
+                del junk
+            got = c(side)
+            side.synchronize()
+            torch.cuda.synchronize()
+            assert all(torch.equal(p, q) for p, q in zip(got, w))
 
 
 def test_same_inputs_same_bits(qnn):

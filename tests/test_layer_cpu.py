@@ -26,7 +26,8 @@ def _norm(qlib, rows=4, cols=8, ldx=8, ldr=8, dtype=0, eps=1e-5, ldh=8, ldc=8, l
 @pytest.mark.parametrize("kw", [dict(rows=-1), dict(cols=0), dict(cols=(1 << 24) + 1, ldx=1 << 25, ldr=1 << 25, ldh=1 << 25,
                                                                    ldc=1 << 25, ldv=1 << 25),
                                 dict(ldx=7), dict(ldr=7), dict(ldh=7), dict(ldc=7), dict(ldv=7), dict(dtype=3), dict(dtype=-1),
-                                dict(eps=0.0), dict(eps=1e-21), dict(eps=1e21), dict(eps=float("nan")), dict(ldx=1 << 41)])
+                                dict(eps=0.0), dict(eps=1e-21), dict(eps=1e21), dict(eps=float("nan")), dict(ldx=1 << 49),
+                                dict(rows=1 << 30, ldx=1 << 20), dict(rows=1 << 31)])
 def test_norm_refuses(qlib, kw):
     assert _norm(qlib, **kw) == BAD
 
@@ -41,7 +42,8 @@ def test_quantize4_refuses(qlib, kw):
     assert qlib.qnn_quantize4(None, a["N"], a["K"], a["ldw"], a["group"], None, None, None, None) == BAD
 
 
-@pytest.mark.parametrize("kw", [dict(M=-1), dict(N=0), dict(K=0), dict(lda=7), dict(ldy=3), dict(group=48), dict(ga=2)])
+@pytest.mark.parametrize("kw", [dict(M=-1), dict(N=0), dict(K=0), dict(lda=7), dict(ldy=3), dict(group=48), dict(ga=2),
+                                dict(M=524281), dict(M=500000, lda=1 << 40)])
 def test_qmatmul4_refuses(qlib, kw):
     a = dict(M=2, K=8, N=4, lda=8, ldy=4, group=32, ga=1) | kw
     assert qlib.qnn_qmatmul4(None, a["lda"], None, a["ga"], a["M"], a["K"], None, None, a["group"], None, a["N"], None, None,
@@ -54,7 +56,8 @@ def test_products_longer_than_the_codes_allow(qlib):
 
 
 @pytest.mark.parametrize("kw", [dict(dtype=3), dict(B=-1), dict(T=-1), dict(D=0), dict(W=0), dict(W=9), dict(x_seq=-1),
-                                dict(y_frame=-8), dict(y_frame=7), dict(y_seq=8), dict(y_seq=0), dict(T=1 << 31)])
+                                dict(y_frame=-8), dict(y_frame=7), dict(y_seq=8), dict(y_seq=0), dict(T=1 << 31), dict(x_seq=1 << 48),
+                                dict(B=1 << 21, T=1 << 20, D=1 << 19, y_frame=1 << 19, y_seq=1 << 39)])
 def test_conv_refuses(qlib, kw):
     a = dict(x_seq=40, x_frame=8, dtype=0, B=2, T=5, D=8, W=4, y_seq=40, y_frame=8) | kw
     assert qlib.qnn_causal_conv(None, a["x_seq"], a["x_frame"], a["dtype"], a["B"], a["T"], a["D"], None, a["W"], None, 1, None,
@@ -74,7 +77,7 @@ def _scan_args(qnn, **kw):
 
 @pytest.mark.parametrize("kw", [dict(dtype=7), dict(B=-1), dict(T=-1), dict(D=0), dict(N=0), dict(N=129), dict(groups=0),
                                 dict(groups=3), dict(u_seq=-1), dict(y_frame=7), dict(y_seq=39), dict(y_seq=0), dict(u=2),
-                                dict(A=3)])
+                                dict(A=3), dict(z=1), dict(Bm_seq=1 << 48)])
 def test_scan_refuses(qlib, kw):
     from paper_1607_04683_gb300 import qnn
     assert qlib.qnn_ssm_scan(C.byref(_scan_args(qnn, **kw)), None) == BAD
