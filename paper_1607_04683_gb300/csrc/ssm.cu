@@ -341,8 +341,8 @@ __device__ __forceinline__ float peer_load(uint32_t at) {
 
 // Whole sequences, a warp by itself: 32 / L channels of one group over a part of a sequence's frames, tile by tile of kTile
 // frames. Its lanes load u, dt (and z) in runs of channels, form s = softplus(dt) and s u, and leave them in shared memory
-// beside the tile's Bm and Cm; then L lanes a channel, NS states each, carry the states over the tile's frames; then the
-// lanes that loaded u and z finish the outputs. The next tile's loads are in flight meanwhile. No block-wide barriers: the
+// beside the tile's Bm and Cm; then L lanes a channel, NS states each (or 2 L lanes two channels, half as many), carry the
+// states over the tile's frames; then the lanes that loaded u and z finish the outputs. The next tile's loads are in flight meanwhile. No block-wide barriers: the
 // phases of a block's warps overlap.
 //
 // Where sequences are few, `parts` warps (of a block, or of a cluster of blocks) share each one's frames. The recurrence is
@@ -354,6 +354,8 @@ template <int NS, int L>
 struct ScanWarp {
     static constexpr int kChans = 32 / L;                // of a warp
     static constexpr int kStates = NS * L;               // of a channel, padded
+    static constexpr int kSide = L < 4 ? 1 : 2;          // channels side by side in a lane
+    static constexpr int kMine = NS / kSide, kLanes = kSide * L;  // states a lane holds of each, lanes of such a set
     static constexpr int kEach = kTile / L;              // values a lane loads of each array
     static constexpr int V = kEach < 4 ? kEach : 4, kRuns = kEach / V;
     static constexpr int kRowLanes = kChans / V, kRows = 32 / kRowLanes;  // lanes a frame, frames a load
@@ -364,54 +366,60 @@ struct ScanWarp {
     alignas(16) float2 s[kTile][kChans];  // steps s and s u
     alignas(16) float B[kTile][kStates], C[kTile][kStates];
     struct Part {
-        float part[NS][32], sum[32];      // r and S
-    };
-    float part[NS][32], sum[32];          // of this warp's part
-    float2 start[NS / 2][32];             // the states that a part starts from, where it is the first
+        float part[NS][32], sum[kSide][32];   // r and S
+    } own;                                // of this warp's part
+    float start[NS][32];                  // the states that a part starts from, where it is the first
 };
 
-// A frame's factors exp2(s A), its inputs su B and the sum of C h, for NS states in pairs: one instruction for two results.
+// A frame's factors exp2(s A), its step h <- f h + su B and the sum of C h, for M states in pairs: one instruction for two
+// results.
 //
 // The hardware's exponential lies low: by 0.5 to 0.8e-8 on average for arguments of -2^-14 .. -2^-8, 1.6 to 2.7e-8 for -2^-8 .. -2^-2
 // (relative; its rounding noise is 3e-8). Over a state's memory of 1/(s A) frames noise grows as the root and bias as itself, so
 // arguments are taken kBias higher, by the multiply-add that forms them: -1.3 to 0.8e-8 are left (a state after 100 frames
 // 2.0e-6 off without, 0.9e-6 with). A step of 0 still has a factor of 1, as exp2(kBias) rounds to it.
 constexpr float kBias = 2e-8f;
-template <int NS>
-__device__ __forceinline__ void factors(float2 (&f)[NS / 2], const float2 (&A)[NS / 2], float s) {
+template <int M>
+__device__ __forceinline__ void factors(float2 (&f)[M / 2], const float2 (&A)[M / 2], float s) {
     const float2 s2 = make_float2(s, s);
 #pragma unroll
-    for (int i = 0; i < NS / 2; ++i) {
+    for (int i = 0; i < M / 2; ++i) {
         const float2 x = ffma2_rn(s2, A[i], f2(kBias));
         f[i] = make_float2(exp2_hw(x.x), exp2_hw(x.y));
     }
 }
-template <int NS>
-__device__ __forceinline__ void inputs(float2 (&bu)[NS / 2], float su, const float *B) {
-    const float2 su2 = make_float2(su, su);
+template <int M>
+__device__ __forceinline__ void load_pairs(float2 (&to)[M / 2], const float *from) {
 #pragma unroll
-    for (int i = 0; i < NS / 2; i += 2) {
-        const float4 b = *reinterpret_cast<const float4 *>(B + 2 * i);
-        bu[i] = fmul2_rn(su2, make_float2(b.x, b.y));
-        bu[i + 1] = fmul2_rn(su2, make_float2(b.z, b.w));
+    for (int i = 0; i < M / 2; i += 2) {
+        const float4 v = *reinterpret_cast<const float4 *>(from + 2 * i);
+        to[i] = make_float2(v.x, v.y), to[i + 1] = make_float2(v.z, v.w);
     }
 }
-template <int NS>
-__device__ __forceinline__ float dot(const float2 (&h)[NS / 2], const float *C) {
-    float2 y = make_float2(0.0f, 0.0f);
+// The steps s and s u of channels side by side.
+__device__ __forceinline__ void load_steps(float2 (&to)[1], const float2 *from) { to[0] = *from; }
+__device__ __forceinline__ void load_steps(float2 (&to)[2], const float2 *from) {
+    const float4 v = *reinterpret_cast<const float4 *>(from);
+    to[0] = make_float2(v.x, v.y), to[1] = make_float2(v.z, v.w);
+}
+template <int M>
+__device__ __forceinline__ void advance(float2 (&h)[M / 2], const float2 (&f)[M / 2], float su, const float2 (&B)[M / 2]) {
+    const float2 su2 = make_float2(su, su);
 #pragma unroll
-    for (int i = 0; i < NS / 2; i += 2) {
-        const float4 c = *reinterpret_cast<const float4 *>(C + 2 * i);
-        y = ffma2_rn(h[i], make_float2(c.x, c.y), y);
-        y = ffma2_rn(h[i + 1], make_float2(c.z, c.w), y);
-    }
+    for (int i = 0; i < M / 2; ++i) h[i] = ffma2_rn(f[i], h[i], fmul2_rn(su2, B[i]));
+}
+template <int M>
+__device__ __forceinline__ float dot(const float2 (&h)[M / 2], const float2 (&C)[M / 2]) {
+    float2 y = fmul2_rn(h[0], C[0]);
+#pragma unroll
+    for (int i = 1; i < M / 2; ++i) y = ffma2_rn(h[i], C[i], y);
     return __fadd_rn(y.x, y.y);
 }
 
 template <typename T, int NS, int L, bool VEC>
 __global__ void __launch_bounds__(32 * ScanWarp<NS, L>::kBlockWarps, sizeof(T) == 4 ? 2 : 3) ssm_scan_kernel(const ScanArgs a) {
     using Sh = ScanWarp<NS, L>;
-    constexpr int V = Sh::V, R = Sh::kRuns, W = Sh::kBlockWarps, BC = Sh::kBCEach;
+    constexpr int V = Sh::V, R = Sh::kRuns, W = Sh::kBlockWarps, BC = Sh::kBCEach, X = Sh::kSide, M = Sh::kMine, Q = Sh::kLanes;
     __shared__ Sh all[W];
     __shared__ typename Sh::Part whole;  // of the block's parts together
     __shared__ __align__(16) float all_y[W][kTile][Sh::kChans];  // sums over the states (apart: nothing else may be waited for with them)
@@ -491,20 +499,33 @@ __global__ void __launch_bounds__(32 * ScanWarp<NS, L>::kBlockWarps, sizeof(T) =
     };
     seek(first);
     fetch(first, a.parts == 1);
-    // and in the recurrence: channel c, states n0 .. n0 + NS
-    const int c = lane / L, q = lane % L, n0 = q * NS;
-    float2 A[NS / 2], h[NS / 2];
+    // and in the recurrence: channels c .. c + X, states n0 .. n0 + M of each. (Two channels side by side share the reads of Bm
+    // and Cm, but have twice the sums to exchange: 16 x 500 x 2048 x 32 bf16 227 us by one, 177 by two; 16 x 1000 x 2048 x 16 198 and
+    // 207.)
+    const int c = lane / Q * X, q = lane % Q, n0 = q * M;
+    float2 A[X][M / 2], h[X][M / 2];
     const bool start = there && rank == 0 && a.state_in;
+    auto state_at = [&](int x, int i) { return (b * a.D + d0 + c + x) * a.N + n0 + i; };
 #pragma unroll
-    for (int i = 0; i < NS; ++i) {
-        const bool ok = c < chans && n0 + i < a.N;
-        const float v = ok ? __fmul_rn(__ldg(a.A + (d0 + c) * a.N + n0 + i), kLog2e) : 0.0f;
-        const float s = ok && start ? a.state_in[(b * a.D + d0 + c) * a.N + n0 + i] : 0.0f;
-        if (i & 1)
-            A[i / 2].y = v, h[i / 2].y = s;
-        else
-            A[i / 2].x = v, h[i / 2].x = s;
-    }
+    for (int x = 0; x < X; ++x)
+#pragma unroll
+        for (int i = 0; i < M; ++i) {
+            const bool ok = c + x < chans && n0 + i < a.N;
+            const float v = ok ? __fmul_rn(__ldg(a.A + (d0 + c + x) * a.N + n0 + i), kLog2e) : 0.0f;
+            const float s = ok && start ? a.state_in[state_at(x, i)] : 0.0f;
+            if (i & 1)
+                A[x][i / 2].y = v, h[x][i / 2].y = s;
+            else
+                A[x][i / 2].x = v, h[x][i / 2].x = s;
+        }
+    auto put = [&](float (&to)[NS][32]) {
+#pragma unroll
+        for (int i = 0; i < NS; ++i) to[i][lane] = i & 1 ? h[i / M][i % M / 2].y : h[i / M][i % M / 2].x;
+    };
+    auto take = [&](const float (&from)[NS][32]) {
+#pragma unroll
+        for (int i = 0; i < NS; i += 2) h[i / M][i % M / 2] = make_float2(from[i][lane], from[i + 1][lane]);
+    };
     auto stage = [&](int t0, bool final) {  // a frame that is not there has a step of 0, which leaves the states as they are
         if constexpr (!Sh::kBCAhead) {
             fetch_bc(t0, rB, pB, a.Bm_frame);
@@ -540,91 +561,99 @@ __global__ void __launch_bounds__(32 * ScanWarp<NS, L>::kBlockWarps, sizeof(T) =
     };
 
     if (a.parts > 1) {
-#pragma unroll
-        for (int i = 0; i < NS / 2; ++i) sh.start[i][lane] = h[i];
-        float sum = 0.0f;
+        put(sh.start);
+        float sum[X] = {};
         for (int t0 = first; t0 < last; t0 += kTile) {
             stage(t0, false);
             __syncwarp();
             fetch(t0 + kTile, false);
 #pragma unroll 4
             for (int t = 0; t < kTile; ++t) {
-                const float2 s = sh.s[t][c];
-                sum = __fadd_rn(sum, s.x);
-                float2 f[NS / 2], bu[NS / 2];
-                factors<NS>(f, A, s.x);
-                inputs<NS>(bu, s.y, &sh.B[t][n0]);
+                float2 s[X], Bt[M / 2];
+                load_steps(s, &sh.s[t][c]);
+                load_pairs<M>(Bt, &sh.B[t][n0]);
 #pragma unroll
-                for (int k = 0; k < NS / 2; ++k) h[k] = ffma2_rn(f[k], h[k], bu[k]);
+                for (int x = 0; x < X; ++x) {
+                    float2 f[M / 2];
+                    sum[x] = __fadd_rn(sum[x], s[x].x);
+                    factors<M>(f, A[x], s[x].x);
+                    advance<M>(h[x], f, s[x].y, Bt);
+                }
             }
             __syncwarp();
         }
+        put(sh.own.part);
 #pragma unroll
-        for (int i = 0; i < NS; ++i) sh.part[i][lane] = i & 1 ? h[i / 2].y : h[i / 2].x;
-        sh.sum[lane] = sum;
+        for (int x = 0; x < X; ++x) sh.own.sum[x][lane] = sum[x];
         seek(first);  // the second pass's first loads are in flight meanwhile
         fetch(first, true);
-        // the parts of a block, then those of the blocks before it, which the last warp of each has put together. `first_part`
-        // takes r as it is: nothing lies before it
+        // The parts of a block, then those of the blocks before it, which the last warp of each has put together. `first_part`
+        // takes r as it is: nothing lies before it.
         const bool cluster = a.parts > W;
         const int w0 = cluster ? 0 : warp - rank;  // the first part's warp in this block
-        auto compose = [&](float2 (&to)[NS / 2], float s, const float (&r)[NS], bool first_part) {
+        auto compose = [&](const float (&s)[X], const float (&r)[NS], bool first_part) {
 #pragma unroll
-            for (int k = 0; k < NS / 2; ++k) {
-                to[k].x = first_part ? r[2 * k] : __fmaf_rn(exp2_hw(__fmul_rn(s, A[k].x)), to[k].x, r[2 * k]);
-                to[k].y = first_part ? r[2 * k + 1] : __fmaf_rn(exp2_hw(__fmul_rn(s, A[k].y)), to[k].y, r[2 * k + 1]);
+            for (int i = 0; i < NS; ++i) {
+                float &to = i & 1 ? h[i / M][i % M / 2].y : h[i / M][i % M / 2].x;
+                const float Ai = i & 1 ? A[i / M][i % M / 2].y : A[i / M][i % M / 2].x;
+                to = first_part ? r[i] : __fmaf_rn(exp2_hw(__fmul_rn(s[i / M], Ai)), to, r[i]);
             }
         };
-        auto compose_warps = [&](float2 (&to)[NS / 2], int end, bool first_part) {  // and the sum of their steps
-            float total = 0.0f;
+        auto compose_warps = [&](float (&total)[X], int end, bool first_part) {  // and the sum of their steps
+#pragma unroll
+            for (int x = 0; x < X; ++x) total[x] = 0.0f;
             for (int w = w0; w < end; ++w) {
                 float r[NS];
 #pragma unroll
-                for (int k = 0; k < NS; ++k) r[k] = all[w].part[k][lane];
-                compose(to, all[w].sum[lane], r, first_part && w == w0);
-                total = __fadd_rn(total, all[w].sum[lane]);
+                for (int k = 0; k < NS; ++k) r[k] = all[w].own.part[k][lane];
+                float s[X];
+#pragma unroll
+                for (int x = 0; x < X; ++x) {
+                    s[x] = all[w].own.sum[x][lane];
+                    total[x] = __fadd_rn(total[x], s[x]);
+                }
+                compose(s, r, first_part && w == w0);
             }
-            return total;
         };
+        float total[X];
         __syncthreads();
         if (cluster) {
             const int block = rank / W;
             if (warp == W - 1) {
-                const float total = compose_warps(h, W, true);
+                compose_warps(total, W, true);
+                put(whole.part);
 #pragma unroll
-                for (int k = 0; k < NS; ++k) whole.part[k][lane] = k & 1 ? h[k / 2].y : h[k / 2].x;
-                whole.sum[lane] = total;
+                for (int x = 0; x < X; ++x) whole.sum[x][lane] = total[x];
             }
             cluster_arrive();
             cluster_wait();
-#pragma unroll
-            for (int i = 0; i < NS / 2; ++i) h[i] = sh.start[i][lane];
+            take(sh.start);
             constexpr int kAtOnce = 4;  // blocks whose values are loaded together
             for (int p0 = 0; p0 < block; p0 += kAtOnce) {
-                float s[kAtOnce], r[kAtOnce][NS];
+                float s[kAtOnce][X], r[kAtOnce][NS];
 #pragma unroll
                 for (int i = 0; i < kAtOnce; ++i) {
                     if (p0 + i >= block) break;
-                    s[i] = peer_load(peer_address(&whole.sum[lane], p0 + i));
+#pragma unroll
+                    for (int x = 0; x < X; ++x) s[i][x] = peer_load(peer_address(&whole.sum[x][lane], p0 + i));
 #pragma unroll
                     for (int k = 0; k < NS; ++k) r[i][k] = peer_load(peer_address(&whole.part[k][lane], p0 + i));
                 }
 #pragma unroll
                 for (int i = 0; i < kAtOnce; ++i) {
                     if (p0 + i >= block) break;
-                    compose(h, s[i], r[i], p0 + i == 0);
+                    compose(s[i], r[i], p0 + i == 0);
                 }
             }
             cluster_arrive();  // waited for at the end: the others may still read this block's
-            compose_warps(h, warp, block == 0);
+            compose_warps(total, warp, block == 0);
         } else {
-#pragma unroll
-            for (int i = 0; i < NS / 2; ++i) h[i] = sh.start[i][lane];
-            compose_warps(h, warp, true);
+            take(sh.start);
+            compose_warps(total, warp, true);
         }
     }
 
-    constexpr int kSteps = L > 8 ? L : 8;  // frames between stores: their loads and products overlap
+    constexpr int kSteps = 8;  // frames between stores: their loads and products overlap
     T *py = static_cast<T *>(a.y) + b * a.y_seq + (first + row) * a.y_frame + d0 + run;
     for (int t0 = first; t0 < last; t0 += kTile) {
         stage(t0, true);
@@ -635,38 +664,50 @@ __global__ void __launch_bounds__(32 * ScanWarp<NS, L>::kBlockWarps, sizeof(T) =
         fetch(t0 + kTile, true);
 #pragma unroll 1
         for (int tb = 0; tb < kTile; tb += kSteps) {
-            float y[kSteps];
-            float2 f[NS / 2];  // a frame's factors are formed beside the products of the one before
-            float su = sh.s[tb][c].y;
-            factors<NS>(f, A, sh.s[tb][c].x);
+            float y[X * kSteps];  // by frame and channel
+            float2 f[X][M / 2];   // a frame's factors are formed beside the products of the one before
+            float2 s[X];
+            load_steps(s, &sh.s[tb][c]);
+#pragma unroll
+            for (int x = 0; x < X; ++x) factors<M>(f[x], A[x], s[x].x);
 #pragma unroll
             for (int i = 0; i < kSteps; ++i) {
-                const int next = i + 1 < kSteps ? tb + i + 1 : tb;
-                float2 bu[NS / 2], f1[NS / 2];
-                inputs<NS>(bu, su, &sh.B[tb + i][n0]);
-                const float2 s = sh.s[next][c];
-                if (i + 1 < kSteps) factors<NS>(f1, A, s.x);
+                float2 f1[X][M / 2], Bt[M / 2], Ct[M / 2], s1[X];
+                load_pairs<M>(Bt, &sh.B[tb + i][n0]);
+                load_steps(s1, &sh.s[i + 1 < kSteps ? tb + i + 1 : tb][c]);
+                if (i + 1 < kSteps)
 #pragma unroll
-                for (int k = 0; k < NS / 2; ++k) h[k] = ffma2_rn(f[k], h[k], bu[k]);
-                y[i] = dot<NS>(h, &sh.C[tb + i][n0]);
-                if (i + 1 < kSteps) {
-                    su = s.y;
+                    for (int x = 0; x < X; ++x) factors<M>(f1[x], A[x], s1[x].x);
 #pragma unroll
-                    for (int k = 0; k < NS / 2; ++k) f[k] = f1[k];
-                }
+                for (int x = 0; x < X; ++x) advance<M>(h[x], f[x], s[x].y, Bt);
+                load_pairs<M>(Ct, &sh.C[tb + i][n0]);
+#pragma unroll
+                for (int x = 0; x < X; ++x) y[X * i + x] = dot<M>(h[x], Ct);
+                if (i + 1 < kSteps)
+#pragma unroll
+                    for (int x = 0; x < X; ++x) {
+                        s[x] = s1[x];
+#pragma unroll
+                        for (int k = 0; k < M / 2; ++k) f[x][k] = f1[x][k];
+                    }
             }
-            // the sums of L frames at a time over L lanes: each exchange halves the frames a lane holds, until lane q has
-            // frame q of them
+            // The sums of as many frames and channels as lanes at a time: each exchange halves the values that a lane holds, until
+            // lane q has the q-th of them. (More lanes than values: whole sums over the lanes beyond first.)
+            constexpr int kAtOnce = Q < X * kSteps ? Q : X * kSteps;
+            if constexpr (Q > kAtOnce)
 #pragma unroll
-            for (int r = 0; r < kSteps; r += L) {
+                for (int i = 0; i < X * kSteps; ++i) y[i] = __fadd_rn(y[i], __shfl_xor_sync(0xffffffffu, y[i], kAtOnce));
 #pragma unroll
-                for (int o = L / 2; o > 0; o >>= 1)
+            for (int r = 0; r < X * kSteps; r += kAtOnce) {
+#pragma unroll
+                for (int o = kAtOnce / 2; o > 0; o >>= 1)
 #pragma unroll
                     for (int i = 0; i < o; ++i) {
                         const float send = q & o ? y[r + i] : y[r + i + o], keep = q & o ? y[r + i + o] : y[r + i];
                         y[r + i] = __fadd_rn(keep, __shfl_xor_sync(0xffffffffu, send, o));
                     }
-                yw[tb + r + q][c] = y[r];
+                const int at = r + (q & (kAtOnce - 1));
+                if (Q <= kAtOnce || q < kAtOnce) yw[tb + at / X][c + at % X] = y[r];
             }
         }
         __syncwarp();
@@ -697,8 +738,10 @@ __global__ void __launch_bounds__(32 * ScanWarp<NS, L>::kBlockWarps, sizeof(T) =
     }
     if (there && a.state_out && rank == a.parts - 1) {
 #pragma unroll
-        for (int i = 0; i < NS; ++i)
-            if (c < chans && n0 + i < a.N) a.state_out[(b * a.D + d0 + c) * a.N + n0 + i] = i & 1 ? h[i / 2].y : h[i / 2].x;
+        for (int x = 0; x < X; ++x)
+#pragma unroll
+            for (int i = 0; i < M; ++i)
+                if (c + x < chans && n0 + i < a.N) a.state_out[state_at(x, i)] = i & 1 ? h[x][i / 2].y : h[x][i / 2].x;
     }
     if (a.parts > W) cluster_wait();
 }
