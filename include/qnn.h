@@ -364,7 +364,7 @@ qnn_status qnn_qmatmul4(const uint8_t *A, int64_t lda, const qnn_qparams *pa, in
  *          zeros), and the last W - 1 inputs after the last one. They may be the same buffer, for streaming.
  *   lengths [B] int32, nullable: frames of each sequence (values outside 0 .. T count as the nearer of them). Frames behind a
  *          sequence's end are not read for it and their outputs are left as they are.
- * One frame of many sequences (T = 1 with states) is the serving form; T = 0 only carries the states over.
+ * One frame of many sequences (T = 1 with states) is the serving form; T = 0 only carries the states over. T <= 2^30.
  */
 qnn_status qnn_causal_conv(const void *x, int64_t x_seq, int64_t x_frame, int dtype, int64_t B, int64_t T, int64_t D,
                            const float *w, int32_t W, const float *bias, int silu, const void *state_in, void *state_out,

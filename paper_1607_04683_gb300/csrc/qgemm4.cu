@@ -133,6 +133,9 @@ __device__ __forceinline__ uint32_t codes_x1(uint32_t v) {
 // contiguous stretches) and add up through shared memory at the end, in a fixed order. Bound: the weights' bytes. Each
 // warp streams its own column tiles through kStages slots of shared memory by asynchronous copies, across row tiles, so that
 // 16 kStages KB a block are in flight at any time; a slot is read into registers and filled again before its products.
+// Measured (weights from HBM): 1 x 8192 x 8192 in groups of 32, 42 MB, 11.9 us (3.5 TB/s; 192 instructions a cell of 16 rows x
+// 128 columns, 0.57 a cycle and scheduler), of 128 10.5; 8 rows 13.8; 16 rows 15.3 in groups of 128; 1 x 2048 x 2048 3.7 us, of
+// which 1.1 are a launch with one load and one store and 0.7 the activations' way into shared memory.
 constexpr int kMmThreads = 512, kMmWarps = kMmThreads / 32, kRedStride = 20, kMostBlocks = 4;
 constexpr float kUnit = 0x1p-20f, kPerUnit = 0x1p20f;
 

@@ -3,6 +3,10 @@
 //
 // Every code of a row goes by the last bit of s, so s must not depend on how the sum is split: the squares are summed in
 // pairs of fp32 (value and remainder, about 2^-46 relative), the root is taken of the pair and rounded once.
+//
+// Bound: HBM in fp32 (16384 x 2048 with the residual's sum and the recovered values, 571 MB: 89.7 us, 6.4 TB/s; 128000 x 500 161 us,
+// 6.8 TB/s), the instructions in 16 bits (bf16, 369 MB, 80 us: some 70 instructions a value, ten of them the exact sum, half
+// the bytes).
 #include <cfloat>
 
 #include "elem.cuh"
