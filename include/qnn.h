@@ -292,7 +292,7 @@ qnn_status qnn_quantize_matrix_static(const float *x, int64_t rows, int64_t cols
  * layer whose state update is element-wise:
  *   qnn_rmsnorm_quantize -> qnn_qmatmul4 (or qnn_qmatmul) -> qnn_causal_conv -> qnn_ssm_scan -> qnn_quantize -> a product.
  * For these calls device pointers have to belong to the current device (or be managed memory), and an output may not
- * overlap an input unless a call allows it; QNN_ERR_INVALID_ARG otherwise, before anything runs. Overlap is judged by the
+ * overlap an input unless a call allows it; QNN_ERR_INVALID_ARG otherwise, before anything runs. Overlap goes by the
  * range from an argument's first byte to its last. Rows (sequences, frames) times their stride may not pass 2^48 elements.
  * The calls take no scratch, so any number may run at once, and may be captured into a graph after a first call on the device
  * (which allocates the device status word).
