@@ -172,12 +172,12 @@ __device__ __forceinline__ void all_here(bool cluster) {
     else
         __syncthreads();
 }
-// A shared variable of another block of the cluster.
+// A shared variable of a block of the cluster, written before all_here. (No order against other loads: several are in flight.)
 __device__ __forceinline__ float peer_load(const float *p, int rank) {
     uint32_t at;
     float v;
     asm("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(at) : "r"((uint32_t)__cvta_generic_to_shared(p)), "r"(rank));
-    asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v) : "r"(at) : "memory");
+    asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v) : "r"(at));
     return v;
 }
 
@@ -374,11 +374,22 @@ __global__ void __launch_bounds__(kMmThreads, 1) qmatmul4_kernel(const Mm4Args a
                 row_sum = __ldg(a.row_sums + n), bias = a.bias ? __ldg(a.bias + n) : 0.0f;
             }
             float sum = 0.0f;
-            for (int b = 0; b < a.blocks; ++b)
-                for (int k = 0; k < segments; ++k) {
-                    const float *at = red + (((tg << a.seg_shift) + k) * kRows + m) * kRedStride + row;
-                    sum = __fadd_rn(sum, b == rank ? *at : peer_load(at, b));
+            const float *at = red + ((tg << a.seg_shift) * kRows + m) * kRedStride + row;
+            if (a.blocks == 1) {
+                for (int k = 0; k < segments; ++k) sum = __fadd_rn(sum, at[k * (kRows * kRedStride)]);
+            } else {  // four loads in flight: one takes as long as the barrier
+                const int all = a.blocks << a.seg_shift;
+                for (int j = 0; j < all; j += 4) {
+                    float part[4];
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        const int k = j + e;
+                        part[e] = k < all ? peer_load(at + (k & (segments - 1)) * (kRows * kRedStride), k >> a.seg_shift) : 0.0f;
+                    }
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) sum = __fadd_rn(sum, part[e]);
                 }
+            }
             a.Y[(m0 + m) * a.ldy + n] = recover4(__fmul_rn(sum, kPerUnit), p.Q, (float)p.z, row_sum, bias);
         }
     }
