@@ -95,8 +95,9 @@ struct Mm4Args {
 };
 
 // y from the sum t1 over centered codes c = a' - 128: sum (a' + za) w^ = t1 + (128 + za) sum w^, over Qa, plus the bias.
-__device__ __forceinline__ float recover4(float t1, float Q, float z, float row_sum, float bias) {
-    return __fadd_rn(__fdiv_rn(__fmaf_rn(__fadd_rn(128.0f, z), row_sum, t1), Q), bias);
+// `unit`: Qa, 128 + za.
+__device__ __forceinline__ float recover4(float t1, float2 unit, float row_sum, float bias) {
+    return __fadd_rn(__fdiv_rn(__fmaf_rn(unit.y, row_sum, t1), unit.x), bias);
 }
 
 __device__ __forceinline__ void mma_f16(float (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
@@ -203,6 +204,7 @@ __global__ void __launch_bounds__(kMmThreads, 1) qmatmul4_kernel(const Mm4Args a
     float *reds = reinterpret_cast<float *>(smem + P::kRing);        // [kReds][warps][kRows][kRedStride]
     uint8_t *sA = smem + P::kRing + P::kReds * P::kRed;              // [rows][stride]
     float *sR = reinterpret_cast<float *>(sA + rows * a.stride);     // [chunk groups][kRows]: group sums of b - 128
+    float2 *sP = reinterpret_cast<float2 *>(sR + a.chunk * kGroups * kRows);  // [rows]: Qa, 128 + za
     const int segments = 1 << a.seg_shift, seg = warp & (segments - 1), tile_group = warp >> a.seg_shift;
     const int tile_groups = kMmWarps >> a.seg_shift;
     const int rank = a.blocks > 1 ? (int)(blockIdx.x & (a.blocks - 1)) : 0;  // (of the cluster: its size divides the grid)
@@ -238,69 +240,84 @@ __global__ void __launch_bounds__(kMmThreads, 1) qmatmul4_kernel(const Mm4Args a
         }
         copies_commit();
     };
+    // A's codes of column tiles kt0 .. kt1, 16 a thread and step (past K: 128, which counts 0), kAtOnce steps at a time: loaded,
+    // and put into shared memory as fp16 values and their sums by groups, over 2 to 8 lanes
+    constexpr int kAtOnce = NT == 1 ? 2 : 4;
+    const int per_row = a.chunk * (kTileCols / 16), total = rows * per_row;
+    uint32_t v[kAtOnce][4];
+    auto load_A = [&](int i0, int kt0) {
+#pragma unroll
+        for (int s = 0; s < kAtOnce; ++s) {
+            const int i = i0 + s * kMmThreads + tid, m = (int)__umulhi((uint32_t)i, a.per_row_magic), k = kt0 * kTileCols + 16 * (i - m * per_row);
+            v[s][0] = v[s][1] = v[s][2] = v[s][3] = 0x80808080u;
+            if (i >= total || k >= a.K) continue;
+            const uint8_t *p = a.A + (m0 + m) * a.lda + k;
+            if (a.align == 16 && k + 16 <= a.K) {
+                const uint4 x = __ldg(reinterpret_cast<const uint4 *>(p));
+                v[s][0] = x.x, v[s][1] = x.y, v[s][2] = x.z, v[s][3] = x.w;
+            } else {
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    if (a.align >= 4 && k + 4 * j + 4 <= a.K) {
+                        v[s][j] = __ldg(reinterpret_cast<const uint32_t *>(p + 4 * j));
+                    } else if (k + 4 * j < a.K) {
+                        v[s][j] = 0;
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) v[s][j] |= (uint32_t)(k + 4 * j + e < a.K ? __ldg(p + 4 * j + e) : 128) << (8 * e);
+                    }
+                }
+            }
+        }
+    };
+    auto put_A = [&](int i0, int there) {  // of a row's steps
+#pragma unroll
+        for (int s = 0; s < kAtOnce; ++s) {
+            const int i = i0 + s * kMmThreads + tid, m = (int)__umulhi((uint32_t)i, a.per_row_magic), blk = i - m * per_row;
+            uint32_t sum = 0;
+#pragma unroll
+            for (int j = 0; j < 4; ++j) sum = __dp4a(v[s][j], 0x01010101u, sum);
+#pragma unroll
+            for (int o = 1; o < GROUP / 16; o *= 2) sum += __shfl_xor_sync(0xffffffffu, sum, o);
+            if (i >= total || blk >= there) continue;
+            uint4 *to = reinterpret_cast<uint4 *>(sA + m * a.stride + 32 * blk);
+            to[0] = make_uint4(codes_x16(v[s][0]), codes_x1(v[s][0]), codes_x16(v[s][1]), codes_x1(v[s][1]));
+            to[1] = make_uint4(codes_x16(v[s][2]), codes_x1(v[s][2]), codes_x16(v[s][3]), codes_x1(v[s][3]));
+            if (blk % (GROUP / 16) == 0) sR[blk / (GROUP / 16) * kRows + m] = (float)((int)sum - 128 * GROUP) * kUnit;
+        }
+    };
+    auto stage = [&](int kt0, int kt1, bool loaded) {
+        for (int i0 = 0; i0 < total; i0 += kAtOnce * kMmThreads) {
+            if (i0 > 0 || !loaded) load_A(i0, kt0);
+            put_A(i0, (kt1 - kt0) * (kTileCols / 16));
+        }
+    };
+    // (A before the weights: behind 16 kStages KB a block of them its first codes came 2.4 us later)
+    load_A(0, kt_begin);
 #pragma unroll
     for (int i = 0; i < P::kStages; ++i) issue(i);
+    stage(kt_begin, min(kt_end, kt_begin + a.chunk), true);
     int slot = 0, red_at = 0;
-    // what this thread's first output of a row tile needs is loaded ahead
+    if (tid < rows) {
+        const qnn_qparams p = a.pa[a.per_row ? m0 + tid : 0];
+        sP[tid] = make_float2(p.Q, __fadd_rn(128.0f, (float)p.z));
+    }
     const int wide_shift = 8 - a.seg_shift, wide = 1 << wide_shift;  // columns of an item: 16 a tile group
     const int share = wide * rows / a.blocks, first_out = rank * share;  // this block's outputs of them
-    const bool mine = tid < share;
-    qnn_qparams my_unit = {};
-    if (mine) my_unit = a.pa[a.per_row ? m0 + ((first_out + tid) >> wide_shift) : 0];
+    const int col = (first_out + tid) & (wide - 1);  // this thread's column, of all its outputs: kMmThreads is a multiple of wide
+    __syncthreads();
 
     for (int64_t item = first_item; item < a.items; item += item_step) {
-        float acc[NT][4] = {}, my_sum = 0.0f, my_bias = 0.0f;
-        if (const int64_t n = item * wide + ((first_out + tid) & (wide - 1)); mine && n < a.N) {
-            my_sum = __ldg(a.row_sums + n);
-            if (a.bias) my_bias = __ldg(a.bias + n);
+        float acc[NT][4] = {}, row_sum = 0.0f, bias = 0.0f;
+        const int64_t n = item * wide + col;
+        if (tid < share && n < a.N) {  // what its outputs need is loaded ahead
+            row_sum = __ldg(a.row_sums + n);
+            if (a.bias) bias = __ldg(a.bias + n);
         }
         for (int chunk = 0; chunk < a.chunks; ++chunk) {
             const int kt0 = min(kt_end, kt_begin + chunk * a.chunk), kt1 = min(kt_end, kt0 + a.chunk);
-            if (a.chunks > 1 || item == first_item) {
-                if (chunk > 0 || item != first_item) __syncthreads();  // all warps are done with what was there
-                // A's codes, 16 a thread and step (past K: 128, which counts 0), as fp16 values, and their sums by groups, over
-                // 2 to 8 lanes; kAtOnce steps' loads in flight
-                constexpr int kAtOnce = NT == 1 ? 2 : 4;
-                const int blocks = a.chunk * (kTileCols / 16), there = (kt1 - kt0) * (kTileCols / 16), total = rows * blocks;
-                for (int i0 = 0; i0 < total; i0 += kAtOnce * kMmThreads) {
-                    uint32_t v[kAtOnce][4];
-#pragma unroll
-                    for (int s = 0; s < kAtOnce; ++s) {
-                        const int i = i0 + s * kMmThreads + tid, m = (int)__umulhi((uint32_t)i, a.per_row_magic), k = kt0 * kTileCols + 16 * (i - m * blocks);
-                        v[s][0] = v[s][1] = v[s][2] = v[s][3] = 0x80808080u;
-                        if (i >= total || k >= a.K) continue;
-                        const uint8_t *p = a.A + (m0 + m) * a.lda + k;
-                        if (a.align == 16 && k + 16 <= a.K) {
-                            const uint4 x = __ldg(reinterpret_cast<const uint4 *>(p));
-                            v[s][0] = x.x, v[s][1] = x.y, v[s][2] = x.z, v[s][3] = x.w;
-                        } else {
-#pragma unroll
-                            for (int j = 0; j < 4; ++j) {
-                                if (a.align >= 4 && k + 4 * j + 4 <= a.K) {
-                                    v[s][j] = __ldg(reinterpret_cast<const uint32_t *>(p + 4 * j));
-                                } else if (k + 4 * j < a.K) {
-                                    v[s][j] = 0;
-#pragma unroll
-                                    for (int e = 0; e < 4; ++e) v[s][j] |= (uint32_t)(k + 4 * j + e < a.K ? __ldg(p + 4 * j + e) : 128) << (8 * e);
-                                }
-                            }
-                        }
-                    }
-#pragma unroll
-                    for (int s = 0; s < kAtOnce; ++s) {
-                        const int i = i0 + s * kMmThreads + tid, m = (int)__umulhi((uint32_t)i, a.per_row_magic), blk = i - m * blocks;
-                        uint32_t sum = 0;
-#pragma unroll
-                        for (int j = 0; j < 4; ++j) sum = __dp4a(v[s][j], 0x01010101u, sum);
-#pragma unroll
-                        for (int o = 1; o < GROUP / 16; o *= 2) sum += __shfl_xor_sync(0xffffffffu, sum, o);
-                        if (i >= total || blk >= there) continue;
-                        uint4 *to = reinterpret_cast<uint4 *>(sA + m * a.stride + 32 * blk);
-                        to[0] = make_uint4(codes_x16(v[s][0]), codes_x1(v[s][0]), codes_x16(v[s][1]), codes_x1(v[s][1]));
-                        to[1] = make_uint4(codes_x16(v[s][2]), codes_x1(v[s][2]), codes_x16(v[s][3]), codes_x1(v[s][3]));
-                        if (blk % (GROUP / 16) == 0) sR[blk / (GROUP / 16) * kRows + m] = (float)((int)sum - 128 * GROUP) * kUnit;
-                    }
-                }
+            if (a.chunks > 1 && (chunk > 0 || item != first_item)) {
+                __syncthreads();  // all warps are done with what was there
+                stage(kt0, kt1, false);
                 __syncthreads();
             }
             const uint8_t *pa[NT];  // (columns past the rows there are repeat the last: their sums go nowhere)
@@ -363,16 +380,8 @@ __global__ void __launch_bounds__(kMmThreads, 1) qmatmul4_kernel(const Mm4Args a
             p[8] = acc[c][2], p[kRedStride + 8] = acc[c][3];
         }
         all_here(a.blocks > 1);
-        for (int i = tid; i < share; i += kMmThreads) {
-            const int o = first_out + i, m = o >> wide_shift, col = o & (wide - 1), tg = col / kTileRows, row = col % kTileRows;
-            const int64_t n = item * wide + col;
-            if (n >= a.N) continue;
-            qnn_qparams p = my_unit;
-            float row_sum = my_sum, bias = my_bias;
-            if (i != tid) {
-                p = a.pa[a.per_row ? m0 + m : 0];
-                row_sum = __ldg(a.row_sums + n), bias = a.bias ? __ldg(a.bias + n) : 0.0f;
-            }
+        for (int i = n < a.N ? tid : share; i < share; i += kMmThreads) {
+            const int m = (first_out + i) >> wide_shift, tg = col / kTileRows, row = col % kTileRows;
             float sum = 0.0f;
             const float *at = red + ((tg << a.seg_shift) * kRows + m) * kRedStride + row;
             if (a.blocks == 1) {
@@ -390,7 +399,7 @@ __global__ void __launch_bounds__(kMmThreads, 1) qmatmul4_kernel(const Mm4Args a
                     for (int e = 0; e < 4; ++e) sum = __fadd_rn(sum, part[e]);
                 }
             }
-            a.Y[(m0 + m) * a.ldy + n] = recover4(__fmul_rn(sum, kPerUnit), p.Q, (float)p.z, row_sum, bias);
+            a.Y[(m0 + m) * a.ldy + n] = recover4(__fmul_rn(sum, kPerUnit), sP[m], row_sum, bias);
         }
     }
     if (a.blocks > 1) all_here(true);  // the others may still read this block's sums
@@ -405,7 +414,7 @@ qnn_status launch_mm4(Mm4Args a, cudaStream_t st) {
     constexpr size_t kMost = 227 * 1024 - 64, kFixed = P::kRing + P::kReds * P::kRed;
     const int rows = (int)std::min<int64_t>(P::kRows, a.M), sms = sm_count();
     const size_t sums = (size_t)P::kGroups * P::kRows * 4;  // a column tile's group sums
-    const int fit = (int)((kMost - kFixed - (size_t)rows * 64) / ((size_t)rows * 2 * kTileCols + sums));
+    const int fit = (int)((kMost - kFixed - (size_t)rows * (64 + sizeof(float2))) / ((size_t)rows * 2 * kTileCols + sums));
     // Blocks that share a row tile's columns: as many as hold all of A between them and convert at most kMostCells cells of it
     // each (a row's column tile), and, where row tiles are few, as many as give half of the SMs one (a column tile each at
     // least). (16 x 8192 x 8192: A in two parts through one block 18.9 us, two blocks 15.8, four 15.3; 8 x 8192 x 8192 one 14.4, two
@@ -431,7 +440,7 @@ qnn_status launch_mm4(Mm4Args a, cudaStream_t st) {
     a.stride = a.chunk * 2 * kTileCols + 64;  // (so that the two rows of a quarter of a load lie in different banks)
     const uint32_t steps = (uint32_t)a.chunk * (kTileCols / 16);
     a.per_row_magic = (uint32_t)((((uint64_t)1 << 32) + steps - 1) / steps);  // (exact: at most 32 rows of 2072 steps)
-    const size_t bytes = kFixed + (size_t)rows * a.stride + (size_t)a.chunk * sums;
+    const size_t bytes = kFixed + (size_t)rows * (a.stride + sizeof(float2)) + (size_t)a.chunk * sums;
     const auto kern = qmatmul4_kernel<GROUP, NT>;
     static std::atomic<bool> allowed[64];  // by device: the attribute costs a microsecond a call
     int dev = 0;
