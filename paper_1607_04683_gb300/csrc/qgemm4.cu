@@ -134,9 +134,11 @@ __device__ __forceinline__ uint32_t codes_x1(uint32_t v) {
 // contiguous stretches) and add up through shared memory at the end, in a fixed order. Bound: the weights' bytes. Each
 // warp streams its own column tiles through kStages slots of shared memory by asynchronous copies, across row tiles, so that
 // 16 kStages KB a block are in flight at any time; a slot is read into registers and filled again before its products.
-// Measured (weights from HBM): 1 x 8192 x 8192 in groups of 32, 42 MB, 11.9 us (3.5 TB/s; 192 instructions a cell of 16 rows x
-// 128 columns, 0.57 a cycle and scheduler), of 128 10.5; 8 rows 13.8; 16 rows 15.3 in groups of 128; 1 x 2048 x 2048 3.7 us, of
-// which 1.1 are a launch with one load and one store and 0.7 the activations' way into shared memory.
+// Measured (weights from HBM): 1 x 8192 x 8192 in groups of 32, 42 MB, 11.2 to 11.8 us (3.7 TB/s; 192 instructions a cell of 16
+// rows x 128 columns), of 128 10.2; 8 rows in groups of 128 10.9; 16 rows 13.2; 1 x 2048 x 2048 3.1 us, of which 1.1 are a launch
+// with one load and one store. Clock stamps, 16 rows: 1.6 us until A's loads and the first copies are out, 1.3 for A's way into
+// shared memory, 7.8 the products (16 cells a warp, 234 cycles each and scheduler, 128 of them the tensor pipe's), 0.6 the
+// barrier, 1.1 the sums and 0.7 the last barrier. Four or five slots a warp: 13.3 and 13.6 us.
 constexpr int kMmThreads = 512, kMmWarps = kMmThreads / 32, kRedStride = 20, kMostBlocks = 4;
 constexpr float kUnit = 0x1p-20f, kPerUnit = 0x1p20f;
 
@@ -415,13 +417,13 @@ qnn_status launch_mm4(Mm4Args a, cudaStream_t st) {
     const int rows = (int)std::min<int64_t>(P::kRows, a.M), sms = sm_count();
     const size_t sums = (size_t)P::kGroups * P::kRows * 4;  // a column tile's group sums
     const int fit = (int)((kMost - kFixed - (size_t)rows * (64 + sizeof(float2))) / ((size_t)rows * 2 * kTileCols + sums));
-    // Blocks that share a row tile's columns: as many as hold all of A between them and convert at most kMostCells cells of it
-    // each (a row's column tile), and, where row tiles are few, as many as give half of the SMs one (a column tile each at
-    // least). (16 x 8192 x 8192: A in two parts through one block 18.9 us, two blocks 15.8, four 15.3; 8 x 8192 x 8192 one 14.4, two
-    // 13.8, 16 x 2048 x 8192 one 7.8, two 8.6.)
+    // Blocks that share a row tile's columns: kMostBlocks where A has more than kMostCells cells (a row's column tile) to convert
+    // or does not fit, and, where row tiles are few, as many as give half of the SMs one (a column tile each at least).
+    // (16 x 8192 x 8192: A in two parts through one block 16.7 us, two blocks 14.5, four 13.2; 8 x 8192 x 8192, 512 cells, one 12.4,
+    // two 11.5, four 10.9; 16 x 2048 x 8192, 256 cells, one 6.7, four 7.7.)
     constexpr int kMostCells = 256;
     a.blocks = 1;
-    while (a.blocks < kMostBlocks && (a.blocks * fit < a.ktiles || rows * a.ktiles > kMostCells * a.blocks ||
+    while (a.blocks < kMostBlocks && (a.blocks * fit < a.ktiles || rows * a.ktiles > kMostCells ||
                                       (2 * ntiles * a.blocks <= sms && 2 * a.blocks <= a.ktiles)))
         a.blocks *= 2;
     a.span = (a.ktiles + a.blocks - 1) / a.blocks;

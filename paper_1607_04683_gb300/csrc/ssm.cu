@@ -46,8 +46,9 @@ struct ConvArgs {
 // has read the old state before it writes the new one, and later chunks (at least WT - 1 frames on) never look at it. W < WT
 // taps stand at the end of WT, the others are not loaded and count 0.
 //
-// Bound: HBM in fp32 (16 x 1000 x 2048, 4 taps: 43 us, 6.1 TB/s), the instructions of SiLU and of the conversions beside it in 16
-// bits (bf16 28.7 us, 4.6 TB/s, 11.6 instructions a value at 0.45 a cycle and scheduler).
+// Bound: HBM. 16 x 1000 x 2048, 4 taps: fp32 42 to 44 us (6.1 TB/s), bf16 27 to 28.5 (4.7 TB/s; without SiLU 25.9, a plain copy of
+// as many bytes 22.9). Tried for bf16 and no faster: two channels a thread at twice the warps, 16 and 24 frames ahead, chunks of 24
+// to 112 frames.
 constexpr int kMostTaps = 8, kConvThreads = 128;
 template <typename T, int WT, int V, int kAhead>
 __global__ void __launch_bounds__(kConvThreads) causal_conv_kernel(const ConvArgs a) {
