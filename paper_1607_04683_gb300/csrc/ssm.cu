@@ -38,25 +38,26 @@ struct ConvArgs {
     const float *w, *bias;
     const int32_t *lengths;
     int64_t x_seq, x_frame, y_seq, y_frame, B, T, D, runs, chunks;
-    int W, silu, chunk;
+    int silu, chunk;
 };
 
-// A thread takes V neighbouring channels of a sequence over a chunk of its frames in rounds of kAhead, the last WT - 1 inputs
+// A thread takes V neighbouring channels of a sequence over a chunk of its frames in rounds of kAhead, the last W - 1 inputs
 // in registers and the next round's loads in flight. The first chunk's thread alone reads and writes the channels' state: it
-// has read the old state before it writes the new one, and later chunks (at least WT - 1 frames on) never look at it. W < WT
-// taps stand at the end of WT, the others are not loaded and count 0.
+// has read the old state before it writes the new one, and later chunks (at least W - 1 frames on) never look at it. A kernel for
+// each number of taps: in one for more of them the missing ones would be products of 0 with older inputs, NaN where those
+// are not finite.
 //
 // Bound: HBM. 16 x 1000 x 2048, 4 taps: fp32 42 to 44 us (6.1 TB/s), bf16 27 to 28.5 (4.7 TB/s; without SiLU 25.9, a plain copy of
 // as many bytes 22.9). Tried for bf16 and no faster: two channels a thread at twice the warps, 16 and 24 frames ahead, chunks of 24
 // to 112 frames.
 constexpr int kMostTaps = 8, kConvThreads = 128;
-template <typename T, int WT, int V, int kAhead>
+template <typename T, int W, int V, int kAhead>
 __global__ void __launch_bounds__(kConvThreads) causal_conv_kernel(const ConvArgs a) {
     const int64_t at = (int64_t)blockIdx.x * kConvThreads + threadIdx.x;
     const Split of_runs = split(at, a.runs), of_chunks = split(of_runs.quot, a.chunks);
     const int64_t run = of_runs.rem, chunk = of_chunks.rem, b = of_chunks.quot;
     if (b >= a.B) return;
-    const int n = frames_of(a.lengths, b, a.T), t0 = (int)chunk * a.chunk, t1 = min(n, t0 + a.chunk), W = a.W;
+    const int n = frames_of(a.lengths, b, a.T), t0 = (int)chunk * a.chunk, t1 = min(n, t0 + a.chunk);
     if (chunk > 0 && t0 >= n) return;
     const int64_t d = run * V;
     const T *x = static_cast<const T *>(a.x) + b * a.x_seq + d;
@@ -67,21 +68,20 @@ __global__ void __launch_bounds__(kConvThreads) causal_conv_kernel(const ConvArg
 #pragma unroll
         for (int v = 0; v < V; ++v) to[v] = r.get(v);
     };
-    float in[WT - 1 + kAhead][V];  // the WT - 1 inputs before a round of kAhead frames, and the round's
+    float in[W - 1 + kAhead][V];  // the W - 1 inputs before a round of kAhead frames, and the round's
     {
-        Run<T, V> r[WT];
+        Run<T, V> r[W];
 #pragma unroll
-        for (int j = 0; j < WT - 1; ++j) {  // before the chunk: WT - 1 - j frames back of t0
-            const int t = t0 - (WT - 1) + j;
+        for (int j = 0; j < W - 1; ++j) {  // before the chunk: W - 1 - j frames back of t0
+            const int t = t0 - (W - 1) + j;
             r[j].clear();
-            if (j < WT - W) continue;
             if (chunk > 0)
                 r[j].load(x + t * a.x_frame);
             else if (a.state_in)
                 r[j].load(s_in + (t + W - 1) * a.D);
         }
 #pragma unroll
-        for (int j = 0; j < WT - 1; ++j) unpack(r[j], in[j]);
+        for (int j = 0; j < W - 1; ++j) unpack(r[j], in[j]);
     }
     if (t0 < t1) {
         Run<T, V> next[kAhead];
@@ -95,17 +95,17 @@ __global__ void __launch_bounds__(kConvThreads) causal_conv_kernel(const ConvArg
             }
         };
         fetch(t1 - t0);
-        float w[WT][V], bias[V];
+        float w[W][V], bias[V];
 #pragma unroll
         for (int v = 0; v < V; ++v) {
             bias[v] = a.bias ? __ldg(a.bias + d + v) : 0.0f;
-            if (WT == 4 && W == 4 && V > 1) {  // (V channels' taps lie side by side: whole loads; one by one, a load's 32 lanes
+            if constexpr (W == 4 && V > 1) {  // (V channels' taps lie side by side: whole loads; one by one, a load's 32 lanes
                                                // touch as many lines)
                 const float4 q = __ldg(reinterpret_cast<const float4 *>(a.w + (d + v) * 4));
                 w[0][v] = q.x, w[1][v] = q.y, w[2][v] = q.z, w[3][v] = q.w;
             } else {
 #pragma unroll
-                for (int j = 0; j < WT; ++j) w[j][v] = j >= WT - W ? __ldg(a.w + (d + v) * W + j - (WT - W)) : 0.0f;
+                for (int j = 0; j < W; ++j) w[j][v] = __ldg(a.w + (d + v) * W + j);
             }
         }
         auto frame = [&](int i) {  // the i-th of the round
@@ -115,14 +115,14 @@ __global__ void __launch_bounds__(kConvThreads) causal_conv_kernel(const ConvArg
                 for (int v = 0; v < V; v += 2) {
                     float2 f = make_float2(bias[v], bias[v + 1]);
 #pragma unroll
-                    for (int j = 0; j < WT; ++j) f = ffma2_rn(make_float2(w[j][v], w[j][v + 1]), make_float2(in[i + j][v], in[i + j][v + 1]), f);
+                    for (int j = 0; j < W; ++j) f = ffma2_rn(make_float2(w[j][v], w[j][v + 1]), make_float2(in[i + j][v], in[i + j][v + 1]), f);
                     if (a.silu) f = silu2(f);
                     o[v] = f.x, o[v + 1] = f.y;
                 }
             } else {
                 o[0] = bias[0];
 #pragma unroll
-                for (int j = 0; j < WT; ++j) o[0] = __fmaf_rn(w[j][0], in[i + j][0], o[0]);
+                for (int j = 0; j < W; ++j) o[0] = __fmaf_rn(w[j][0], in[i + j][0], o[0]);
                 if (a.silu) o[0] = silu(o[0]);
             }
             Run<T, V> out;
@@ -133,22 +133,22 @@ __global__ void __launch_bounds__(kConvThreads) causal_conv_kernel(const ConvArg
         int t = t0;
         for (; t + kAhead <= t1; t += kAhead) {
 #pragma unroll
-            for (int i = 0; i < kAhead; ++i) unpack(next[i], in[WT - 1 + i]);
+            for (int i = 0; i < kAhead; ++i) unpack(next[i], in[W - 1 + i]);
             fetch(t1 - t - kAhead);
 #pragma unroll
             for (int i = 0; i < kAhead; ++i) frame(i);
 #pragma unroll
-            for (int j = 0; j < WT - 1; ++j)
+            for (int j = 0; j < W - 1; ++j)
 #pragma unroll
                 for (int v = 0; v < V; ++v) in[j][v] = in[j + kAhead][v];
         }
 #pragma unroll
         for (int i = 0; i < kAhead - 1; ++i) {  // the frames of a last, shorter round
             if (t + i >= t1) break;
-            unpack(next[i], in[WT - 1]);
+            unpack(next[i], in[W - 1]);
             frame(0);
 #pragma unroll
-            for (int j = 0; j < WT - 1; ++j)
+            for (int j = 0; j < W - 1; ++j)
 #pragma unroll
                 for (int v = 0; v < V; ++v) in[j][v] = in[j + 1][v];
         }
@@ -157,12 +157,11 @@ __global__ void __launch_bounds__(kConvThreads) causal_conv_kernel(const ConvArg
     // the last W - 1 of old state and n frames. Where the chunk holds all frames they are at hand
     if (n <= a.chunk) {
 #pragma unroll
-        for (int j = 0; j < WT - 1; ++j)
-            if (j >= WT - W) {
-                Run<T, V> last;
-                last.set(in[j]);
-                last.store(s_out + (j - (WT - W)) * a.D);
-            }
+        for (int j = 0; j < W - 1; ++j) {
+            Run<T, V> last;
+            last.set(in[j]);
+            last.store(s_out + j * a.D);
+        }
     } else {
         for (int j = 0; j < W - 1; ++j) {
             Run<T, V> last;
@@ -838,7 +837,7 @@ qnn_status launch_scan(ScanArgs &a, cudaStream_t st) {
     return launch_tiles<T, 8, 16>(a, st);
 }
 
-template <typename T, int WT>
+template <typename T, int W>
 qnn_status launch_conv(ConvArgs a, cudaStream_t st) {
     constexpr int V = 4;  // (eight 16-bit values a thread: 26 us where four take 22)
     const int e = sizeof(T);
@@ -853,10 +852,25 @@ qnn_status launch_conv(ConvArgs a, cudaStream_t st) {
     a.chunks = std::max<int64_t>(1, (a.T + a.chunk - 1) / a.chunk);
     const int64_t blocks = (a.B * a.runs * a.chunks + kConvThreads - 1) / kConvThreads;
     if (blocks > INT32_MAX) return QNN_FAIL(QNN_ERR_INVALID_ARG);
-    const auto kern = vec ? (few ? causal_conv_kernel<T, WT, V, 1> : causal_conv_kernel<T, WT, V, 8>)
-                          : (few ? causal_conv_kernel<T, WT, 1, 1> : causal_conv_kernel<T, WT, 1, 8>);
+    const auto kern = vec ? (few ? causal_conv_kernel<T, W, V, 1> : causal_conv_kernel<T, W, V, 8>)
+                          : (few ? causal_conv_kernel<T, W, 1, 1> : causal_conv_kernel<T, W, 1, 8>);
     kern<<<(unsigned)blocks, kConvThreads, 0, st>>>(a);
     return QNN_OK;
+}
+
+template <typename T>
+qnn_status launch_conv(const ConvArgs &a, int W, cudaStream_t st) {
+    static_assert(kMostTaps == 8);
+    switch (W) {
+        case 1: return launch_conv<T, 1>(a, st);
+        case 2: return launch_conv<T, 2>(a, st);
+        case 3: return launch_conv<T, 3>(a, st);
+        case 4: return launch_conv<T, 4>(a, st);
+        case 5: return launch_conv<T, 5>(a, st);
+        case 6: return launch_conv<T, 6>(a, st);
+        case 7: return launch_conv<T, 7>(a, st);
+        default: return launch_conv<T, 8>(a, st);
+    }
 }
 
 constexpr int64_t kMostCount = (int64_t)1 << 40, kMostFrames = 1 << 30;
@@ -906,12 +920,10 @@ extern "C" qnn_status qnn_causal_conv(const void *x, int64_t x_seq, int64_t x_fr
         if (ys.meets(in[i]) || (so.meets(in[i]) && !(i == 4 && state_in == state_out))) return QNN_ERR_INVALID_ARG;
     ConvArgs a;
     a.x = x, a.state_in = state_in, a.state_out = state_out, a.y = y, a.w = w, a.bias = bias, a.lengths = lengths;
-    a.x_seq = x_seq, a.x_frame = x_frame, a.y_seq = y_seq, a.y_frame = y_frame, a.B = B, a.T = T, a.D = D, a.W = W, a.silu = silu != 0;
+    a.x_seq = x_seq, a.x_frame = x_frame, a.y_seq = y_seq, a.y_frame = y_frame, a.B = B, a.T = T, a.D = D, a.silu = silu != 0;
     cudaStream_t st = as_stream(stream);
     ProfScope prof("causal_conv", st);
-    QNN_TRY(with_type(dtype, [&](auto t) {
-        return W <= 4 ? launch_conv<decltype(t), 4>(a, st) : launch_conv<decltype(t), kMostTaps>(a, st);
-    }));
+    QNN_TRY(with_type(dtype, [&](auto t) { return launch_conv<decltype(t)>(a, W, st); }));
     QNN_CUDA_TRY(cudaGetLastError());
     return QNN_OK;
 }
