@@ -311,7 +311,7 @@ typedef enum { QNN_F32 = 0, QNN_BF16 = 1, QNN_F16 = 2 } qnn_dtype;
  *                 v = (h s) weight, s = 1 / sqrt(sum h^2 / cols + eps); code_sums nullable.
  *   values        [rows x cols] fp32 (ldv >= cols), nullable: the values that the codes stand for, (code + z) / Q (eq. 3),
  *                 for consumers in float (the "quant" output layer of Sec. 5).
- * The codes are defined to the bit: the norm is taken of h before it is rounded to `dtype`; s is computed to about 2^-45
+ * The codes are defined to the bit: the norm is taken of h before it is rounded to `dtype`; s is computed to about 2^-44
  * relative and rounded once to fp32; h s and its product with the weight are each rounded once to fp32.
  * 1 <= cols <= 2^24. A row with a value of v that is not finite: its codes and values are unspecified and QNN_ERR_NONFINITE
  * is recorded, as for qnn_quantize (h is stored all the same).

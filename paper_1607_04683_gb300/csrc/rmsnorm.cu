@@ -1,8 +1,8 @@
 // rmsnorm.cu — residual addition, root-mean-square norm and the on-the-fly quantizer (Sec. 3, eq. 2) on sm_103a:
 // h = x + r; s = 1 / sqrt(mean h^2 + eps); v = (h s) w; one 8-bit unit per row of v.
 //
-// Every code of a row goes by the last bit of s, so s must not depend on how the sum is split: the squares are summed in
-// pairs of fp32 (value and remainder, about 2^-46 relative), the root is taken of the pair and rounded once.
+// Every code of a row goes by the last bit of s, so s should hardly ever depend on how the sum is split: the squares are summed
+// in pairs of fp32 (value and remainder, to about 2^-44 relative), the root is taken of the pair and rounded once.
 //
 // Bound: HBM in fp32 (16384 x 2048 with the residual's sum and the recovered values, 571 MB: 89.7 us, 6.4 TB/s; 128000 x 500 161 us,
 // 6.8 TB/s), the instructions in 16 bits (bf16, 369 MB, 80 us: some 70 instructions a value, ten of them the exact sum, half
@@ -33,6 +33,13 @@ struct Pair {
         add(p, __fmaf_rn(v, v, -p));
     }
     __device__ __forceinline__ void add(const Pair &o) { add(o.hi, o.lo); }
+    // The same sum with a remainder of at most half a step of hi. (Additions leave what they round off in lo, which is rounded
+    // itself: relative to a sum of n squares by up to n^2 2^-53, so that no more than 16 or 32 are added without this.)
+    __device__ __forceinline__ void settle() {
+        const float s = __fadd_rn(hi, lo);
+        lo = __fsub_rn(lo, __fsub_rn(s, hi));
+        hi = s;
+    }
 };
 
 __device__ __forceinline__ Pair warp_sum_pair(Pair a) {
@@ -270,8 +277,21 @@ __global__ void __launch_bounds__(kThreads) rmsnorm_long_rows_kernel(const NormA
     const T *r = a.r ? static_cast<const T *>(a.r) + row * a.ldr : nullptr;
     auto h_at = [&](int k) { return r ? __fadd_rn(to_f32(x[k]), to_f32(r[k])) : to_f32(x[k]); };
     const float s = row_scale(a, [&](float scale) {
+        // a thread's squares (up to 2^14) in sums of 16, of 32 of those, of 32 of those: in one sum, of 2^14 equal ones, up to
+        // 2^-25 were lost, so 2^-44
         Pair p;
-        for (int k = threadIdx.x; k < a.cols; k += kThreads) p.add_square(__fmul_rn(h_at(k), scale));
+        for (int k = threadIdx.x; k < a.cols;) {
+            Pair p32;
+            for (int i = 0; i < 32 && k < a.cols; ++i) {
+                Pair p16;
+#pragma unroll 4
+                for (int j = 0; j < 16 && k < a.cols; ++j, k += kThreads) p16.add_square(__fmul_rn(h_at(k), scale));
+                p32.add(p16);
+                p32.settle();
+            }
+            p.add(p32);
+            p.settle();
+        }
         return block_sum(p, sh, kThreads / 32, scale != 1.0f);
     });
     float mn = FLT_MAX, mx = -FLT_MAX, bad = 0.0f;

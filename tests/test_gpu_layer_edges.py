@@ -46,3 +46,25 @@ def test_conv_keeps_what_is_not_finite_to_its_taps(qnn, W, D, kind):
         assert same(torch.cat(parts, 1), got), n
     gated = qnn.qnn_causal_conv(x, w, bias=b, state_in=s)
     assert torch.isfinite(gated[~touched]).all()
+
+
+# --------------------------------------------------------------------------------------- norm
+
+def test_norm_of_the_longest_rows(qnn):
+    """Rows of one value: s = 1 / sqrt(v^2 + eps), which 64 bits hold (v^2 is exact there), and every v of the row is (v s) w."""
+    cols, n = 1 << 24, 64
+    v = rng(24).uniform(0.5, 2, n).astype(np.float32)
+    x = gpu(v)[:, None].expand(n, cols).contiguous()
+    _, params, _, _, _ = qnn.qnn_rmsnorm_quantize(x, torch.ones(cols, device="cuda"))
+    s = (1 / np.sqrt(v.astype(np.float64) ** 2 + 1e-5)).astype(np.float32)
+    got = qnn.params_view(params)
+    assert np.array_equal(got["vmin"], v * s) and np.array_equal(got["vmax"], v * s)
+    assert qnn.device_status() == qnn.QNN_OK
+
+
+@pytest.mark.parametrize("kind", ["f32", "bf16"])
+@pytest.mark.parametrize("cols", [1 << 20, (1 << 22) + 3])
+def test_norm_of_long_rows(qnn, cols, kind):
+    from test_gpu_layer import check_norm, norm_inputs
+    x, w, r = norm_inputs(cols, 1, cols, kind)
+    check_norm(qnn, x, w, r)
