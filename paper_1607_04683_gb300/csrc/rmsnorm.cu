@@ -371,9 +371,9 @@ extern "C" qnn_status qnn_rmsnorm_quantize(const void *x, int64_t ldx, const voi
                                            const float *weight, double eps, int64_t rows, int64_t cols, void *residual_out,
                                            int64_t ldh, uint8_t *codes, int64_t ldc, qnn_qparams *params,
                                            int32_t *code_sums, float *values, int64_t ldv, void *stream) {
-    constexpr int64_t kMostCols = 1 << 24, kMostRows = INT32_MAX;
+    constexpr int64_t kMostCols = 1 << 24, kMostRows = INT32_MAX, kMostSummed = INT32_MAX / 255;  // (sums of codes are 32 bits)
     auto bad = [&](int64_t ld) { return ld < cols || !reach_ok(rows, ld); };
-    if (!dtype_ok(dtype) || rows < 0 || rows > kMostRows || cols < 1 || cols > kMostCols || !(eps >= 1e-20 && eps <= 1e20) ||
+    if (!dtype_ok(dtype) || rows < 0 || rows > kMostRows || cols < 1 || cols > (code_sums ? kMostSummed : kMostCols) || !(eps >= 1e-20 && eps <= 1e20) ||
         bad(ldx) || bad(ldc) || (residual && bad(ldr)) || (residual_out && bad(ldh)) || (values && bad(ldv)))
         return QNN_ERR_INVALID_ARG;
     if (rows == 0) return QNN_OK;

@@ -40,6 +40,7 @@ EXPORTS = ("qnn_status_string", "qnn_device_status", "qnn_quantize", "qnn_qmatmu
            "qnn_rmsnorm_quantize", "qnn_quantize4", "qnn_qmatmul4", "qnn_causal_conv", "qnn_ssm_scan")
 
 _DTYPES = {}  # qnn_dtype of a torch type
+_MOST_SUMMED = (2 ** 31 - 1) // 255  # values of a row whose codes' sum has 32 bits
 # qnn_ssm_args as it lies in memory
 _SSM_ARGS = struct.Struct("=3q4i" + 6 * "Q2q" + "6Q")
 
@@ -345,7 +346,8 @@ def qnn_rmsnorm_quantize(x, weight, residual=None, eps=1e-5, residual_out=None, 
     """Rows of x (+ residual) [rows, cols] (fp32, bf16 or fp16), through a root-mean-square norm with weight [cols] fp32, to
     8-bit codes, one unit per row. Returns (codes u8, params int32 [rows, 4], code_sums int32 [rows], h, values): h = x +
     residual in x's type (residual_out, which may be x or residual, or a new tensor; None without a residual), values the
-    fp32 values that the codes stand for (None unless wanted)."""
+    fp32 values that the codes stand for (None unless wanted). Rows of more than 8421504 values have no code_sums (None): they
+    could pass 32 bits."""
     torch, L = _libs()
     if x.dim() != 2 or not x.is_cuda:
         _bad("x: a CUDA matrix")
@@ -371,13 +373,13 @@ def qnn_rmsnorm_quantize(x, weight, residual=None, eps=1e-5, residual_out=None, 
     w = _flat(weight, "weight", torch.float32, (cols,))
     codes = empty(shape, dtype=torch.uint8, device=dev)
     params = empty((rows, 4), dtype=torch.int32, device=dev)
-    sums = empty((rows,), dtype=torch.int32, device=dev)
+    sums = empty((rows,), dtype=torch.int32, device=dev) if cols <= _MOST_SUMMED else None
     values = None
     if want_values:
         values = empty(shape, dtype=torch.float32, device=dev)
         pv = values.data_ptr()
     st = L.qnn_rmsnorm_quantize(x.data_ptr(), ldx, pr, ldr, dt, w, eps, rows, cols, ph, ldh, codes.data_ptr(), cols,
-                                params.data_ptr(), sums.data_ptr(), pv, cols, _here(torch))
+                                params.data_ptr(), sums.data_ptr() if sums is not None else 0, pv, cols, _here(torch))
     if st:
         _check(st, "qnn_rmsnorm_quantize")
     return codes, params, sums, h, values

@@ -68,3 +68,13 @@ def test_norm_of_long_rows(qnn, cols, kind):
     from test_gpu_layer import check_norm, norm_inputs
     x, w, r = norm_inputs(cols, 1, cols, kind)
     check_norm(qnn, x, w, r)
+
+
+def test_norm_code_sums_end_where_they_could_pass_32_bits(qnn):
+    most = (2 ** 31 - 1) // 255
+    x, w = torch.full((1, most + 1), 1.0, device="cuda"), torch.ones(most + 1, device="cuda")
+    x[:, 0] = -1e-6  # nearly all codes are 255
+    codes, _, sums, _, _ = qnn.qnn_rmsnorm_quantize(x[:, :most], w[:most])
+    assert codes.long().sum().item() == sums.item() > 2 ** 31 - 1000
+    codes, _, sums, _, _ = qnn.qnn_rmsnorm_quantize(x, w)
+    assert sums is None and codes.long().sum().item() > 2 ** 31 - 1000
