@@ -177,6 +177,13 @@ __global__ void __launch_bounds__(kConvThreads) causal_conv_kernel(const ConvArg
 
 constexpr int kMostStates = 128;
 
+// The hardware's exponential lies low: by 0.5 to 0.8e-8 on average for arguments of -2^-14 .. -2^-8, 1.6 to 2.7e-8 for -2^-8 .. -2^-2
+// (relative; its rounding noise is 3e-8). Over a state's memory of 1/(s A) frames noise grows as the root and bias as itself, so
+// arguments are taken kBias higher, by the multiply-add that forms them: -1.3 to 0.8e-8 are left (a state after 100 frames
+// 2.0e-6 off without, 0.9e-6 with). A step of 0 still has a factor of 1, as exp2(kBias) rounds to it.
+constexpr float kBias = 2e-8f;
+__device__ __forceinline__ float factor(float s, float A) { return exp2_hw(__fmaf_rn(s, A, kBias)); }
+
 struct ScanArgs : qnn_ssm_args {
     bool vec;             // (few frames) runs of four states are loaded and stored whole
     int64_t group_chans;  // D / groups
@@ -288,7 +295,7 @@ __global__ void __launch_bounds__(kStepThreads, 4) ssm_step_kernel(const ScanArg
                 y[i] = 0.0f;
 #pragma unroll
                 for (int k = 0; k < 4; ++k) {
-                    h[i][k] = __fmaf_rn(exp2_hw(__fmul_rn(si, A[k])), h[i][k], __fmul_rn(sui, rB[i].get(k)));
+                    h[i][k] = __fmaf_rn(factor(si, A[k]), h[i][k], __fmul_rn(sui, rB[i].get(k)));
                     y[i] = __fmaf_rn(rC[i].get(k), h[i][k], y[i]);
                 }
             }
@@ -383,12 +390,6 @@ struct ScanWarp {
 
 // A frame's factors exp2(s A), its step h <- f h + su B and the sum of C h, for M states in pairs: one instruction for two
 // results.
-//
-// The hardware's exponential lies low: by 0.5 to 0.8e-8 on average for arguments of -2^-14 .. -2^-8, 1.6 to 2.7e-8 for -2^-8 .. -2^-2
-// (relative; its rounding noise is 3e-8). Over a state's memory of 1/(s A) frames noise grows as the root and bias as itself, so
-// arguments are taken kBias higher, by the multiply-add that forms them: -1.3 to 0.8e-8 are left (a state after 100 frames
-// 2.0e-6 off without, 0.9e-6 with). A step of 0 still has a factor of 1, as exp2(kBias) rounds to it.
-constexpr float kBias = 2e-8f;
 template <int M>
 __device__ __forceinline__ void factors(float2 (&f)[M / 2], const float2 (&A)[M / 2], float s) {
     const float2 s2 = make_float2(s, s);
@@ -606,7 +607,7 @@ __global__ void __launch_bounds__(32 * ScanWarp<NS, L>::kBlockWarps, sizeof(T) =
             for (int i = 0; i < NS; ++i) {
                 float &to = i & 1 ? h[i / M][i % M / 2].y : h[i / M][i % M / 2].x;
                 const float Ai = i & 1 ? A[i / M][i % M / 2].y : A[i / M][i % M / 2].x;
-                to = first_part ? r[i] : __fmaf_rn(exp2_hw(__fmul_rn(s[i / M], Ai)), to, r[i]);
+                to = first_part ? r[i] : __fmaf_rn(factor(s[i / M], Ai), to, r[i]);
             }
         };
         auto compose_warps = [&](float (&total)[X], int end, bool first_part) {  // and the sum of their steps

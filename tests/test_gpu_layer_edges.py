@@ -3,7 +3,7 @@ add up: against 64-bit references with bounds tighter than the general ones (lay
 import numpy as np
 import pytest
 
-from test_gpu_layer import gpu, qnn, rng  # noqa: F401
+from test_gpu_layer import gpu, host, qnn, rng  # noqa: F401
 
 torch = pytest.importorskip("torch")
 pytestmark = pytest.mark.gpu
@@ -78,3 +78,37 @@ def test_norm_code_sums_end_where_they_could_pass_32_bits(qnn):
     assert codes.long().sum().item() == sums.item() > 2 ** 31 - 1000
     codes, _, sums, _, _ = qnn.qnn_rmsnorm_quantize(x, w)
     assert sums is None and codes.long().sum().item() > 2 ** 31 - 1000
+
+
+# --------------------------------------------------------------------------------------- scan
+
+def long_memory(qnn, frames_a_call):
+    """(signed and root-mean-square deviation of states after 400 frames in calls of some frames): of sums of positive terms, whose
+    factors exp(-x), x = 2^-8 .. 2^-3, are each 1 + d times theirs. h' = f (1 + d) h + b deviates by d g, g' = f (g + h)."""
+    g = rng(17)
+    B, T, D, N = 2, 400, 256, 16
+    s = gpu(g.uniform(0.5, 1, (B, T, D)).astype(np.float32))
+    A = (-2.0 ** g.uniform(-7, -3, (D, N))).astype(np.float32)
+    one, bc = torch.ones(B, T, D, device="cuda"), torch.ones(B, T, N, device="cuda")
+    state, Ag = torch.zeros(B, D, N, device="cuda"), gpu(A)
+    for t in range(0, T, frames_a_call):
+        k = slice(t, t + frames_a_call)
+        qnn.qnn_ssm_scan(one[:, k], s[:, k], Ag, bc[:, k], bc[:, k], softplus=False, state_in=state, state_out=state)
+    h, dev = np.zeros((B, D, N)), np.zeros((B, D, N))
+    for t in range(T):
+        st = host(s[:, t])[..., None]
+        f = np.exp(st * A.astype(np.float64))
+        h, dev = f * h + st, f * (dev + h)
+    e, memory = (host(state) - h) / h, dev / h
+    # noise a frame: 3e-8 of the exponential, 2^-24 / sqrt(3) each of the product and the sum, which fade with the state
+    allowed = 1.5e-8 * memory + 6e-8 * np.sqrt(memory) + 6e-8
+    return e.sum() / memory.sum(), np.sqrt((e ** 2).mean()) / np.sqrt((allowed ** 2).mean())
+
+
+@pytest.mark.parametrize("frames_a_call", [1, 2, 4, 8, 400])
+def test_scan_long_memory(qnn, frames_a_call):
+    """Factors are right on average to 1.3e-8, whose sum over a state's memory noise does not hide; 0.2e-8 for the rest (log2 e
+    rounded to fp32 counts 1.3e-8 x)."""
+    bias, noise = long_memory(qnn, frames_a_call)
+    print(f"calls of {frames_a_call}: factors off by {bias:.2e} on average, states by {noise:.2f} of what is allowed")
+    assert abs(bias) <= 1.5e-8 and noise <= 1
