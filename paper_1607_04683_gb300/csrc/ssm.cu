@@ -1,6 +1,7 @@
 // ssm.cu — the recurrent half of a selective state-space layer on sm_103a: a short causal convolution per channel and the
 // selective scan, for whole sequences and for single frames with carried states.
 #include <algorithm>
+#include <cfloat>
 
 #include "elem.cuh"
 #include "qnn_device.cuh"
@@ -182,6 +183,12 @@ constexpr int kMostStates = 128;
 // arguments are taken kBias higher, by the multiply-add that forms them: -1.3 to 0.8e-8 are left (a state after 100 frames
 // 2.0e-6 off without, 0.9e-6 with). A step of 0 still has a factor of 1, as exp2(kBias) rounds to it.
 constexpr float kBias = 2e-8f;
+// A log2(e), as a number: a frame that is not there has a step of 0, whose product with an infinity would be a NaN. (Steps
+// of 2^-120 and more have factors of 0 by minus FLT_MAX as by minus infinity.)
+__device__ __forceinline__ float rate(float A) {
+    const float v = __fmul_rn(A, kLog2e);
+    return isinf(v) ? copysignf(FLT_MAX, v) : v;
+}
 __device__ __forceinline__ float factor(float s, float A) { return exp2_hw(__fmaf_rn(s, A, kBias)); }
 
 struct ScanArgs : qnn_ssm_args {
@@ -215,7 +222,7 @@ __global__ void __launch_bounds__(kStepThreads, 4) ssm_step_kernel(const ScanArg
         else if (count)
             r.load(a.A + d * a.N + n0);
 #pragma unroll
-        for (int k = 0; k < 4; ++k) A[k] = __fmul_rn(r.get(k), kLog2e);
+        for (int k = 0; k < 4; ++k) A[k] = rate(r.get(k));
     }
     const float skip = a.skip ? __ldg(a.skip + d) : 0.0f, bias = a.dt_bias ? __ldg(a.dt_bias + d) : 0.0f;
 
@@ -522,7 +529,7 @@ __global__ void __launch_bounds__(32 * ScanWarp<NS, L>::kBlockWarps, sizeof(T) =
 #pragma unroll
         for (int i = 0; i < M; ++i) {
             const bool ok = c + x < chans && n0 + i < a.N;
-            const float v = ok ? __fmul_rn(__ldg(a.A + (d0 + c + x) * a.N + n0 + i), kLog2e) : 0.0f;
+            const float v = ok ? rate(__ldg(a.A + (d0 + c + x) * a.N + n0 + i)) : 0.0f;
             const float s = ok && start ? a.state_in[state_at(x, i)] : 0.0f;
             if (i & 1)
                 A[x][i / 2].y = v, h[x][i / 2].y = s;

@@ -3,7 +3,7 @@ add up: against 64-bit references with bounds tighter than the general ones (lay
 import numpy as np
 import pytest
 
-from test_gpu_layer import gpu, host, qnn, rng  # noqa: F401
+from test_gpu_layer import gpu, host, qnn, rng, scan_inputs, scan_want, within  # noqa: F401
 
 torch = pytest.importorskip("torch")
 pytestmark = pytest.mark.gpu
@@ -112,3 +112,22 @@ def test_scan_long_memory(qnn, frames_a_call):
     bias, noise = long_memory(qnn, frames_a_call)
     print(f"calls of {frames_a_call}: factors off by {bias:.2e} on average, states by {noise:.2f} of what is allowed")
     assert abs(bias) <= 1.5e-8 and noise <= 1
+
+
+@pytest.mark.parametrize("T", [1, 4, 40, 600])
+def test_scan_channels_without_a_memory(qnn, T):
+    """A of minus infinity, or so low that its product with log2 e has no fp32 value: a factor of 0, as A = -1e6 gives; a frame that
+    is not there leaves the states as they are."""
+    lengths = [T, 0, 1, T // 2, max(T - 1, 0), T - T // 3]
+    i = scan_inputs(3, len(lengths), T, 40, 16, 1, "f32", softplus=False)
+    i["dt_bias"] = None
+    i["A"][3], i["A"][17, 5] = -1e6, -1e6
+    want, bound, state, sbound = scan_want(i, False, lengths, "f32")
+    i["A"][3], i["A"][17, 5] = -np.inf, -3e38
+    a = {k: v if isinstance(v, torch.Tensor) else gpu(v) for k, v in i.items()}
+    out = torch.empty(len(lengths), 40, 16, device="cuda")
+    got = host(qnn.qnn_ssm_scan(a["u"], a["dt"], a["A"], a["B"], a["C"], D=a["D"], z=a["z"], softplus=False, state_in=a["state_in"],
+                                state_out=out, lengths=torch.tensor(lengths, dtype=torch.int32, device="cuda")))
+    assert np.isfinite(sbound).all()
+    within(got, want, bound)
+    within(host(out), state, sbound)
