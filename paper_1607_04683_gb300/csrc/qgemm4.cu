@@ -128,7 +128,9 @@ __device__ __forceinline__ uint32_t codes_x1(uint32_t v) {
 //   - an 8-bit code b under the byte 0x64 is the fp16 number 1024 + b, from which one multiply-add makes 16 (b - 128) for
 //     columns whose weights count once and b - 128 for those that count 16 times.
 // So every product is (b - 128) code 2^-20, and a group's sum, below 2^24 of that unit, is exact in fp32. The sum of a
-// group starts from offset x (sum of b - 128) and is taken into the output's sum by its scale, in fp32.
+// group starts from offset x (sum of b - 128) and is taken into the output's sum by its scale, in fp32, 2^4 times as large: a
+// scale is a multiple of 2^-133 (eight bits from 2^-126 on), so products with it are multiples of 2^-149, as every fp32 number is,
+// and none loses bits below the range's end; at its other end they overflow no earlier than the whole sum.
 //
 // A block's 16 warps split the columns of its row tiles (`segments` of them, tile by tile in turn, so that a block reads long
 // contiguous stretches) and add up through shared memory at the end, in a fixed order. Bound: the weights' bytes. Each
@@ -140,7 +142,7 @@ __device__ __forceinline__ uint32_t codes_x1(uint32_t v) {
 // shared memory, 7.8 the products (16 cells a warp, 234 cycles each and scheduler, 128 of them the tensor pipe's), 0.6 the
 // barrier, 1.1 the sums and 0.7 the last barrier. Four or five slots a warp: 13.3 and 13.6 us.
 constexpr int kMmThreads = 512, kMmWarps = kMmThreads / 32, kRedStride = 20, kMostBlocks = 4;
-constexpr float kUnit = 0x1p-20f, kPerUnit = 0x1p20f;
+constexpr float kUnit = 0x1p-20f, kUp = 0x1p4f, kPerUnit = 0x1p16f;
 
 __device__ __forceinline__ void copy16_async(uint32_t to, const void *from) {
     asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(to), "l"(from) : "memory");
@@ -309,7 +311,8 @@ __global__ void __launch_bounds__(kMmThreads, 1) qmatmul4_kernel(const Mm4Args a
     __syncthreads();
 
     for (int64_t item = first_item; item < a.items; item += item_step) {
-        float acc[NT][4] = {}, row_sum = 0.0f, bias = 0.0f;
+        float2 acc[NT][2] = {};  // by row; its two columns
+        float row_sum = 0.0f, bias = 0.0f;
         const int64_t n = item * wide + col;
         if (tid < share && n < a.N) {  // what its outputs need is loaded ahead
             row_sum = __ldg(a.row_sums + n);
@@ -343,12 +346,11 @@ __global__ void __launch_bounds__(kMmThreads, 1) qmatmul4_kernel(const Mm4Args a
                     const int q = j * 32 / GROUP;
                     if (j * 32 % GROUP == 0) {  // a group begins: offset x (sum of its b - 128)
                         const float2 *R = reinterpret_cast<const float2 *>(sR + ((kt - kt0) * kGroups + q) * kRows) + t;
-                        const float z0 = unit_offset(u0.u[q]), z1 = unit_offset(u1.u[q]);
+                        const float2 z0 = f2(unit_offset(u0.u[q])), z1 = f2(unit_offset(u1.u[q]));
 #pragma unroll
                         for (int c = 0; c < NT; ++c) {
-                            const float2 v = R[4 * c];
-                            sum[c][0] = __fmul_rn(z0, v.x), sum[c][1] = __fmul_rn(z0, v.y);
-                            sum[c][2] = __fmul_rn(z1, v.x), sum[c][3] = __fmul_rn(z1, v.y);
+                            const float2 v = R[4 * c], s0 = fmul2_rn(z0, v), s1 = fmul2_rn(z1, v);
+                            sum[c][0] = s0.x, sum[c][1] = s0.y, sum[c][2] = s1.x, sum[c][3] = s1.y;
                         }
                     }
                     const uint32_t x = w0[j], y = w1[j], x8 = x >> 8, y8 = y >> 8;
@@ -361,11 +363,11 @@ __global__ void __launch_bounds__(kMmThreads, 1) qmatmul4_kernel(const Mm4Args a
                         mma_f16(sum[c], wb, v.z, v.w);
                     }
                     if ((j + 1) * 32 % GROUP == 0) {  // and ends
-                        const float s0 = unit_scale(u0.u[q]), s1 = unit_scale(u1.u[q]);
+                        const float2 s0 = f2(unit_scale(u0.u[q])), s1 = f2(unit_scale(u1.u[q]));
 #pragma unroll
                         for (int c = 0; c < NT; ++c) {
-                            acc[c][0] = __fmaf_rn(s0, sum[c][0], acc[c][0]), acc[c][1] = __fmaf_rn(s0, sum[c][1], acc[c][1]);
-                            acc[c][2] = __fmaf_rn(s1, sum[c][2], acc[c][2]), acc[c][3] = __fmaf_rn(s1, sum[c][3], acc[c][3]);
+                            acc[c][0] = ffma2_rn(s0, fmul2_rn(make_float2(sum[c][0], sum[c][1]), f2(kUp)), acc[c][0]);
+                            acc[c][1] = ffma2_rn(s1, fmul2_rn(make_float2(sum[c][2], sum[c][3]), f2(kUp)), acc[c][1]);
                         }
                     }
                 }
@@ -378,8 +380,8 @@ __global__ void __launch_bounds__(kMmThreads, 1) qmatmul4_kernel(const Mm4Args a
 #pragma unroll
         for (int c = 0; c < NT; ++c) {
             float *p = red + (warp * kRows + 8 * c + 2 * t) * kRedStride + g;
-            p[0] = acc[c][0], p[kRedStride] = acc[c][1];
-            p[8] = acc[c][2], p[kRedStride + 8] = acc[c][3];
+            p[0] = acc[c][0].x, p[kRedStride] = acc[c][0].y;
+            p[8] = acc[c][1].x, p[kRedStride + 8] = acc[c][1].y;
         }
         all_here(a.blocks > 1);
         for (int i = n < a.N ? tid : share; i < share; i += kMmThreads) {

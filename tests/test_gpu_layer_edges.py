@@ -3,7 +3,8 @@ add up: against 64-bit references with bounds tighter than the general ones (lay
 import numpy as np
 import pytest
 
-from test_gpu_layer import gpu, host, qnn, rng, scan_inputs, scan_want, within  # noqa: F401
+import layer_ref as ref
+from test_gpu_layer import activations, gpu, host, qnn, rng, scan_inputs, scan_want, within  # noqa: F401
 
 torch = pytest.importorskip("torch")
 pytestmark = pytest.mark.gpu
@@ -78,6 +79,52 @@ def test_norm_code_sums_end_where_they_could_pass_32_bits(qnn):
     assert codes.long().sum().item() == sums.item() > 2 ** 31 - 1000
     codes, _, sums, _, _ = qnn.qnn_rmsnorm_quantize(x, w)
     assert sums is None and codes.long().sum().item() > 2 ** 31 - 1000
+
+
+# --------------------------------------------------------------------------------------- 4-bit products
+
+def check_product_by_groups(qnn, A, params, w, group, bias=None):
+    """The sum of a group's codes is exact. What is rounded: each addition of a group's term (any order: `groups` of them, each
+    relative to the terms' sizes), the row sum, 128 + z, their product's addition, the quotient and the bias' addition."""
+    codes, off, scale = ref.quantize4(w, group)
+    N, K = w.shape
+    ng = off.shape[1]
+    full = np.zeros((N, ng * group))
+    full[:, :K] = codes
+    c = (full.reshape(N, ng, group) + off[..., None])
+    if K % group:
+        c[:, -1, K % group:] = 0
+    a = np.zeros((len(A), ng * group))
+    a[:, :K] = A.astype(np.float64) - 128
+    terms = np.einsum("mgk,ngk->mng", a.reshape(len(A), ng, group), c) * scale.astype(np.float64)
+    z, Q = params["z"].astype(np.float64)[:, None] + 128, params["Q"].astype(np.float64)[:, None]
+    rows = (c.sum(2) * scale.astype(np.float64)).sum(1)
+    y = (terms.sum(2) + z * rows) / Q
+    bound = ((ng + 2) * np.abs(terms).sum(2) + 3 * np.abs(z * rows)) * ref.U / Q
+    if bias is not None:
+        y = y + bias.astype(np.float64)
+        bound = bound + 3 * ref.U * np.abs(bias)
+    got = qnn.qnn_qmatmul4(gpu(A), qnn.params_tensor(params), qnn.qnn_quantize4(gpu(w), group), bias=gpu(bias))
+    within(host(got), y, bound + 3 * ref.U * np.abs(y))
+
+
+@pytest.mark.parametrize("group", [32, 64, 128])
+@pytest.mark.parametrize("M", [1, 9, 20])
+def test_qmatmul4_scales_near_the_least(qnn, M, group):
+    """Scales of 2^-126 to 2^-122 on activations large enough that the results are ordinary numbers; few codes off the center, so
+    that groups' sums are a few units."""
+    g = rng(M + group)
+    N, K = 24, 512
+    w = g.integers(0, 16, (N, K)).astype(np.float64)
+    w[:, 0::32], w[:, 1::32] = 0, 15
+    w = (w * (g.uniform(1, 16, (N, 1)) * 2.0 ** -126)).astype(np.float32)
+    A = np.full((M, K), 128, np.uint8)
+    for m in range(M):
+        at = g.integers(0, 32, K // 32) + np.arange(0, K, 32)
+        A[m, at] = 128 + g.integers(-3, 4, K // 32)
+    params = np.zeros(M, qnn.QPARAMS_DTYPE)
+    params["Q"], params["z"], params["vmax"] = 2.0 ** -100, -128, 1.0
+    check_product_by_groups(qnn, A, params, w, group)
 
 
 # --------------------------------------------------------------------------------------- scan
