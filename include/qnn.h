@@ -403,10 +403,11 @@ typedef struct {
  *   y[t][d] = (sum_n Cm[t][g][n] h[n] + skip[d] u[t][d]) * z / (1 + exp(-z)),  z = z[t][d],
  * with the last factor only where z is given and g = d / (D / groups). States and sums are fp32. lengths, frames behind a
  * sequence's end and T = 0 as for qnn_causal_conv; state_out is the state after each sequence's last frame, and
- * the states of a sequence do not depend on the others. Long sequences are taken in parts whose states are put together by
- * their factors over a part (where states grow, A s > 0, that factor may overflow before a state does). One frame of many sequences is the serving form. An A
- * whose product with log2(e) is infinite counts as the last with a finite one, so that a step of 0 leaves its state as it is. Other non-finite inputs give non-finite outputs
- * (infinities or NaN), in their own channel and sequence (group, for Bm and Cm).
+ * the states of a sequence do not depend on the others. One frame of many sequences is the serving form.
+ * Long sequences are taken in parts whose states are put together by their factors over a part, unless that is not finite: it
+ * may overflow where states grow (A s > 0) although no state does, and the frames before a part are then gone over one by one.
+ * An A whose product with log2(e) is infinite counts as the last with a finite one, so that a step of 0 leaves its state as it is.
+ * Other non-finite inputs give non-finite outputs (infinities or NaN), in their own channel and sequence (group, for Bm and Cm).
  */
 qnn_status qnn_ssm_scan(const qnn_ssm_args *args, void *stream);
 

@@ -365,7 +365,9 @@ __device__ __forceinline__ float peer_load(uint32_t at) {
 // Where sequences are few, `parts` warps (of a block, or of a cluster of blocks) share each one's frames. The recurrence is
 // linear: over a part, h' = exp(A S) h + r, with S the sum of its steps and r what it reaches from h = 0. Each warp first
 // finds S and r of its part (no Cm, z or outputs), reads those of the parts before its own from shared memory, composes its
-// first state from them, and then goes over its part once more with it.
+// first state from them, and then goes over its part once more with it. Where that state is not finite, the factor of a part
+// (exp(A S) with A S > 0) or what it reached alone may have overflowed although the state does not: the warp then goes over all
+// frames from the first on, without their outputs before its part, and has what the formula gives.
 //
 // Bound: instructions. A frame of 16 channels x 16 states takes a warp 57 of them (16 states x 2: a product each for the
 // exponent and the input, a multiply-add each for the state and the sum, the exponential), 103 cycles alone for the steps and 68
@@ -578,6 +580,7 @@ __global__ void __launch_bounds__(32 * ScanWarp<NS, L>::kBlockWarps, sizeof(T) =
         }
     };
 
+    int begin = first;  // of the frames that this warp goes over for its outputs
     if (a.parts > 1) {
         put(sh.start);
         float sum[X] = {};
@@ -663,17 +666,34 @@ __global__ void __launch_bounds__(32 * ScanWarp<NS, L>::kBlockWarps, sizeof(T) =
                     compose(s[i], r[i], p0 + i == 0);
                 }
             }
-            cluster_arrive();  // waited for at the end: the others may still read this block's
             compose_warps(total, warp, block == 0);
         } else {
             take(sh.start);
             compose_warps(total, warp, true);
         }
+        float2 odd = f2(0.0f);
+#pragma unroll
+        for (int i = 0; i < NS; i += 2) odd = ffma2_rn(h[i / M][i % M / 2], f2(0.0f), odd);
+        if (__any_sync(0xffffffffu, !(odd.x == 0.0f && odd.y == 0.0f))) {  // from the sequence's first frame on
+            begin = 0;
+            seek(0);
+            fetch(0, true);
+#pragma unroll
+            for (int i = 0; i < NS; ++i) {
+                const float *at = &all[w0].start[i][lane];
+                const float v = cluster ? peer_load(peer_address(at, 0)) : *at;
+                if (i & 1)
+                    h[i / M][i % M / 2].y = v;
+                else
+                    h[i / M][i % M / 2].x = v;
+            }
+        }
+        if (cluster) cluster_arrive();  // waited for at the end: the others may still read this block's
     }
 
     constexpr int kSteps = 8;  // frames between stores: their loads and products overlap
-    T *py = static_cast<T *>(a.y) + b * a.y_seq + (first + row) * a.y_frame + d0 + run;
-    for (int t0 = first; t0 < last; t0 += kTile) {
+    T *py = static_cast<T *>(a.y) + b * a.y_seq + (begin + row) * a.y_frame + d0 + run;
+    for (int t0 = begin; t0 < last; t0 += kTile) {
         stage(t0, true);
 #pragma unroll
         for (int j = 0; j < R; ++j) cu[j] = ru[j];
@@ -732,7 +752,7 @@ __global__ void __launch_bounds__(32 * ScanWarp<NS, L>::kBlockWarps, sizeof(T) =
 #pragma unroll
         for (int j = 0; j < R; ++j) {
             const int r = row + j * Sh::kRows;
-            if (t0 + r < last) {
+            if (t0 + r < last && t0 >= first) {
                 float o[V];
 #pragma unroll
                 for (int v = 0; v < V; v += 2) {

@@ -178,3 +178,38 @@ def test_scan_channels_without_a_memory(qnn, T):
     assert np.isfinite(sbound).all()
     within(got, want, bound)
     within(host(out), state, sbound)
+
+
+def grown(T, D, N, from_state):
+    """States that grow by e^2 a frame over 70 frames and shrink again, from 1e-30; or that are 0 until they grow at the end."""
+    g = rng(T + D)
+    i = scan_inputs(4, 1, T, D, N, 1, "f32", gate=False, bias=False, softplus=False)
+    s = np.full((1, T, D), 0.05)
+    u = np.zeros((1, T, D))
+    if from_state:
+        s[:, :48] = 0
+        s[:, 48:118] = -2
+        s[:, 118:160] = 0.5
+        i["state_in"] = np.full((1, D, N), 1e-30, np.float32) * g.uniform(0.5, 1.5, (1, D, N)).astype(np.float32)
+    else:
+        s[:, :] = -2
+        u[:, T - 12:] = g.normal(0, 1, (1, 12, D))
+        i["state_in"] = None
+    i["A"] = np.full((D, N), -1.0, np.float32)
+    i["dt"], i["u"] = gpu(s.astype(np.float32)), gpu(u.astype(np.float32))
+    return i
+
+
+@pytest.mark.parametrize("from_state", [True, False])
+@pytest.mark.parametrize("T,D,N", [(200, 40, 16), (600, 40, 16), (600, 12, 4), (2050, 6, 100), (1200, 33, 24)])
+def test_scan_states_that_grow_where_a_sequence_is_shared(qnn, T, D, N, from_state):
+    """The factor over a part of the sequence has no fp32 value, the states and outputs have."""
+    i = grown(T, D, N, from_state)
+    want, bound, state, sbound = scan_want(i, False, None, "f32")
+    assert np.isfinite(bound).all() and np.isfinite(sbound).all()
+    a = {k: v if isinstance(v, torch.Tensor) else gpu(v) for k, v in i.items()}
+    out = torch.empty(1, D, N, device="cuda") if a["state_in"] is None else a["state_in"]
+    got = host(qnn.qnn_ssm_scan(a["u"], a["dt"], a["A"], a["B"], a["C"], D=a["D"], softplus=False, state_in=a["state_in"],
+                                state_out=out))
+    within(got, want, bound)
+    within(host(out), state, sbound)
