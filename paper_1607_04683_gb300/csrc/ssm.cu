@@ -1,6 +1,7 @@
 // ssm.cu — the recurrent half of a selective state-space layer on sm_103a: a short causal convolution per channel and the
 // selective scan, for whole sequences and for single frames with carried states.
 #include <algorithm>
+#include <atomic>
 #include <cfloat>
 
 #include "elem.cuh"
@@ -820,22 +821,39 @@ qnn_status launch_tiles(ScanArgs a, cudaStream_t st) {
     const int64_t tiles = (a.T + kTile - 1) / kTile;
     int parts = 1;
     while (parts < 16 * W && a.units * parts < 4 * (int64_t)sm_count() && 4 * parts <= tiles) parts *= 2;
-    const int64_t blocks = (a.units * parts + W - 1) / W;
-    if (blocks > INT32_MAX) return QNN_FAIL(QNN_ERR_INVALID_ARG);
     const auto kern = vec ? ssm_scan_kernel<T, NS, L, true> : ssm_scan_kernel<T, NS, L, false>;
-    const int cluster = std::max(1, parts / W);
-    if (cluster > 8) QNN_CUDA_TRY(cudaFuncSetAttribute(kern, cudaFuncAttributeNonPortableClusterSizeAllowed, 1));
-    a.parts = parts;
     cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3((unsigned)blocks);
-    cfg.blockDim = dim3(32 * W);
-    cfg.stream = st;
     cudaLaunchAttribute attr[1];
     attr[0].id = cudaLaunchAttributeClusterDimension;
-    attr[0].val.clusterDim.x = (unsigned)cluster;
     attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
+    cfg.blockDim = dim3(32 * W);
+    cfg.stream = st;
     cfg.attrs = attr;
-    cfg.numAttrs = cluster > 1 ? 1 : 0;
+    auto shared_by = [&](int n) {  // a cluster of as many blocks a unit
+        const int cluster = std::max(1, n / W);
+        a.parts = n;
+        attr[0].val.clusterDim.x = (unsigned)cluster;
+        cfg.numAttrs = cluster > 1 ? 1 : 0;
+        cfg.gridDim = dim3((unsigned)std::min<int64_t>((a.units * n + W - 1) / W, UINT32_MAX));
+    };
+    shared_by(parts);
+    if (parts > 8 * W) {  // a device need not have room for more than eight (it is asked once)
+        static std::atomic<int> room[2][64];
+        int dev = 0;
+        QNN_CUDA_TRY(cudaGetDevice(&dev));
+        if (dev < 0 || dev >= 64) return QNN_FAIL(QNN_ERR_CUDA);
+        int known = room[vec][dev].load(std::memory_order_acquire);
+        if (!known) {
+            int clusters = 0;
+            if (cudaFuncSetAttribute(kern, cudaFuncAttributeNonPortableClusterSizeAllowed, 1) != cudaSuccess ||
+                cudaOccupancyMaxActiveClusters(&clusters, kern, &cfg) != cudaSuccess)
+                cudaGetLastError();
+            known = clusters > 0 ? 1 : -1;
+            room[vec][dev].store(known, std::memory_order_release);
+        }
+        if (known < 0) shared_by(8 * W);
+    }
+    if (cfg.gridDim.x > INT32_MAX) return QNN_FAIL(QNN_ERR_INVALID_ARG);
     QNN_CUDA_TRY(cudaLaunchKernelEx(&cfg, kern, a));
     return QNN_OK;
 }

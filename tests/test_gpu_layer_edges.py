@@ -1,10 +1,14 @@
 """The selective state-space layer's calls where values are not finite, far apart or nearly out of range, and where small errors
 add up: against 64-bit references with bounds tighter than the general ones (layer_ref.py)."""
+import os
+import subprocess
+import sys
+
 import numpy as np
 import pytest
 
 import layer_ref as ref
-from test_gpu_layer import activations, gpu, host, qnn, rng, scan_inputs, scan_want, within  # noqa: F401
+from test_gpu_layer import activations, check_scan, gpu, host, qnn, rng, scan_inputs, scan_want, within  # noqa: F401
 
 torch = pytest.importorskip("torch")
 pytestmark = pytest.mark.gpu
@@ -213,3 +217,34 @@ def test_scan_states_that_grow_where_a_sequence_is_shared(qnn, T, D, N, from_sta
                                 state_out=out))
     within(got, want, bound)
     within(host(out), state, sbound)
+
+
+@pytest.mark.parametrize("B,T,D,N", [(1, 2050, 6, 100), (1, 1030, 5, 128), (2, 520, 40, 128), (3, 300, 9, 65), (1, 2100, 40, 16),
+                                     (1, 1100, 70, 64)])
+def test_scan_long_sequences_shared_by_many_blocks(qnn, B, T, D, N):
+    check_scan(qnn, B, T, D, N)
+    check_scan(qnn, B, T, D, N, place="in place", lengths=[T - 5, 0, T // 2][:B])
+
+
+def test_scan_captured_before_its_first_call(qnn):
+    """In a process of its own: a plan of many blocks a sequence, asked for while a graph is captured, has the bits of a plain call."""
+    code = '''
+import torch
+from paper_1607_04683_gb300 import qnn
+torch.cuda.set_device(0)
+qnn.device_status()
+g = torch.Generator(device="cuda").manual_seed(1)
+T, D, N = 2050, 6, 16
+u, dt = (torch.rand((1, T, D), generator=g, device="cuda") for _ in range(2))
+bc, A, out = torch.rand((1, T, N), generator=g, device="cuda"), -torch.rand((D, N), generator=g, device="cuda"), torch.zeros(1, T, D, device="cuda")
+torch.cuda.synchronize()
+graph = torch.cuda.CUDAGraph()
+with torch.cuda.graph(graph):
+    qnn.qnn_ssm_scan(u, dt, A, bc, bc, out=out)
+graph.replay()
+torch.cuda.synchronize()
+assert torch.equal(out, qnn.qnn_ssm_scan(u, dt, A, bc, bc)) and out.abs().sum() > 0
+'''
+    root = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+    r = subprocess.run([sys.executable, "-c", code], cwd=root, capture_output=True, text=True, timeout=240)
+    assert r.returncode == 0, r.stderr[-2000:]
