@@ -8,7 +8,7 @@ import numpy as np
 import pytest
 
 import layer_ref as ref
-from test_gpu_layer import activations, check_scan, gpu, host, qnn, rng, scan_inputs, scan_want, within  # noqa: F401
+from test_gpu_layer import activations, check_scan, gpu, host, qnn, rng, scan_inputs, scan_want, weights, within  # noqa: F401
 
 torch = pytest.importorskip("torch")
 pytestmark = pytest.mark.gpu
@@ -51,6 +51,16 @@ def test_conv_keeps_what_is_not_finite_to_its_taps(qnn, W, D, kind):
         assert same(torch.cat(parts, 1), got), n
     gated = qnn.qnn_causal_conv(x, w, bias=b, state_in=s)
     assert torch.isfinite(gated[~touched]).all()
+
+
+def test_conv_refuses_a_state_over_the_outputs(qnn):
+    x, w = torch.randn(2, 5, 16, device="cuda"), torch.randn(16, 4, device="cuda")
+    buf = torch.zeros(2 * 5 * 16 + 2 * 3 * 16, device="cuda")
+    with pytest.raises(qnn.QnnError):
+        qnn.qnn_causal_conv(x, w, out=buf[:160].view(2, 5, 16), state_out=buf[150:246].view(2, 3, 16))
+    with pytest.raises(qnn.QnnError):  # the states shifted over one another
+        qnn.qnn_causal_conv(x, w, state_in=buf[:96].view(2, 3, 16), state_out=buf[16:112].view(2, 3, 16))
+    qnn.qnn_causal_conv(x, w, out=buf[:160].view(2, 5, 16), state_out=buf[160:256].view(2, 3, 16))
 
 
 # --------------------------------------------------------------------------------------- norm
@@ -110,6 +120,28 @@ def check_product_by_groups(qnn, A, params, w, group, bias=None):
         bound = bound + 3 * ref.U * np.abs(bias)
     got = qnn.qnn_qmatmul4(gpu(A), qnn.params_tensor(params), qnn.qnn_quantize4(gpu(w), group), bias=gpu(bias))
     within(host(got), y, bound + 3 * ref.U * np.abs(y))
+
+
+@pytest.mark.parametrize("group", [32, 64, 128])
+@pytest.mark.parametrize("M,K,N", [(1, 8192, 48), (8, 8192, 20), (16, 8192, 33), (32, 4000, 20), (3, 500, 40), (33, 1000, 17),
+                                   (1, 33025, 16)])
+def test_qmatmul4_sums_of_groups(qnn, M, K, N, group):
+    A, params, _ = activations(M + K, M, K)
+    check_product_by_groups(qnn, A, params, weights(N + K, N, K), group, rng(N).normal(0, 1, N).astype(np.float32))
+
+
+@pytest.mark.parametrize("group", [32, 64, 128])
+@pytest.mark.parametrize("M,K", [(1, 8192), (9, 8192), (16, 1000), (32, 4096), (40, 8192)])
+def test_qmatmul4_of_whole_numbers_is_exact(qnn, M, K, group):
+    """Every code 0 or 255, every weight 0 or 15, a scale of 1: below 2^24, so no addition rounds."""
+    g = rng(M + K)
+    A = np.where(g.random((M, K)) < 0.7, 255, 0).astype(np.uint8)
+    w = np.where(g.random((40, K)) < 0.5, 0.0, 15.0).astype(np.float32)
+    w[:, 0::32], w[:, 1::32] = 0.0, 15.0
+    params = np.zeros(M, qnn.QPARAMS_DTYPE)
+    params["Q"], params["z"], params["vmax"] = 1.0, -128, 1.0
+    got = qnn.qnn_qmatmul4(gpu(A), qnn.params_tensor(params), qnn.qnn_quantize4(gpu(w), group))
+    assert np.array_equal(host(got), (A.astype(np.int64) - 128) @ w.astype(np.int64).T)
 
 
 @pytest.mark.parametrize("group", [32, 64, 128])
