@@ -279,19 +279,23 @@ __global__ void __launch_bounds__(kThreads) rmsnorm_long_rows_kernel(const NormA
     const float s = row_scale(a, [&](float scale) {
         // a thread's squares (up to 2^14) in sums of 16, of 32 of those, of 32 of those: in one sum, of 2^14 equal ones, up to
         // 2^-25 were lost, so 2^-44
-        Pair p;
-        for (int k = threadIdx.x; k < a.cols;) {
-            Pair p32;
-            for (int i = 0; i < 32 && k < a.cols; ++i) {
-                Pair p16;
-#pragma unroll 4
-                for (int j = 0; j < 16 && k < a.cols; ++j, k += kThreads) p16.add_square(__fmul_rn(h_at(k), scale));
-                p32.add(p16);
-                p32.settle();
-            }
-            p.add(p32);
-            p.settle();
+        Pair p, p32;
+        auto take = [](Pair &to, Pair &from) {
+            to.add(from);
+            to.settle();
+            from = Pair();
+        };
+        int k = threadIdx.x;
+        Pair p16;
+        for (int i = 1; k + 15 * kThreads < a.cols; ++i) {
+#pragma unroll
+            for (int j = 0; j < 16; ++j, k += kThreads) p16.add_square(__fmul_rn(h_at(k), scale));
+            take(p32, p16);
+            if (i % 32 == 0) take(p, p32);
         }
+        for (; k < a.cols; k += kThreads) p16.add_square(__fmul_rn(h_at(k), scale));
+        take(p32, p16);
+        take(p, p32);
         return block_sum(p, sh, kThreads / 32, scale != 1.0f);
     });
     float mn = FLT_MAX, mx = -FLT_MAX, bad = 0.0f;
