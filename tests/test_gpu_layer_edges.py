@@ -144,6 +144,19 @@ def test_qmatmul4_of_whole_numbers_is_exact(qnn, M, K, group):
     assert np.array_equal(host(got), (A.astype(np.int64) - 128) @ w.astype(np.int64).T)
 
 
+@pytest.mark.parametrize("M,N,K", [(16, 9800, 8192), (32, 19000, 4352), (8, 9800, 8300), (2000, 100, 1000), (5000, 33, 300)])
+def test_qmatmul4_of_whole_numbers_over_many_tiles(qnn, M, N, K):
+    """More row tiles than clusters run at once, and many blocks of rows: exact as above."""
+    g = torch.Generator(device="cuda").manual_seed(M + N)
+    A = torch.randint(0, 256, (M, K), generator=g, device="cuda", dtype=torch.uint8)
+    w = torch.randint(0, 16, (N, K), generator=g, device="cuda").float()
+    w[:, 0::32], w[:, 1::32] = 0.0, 15.0
+    params = np.zeros(M, qnn.QPARAMS_DTYPE)
+    params["Q"], params["z"], params["vmax"] = 1.0, -128, 1.0
+    got = qnn.qnn_qmatmul4(A, qnn.params_tensor(params), qnn.qnn_quantize4(w, 64))
+    assert torch.equal(got.double(), (A.double() - 128) @ w.double().t())
+
+
 @pytest.mark.parametrize("group", [32, 64, 128])
 @pytest.mark.parametrize("M", [1, 9, 20])
 def test_qmatmul4_scales_near_the_least(qnn, M, group):
