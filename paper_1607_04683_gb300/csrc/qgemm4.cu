@@ -136,11 +136,11 @@ __device__ __forceinline__ uint32_t codes_x1(uint32_t v) {
 // contiguous stretches) and add up through shared memory at the end, in a fixed order. Bound: the weights' bytes. Each
 // warp streams its own column tiles through kStages slots of shared memory by asynchronous copies, across row tiles, so that
 // 16 kStages KB a block are in flight at any time; a slot is read into registers and filled again before its products.
-// Measured (weights from HBM): 1 x 8192 x 8192 in groups of 32, 42 MB, 11.2 to 11.8 us (3.7 TB/s; 192 instructions a cell of 16
-// rows x 128 columns), of 128 10.2; 8 rows in groups of 128 10.9; 16 rows 13.2; 1 x 2048 x 2048 3.1 us, of which 1.1 are a launch
-// with one load and one store. Clock stamps, 16 rows: 1.6 us until A's loads and the first copies are out, 1.3 for A's way into
-// shared memory, 7.8 the products (16 cells a warp, 234 cycles each and scheduler, 128 of them the tensor pipe's), 0.6 the
-// barrier, 1.1 the sums and 0.7 the last barrier. Four or five slots a warp: 13.3 and 13.6 us.
+// Measured (weights from HBM): 1 x 8192 x 8192 in groups of 32, 42 MB, 11.2 to 11.8 us (3.7 TB/s; 175 instructions a cell of 16
+// rows x 128 columns), of 128 10.2; 8 rows in groups of 128 10.9 to 11.4; 16 rows 13.2 to 13.3; 1 x 2048 x 2048 3.2 us, of which
+// 1.1 are a launch with one load and one store. Clock stamps, 16 rows: 1.6 us until A's loads and the first copies are out, 1.3 for
+// A's way into shared memory, 7.8 the products (16 cells a warp, 234 cycles each and scheduler, 128 of them the tensor pipe's), 0.6
+// the barrier, 1.1 the sums and 0.7 the last barrier. Four or five slots a warp, where three took 13.2: 13.3 and 13.6 us.
 constexpr int kMmThreads = 512, kMmWarps = kMmThreads / 32, kRedStride = 20, kMostBlocks = 4;
 constexpr float kUnit = 0x1p-20f, kUp = 0x1p4f, kPerUnit = 0x1p16f;
 
@@ -474,8 +474,10 @@ qnn_status launch_mm4(Mm4Args a, cudaStream_t st) {
         static std::atomic<int> room[kMostBlocks + 1][64];
         int clusters = room[a.blocks][dev].load(std::memory_order_acquire);
         if (clusters == 0) {
-            if (cudaOccupancyMaxActiveClusters(&clusters, kern, &cfg) != cudaSuccess) cudaGetLastError(), clusters = 0;
-            clusters = std::max(1, clusters);
+            if (cudaOccupancyMaxActiveClusters(&clusters, kern, &cfg) != cudaSuccess || clusters < 1) {
+                cudaGetLastError();
+                clusters = std::max(1, sms / a.blocks);
+            }
             room[a.blocks][dev].store(clusters, std::memory_order_release);
         }
         most = clusters;
