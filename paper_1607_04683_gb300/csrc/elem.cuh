@@ -117,6 +117,25 @@ struct Run {
     }
 };
 
+// Frames of sequence b.
+__device__ __forceinline__ int frames_of(const int32_t *lengths, int64_t b, int64_t T) {
+    if (!lengths) return (int)T;
+    const int n = __ldg(lengths + b);
+    return n < 0 ? 0 : n > T ? (int)T : n;
+}
+
+// i / n and i % n. 64-bit divisions take a hundred instructions; most indices need 32.
+struct Split {
+    int64_t quot, rem;
+};
+__device__ __forceinline__ Split split(int64_t i, int64_t n) {
+    if (((i | n) >> 32) == 0) {
+        const uint32_t q = (uint32_t)i / (uint32_t)n;
+        return {(int64_t)q, (int64_t)((uint32_t)i - q * (uint32_t)n)};
+    }
+    return {i / n, i % n};
+}
+
 // 2^x and 1/x by the hardware: 2 ulp and 1 ulp off at most; results below 2^-126 are 0.
 __device__ __forceinline__ float exp2_hw(float x) {
     float r;

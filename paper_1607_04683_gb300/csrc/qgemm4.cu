@@ -495,7 +495,6 @@ qnn_status launch_mm4(const Mm4Args &a, cudaStream_t st) {
 }
 
 bool aligned16(const void *p) { return (reinterpret_cast<uintptr_t>(p) & 15) == 0; }
-bool aligned4(const void *p) { return (reinterpret_cast<uintptr_t>(p) & 3) == 0; }
 bool group_ok(int g) { return g == 32 || g == 64 || g == 128; }
 
 constexpr int64_t kMostN = INT32_MAX / 2, kMostM = 65535 * 8;  // (grid rows of 8 rows at least)

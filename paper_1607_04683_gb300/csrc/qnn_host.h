@@ -58,6 +58,21 @@ inline bool reach_ok(int64_t count, int64_t stride) {
     return stride >= 0 && (count <= 1 || stride <= ((int64_t)1 << 48) / count) && stride <= (int64_t)1 << 48;
 }
 
+// A [B][T][width] array: its strides are in range, its first element aligned to its type.
+inline bool frames_ok(const void *p, int64_t B, int64_t T, int64_t seq, int64_t frame, int e) {
+    return reach_ok(B, seq) && reach_ok(T, frame) && (reinterpret_cast<uintptr_t>(p) & (e - 1)) == 0;
+}
+// No frame of an output overlaps another: sequences apart and frames apart within one, or the other way round.
+inline bool apart(int64_t B, int64_t T, int64_t width, int64_t seq, int64_t frame) {
+    const bool inner = T <= 1 || frame >= width, outer = B <= 1 || seq >= width;
+    return inner && outer && (B <= 1 || T <= 1 || seq >= (T - 1) * frame + width || frame >= (B - 1) * seq + width);
+}
+inline Span frames_span(const void *p, int64_t B, int64_t T, int64_t width, int64_t seq, int64_t frame, int e) {
+    return T > 0 ? Span(p, ((B - 1) * seq + (T - 1) * frame + width) * e) : Span();
+}
+inline bool aligned4(const void *p) { return (reinterpret_cast<uintptr_t>(p) & 3) == 0; }
+inline bool local_or_null(const void *p) { return !p || is_local_ptr(p); }
+
 inline int dtype_size(int dtype) { return dtype == QNN_F32 ? 4 : 2; }
 inline bool dtype_ok(int dtype) { return dtype == QNN_F32 || dtype == QNN_BF16 || dtype == QNN_F16; }
 

@@ -11,25 +11,6 @@
 namespace qnn {
 namespace {
 
-// Frames of sequence b.
-__device__ __forceinline__ int frames_of(const int32_t *lengths, int64_t b, int64_t T) {
-    if (!lengths) return (int)T;
-    const int n = __ldg(lengths + b);
-    return n < 0 ? 0 : n > T ? (int)T : n;
-}
-
-// i / n and i % n. 64-bit divisions take a hundred instructions; most indices need 32.
-struct Split {
-    int64_t quot, rem;
-};
-__device__ __forceinline__ Split split(int64_t i, int64_t n) {
-    if (((i | n) >> 32) == 0) {
-        const uint32_t q = (uint32_t)i / (uint32_t)n;
-        return {(int64_t)q, (int64_t)((uint32_t)i - q * (uint32_t)n)};
-    }
-    return {i / n, i % n};
-}
-
 // ------------------------------------------------------------------------------------------------
 // Convolution
 // ------------------------------------------------------------------------------------------------
@@ -922,24 +903,9 @@ qnn_status launch_conv(const ConvArgs &a, int W, cudaStream_t st) {
 
 constexpr int64_t kMostCount = (int64_t)1 << 40, kMostFrames = 1 << 30;
 
-// A [B][T][width] array: its strides are in range, its first element aligned to its type.
-bool frames_ok(const void *p, int64_t B, int64_t T, int64_t seq, int64_t frame, int e) {
-    return reach_ok(B, seq) && reach_ok(T, frame) && (reinterpret_cast<uintptr_t>(p) & (e - 1)) == 0;
-}
-// No frame of an output overlaps another: sequences apart and frames apart within one, or the other way round.
-bool apart(int64_t B, int64_t T, int64_t width, int64_t seq, int64_t frame) {
-    const bool inner = T <= 1 || frame >= width, outer = B <= 1 || seq >= width;
-    return inner && outer && (B <= 1 || T <= 1 || seq >= (T - 1) * frame + width || frame >= (B - 1) * seq + width);
-}
-Span frames_span(const void *p, int64_t B, int64_t T, int64_t width, int64_t seq, int64_t frame, int e) {
-    return T > 0 ? Span(p, ((B - 1) * seq + (T - 1) * frame + width) * e) : Span();
-}
 bool sizes_ok(int64_t B, int64_t T, int64_t D) {
     return B >= 0 && T >= 0 && D >= 1 && T <= kMostFrames && D <= INT32_MAX && B <= INT32_MAX && B * D <= kMostCount && reach_ok(T, B * D);
 }
-bool aligned4(const void *p) { return (reinterpret_cast<uintptr_t>(p) & 3) == 0; }
-bool local_or_null(const void *p) { return !p || is_local_ptr(p); }
-
 }  // namespace
 }  // namespace qnn
 
