@@ -412,6 +412,98 @@ typedef struct {
  */
 qnn_status qnn_ssm_scan(const qnn_ssm_args *args, void *stream);
 
+/* Arguments of qnn_linear_attention. Strides in elements: frame t of sequence b at b * seq + t * frame, its heads and their
+ * values contiguous. q, k and v have any number of heads that divides H: head h of the H uses head h / (H / heads) of each. */
+typedef struct {
+    int64_t B, T;     /* sequences, frames */
+    int32_t H;        /* heads of the output and the states */
+    int32_t q_heads, k_heads, v_heads;
+    int32_t dk, dv;   /* 1 .. 256 */
+    int32_t dtype;    /* of q, k, v and y */
+    float scale;
+    const void *q;    /* [B][T][q_heads][dk] */
+    int64_t q_seq, q_frame;
+    const void *k;    /* [B][T][k_heads][dk] */
+    int64_t k_seq, k_frame;
+    const void *v;    /* [B][T][v_heads][dv] */
+    int64_t v_seq, v_frame;
+    void *y;          /* [B][T][H][dv] out */
+    int64_t y_seq, y_frame;
+    const float *log_decay; /* [H] */
+    const float *state_in;  /* [B][H][dk][dv], nullable: zeros */
+    float *state_out;       /* [B][H][dk][dv], nullable; may be state_in */
+    const int32_t *lengths; /* [B], nullable */
+} qnn_linear_args;
+
+/*
+ * qnn_linear_attention — linear attention with a decay for each head, every head h of every sequence with a state S of its own:
+ *   S = exp(min(log_decay[h], 0)) S + k_t v_t^T;  y_t = scale q_t S.
+ * States and sums are fp32. Whole sequences are taken by chunks of frames (and long ones of few sequences in parts whose
+ * states are put together by their decays), a few frames one by one: a prompt and the frames after it may be given in any
+ * division, and one frame of many sequences is the serving form. lengths, frames behind a sequence's end and T = 0 as for
+ * qnn_causal_conv; state_out is the state after each sequence's last frame. A decay above 1 counts as 1, one below exp(-200) as 0.
+ * Inputs that are not finite give outputs that are not (infinities or NaN) from their frame on, in the heads that use them: v in
+ * its own column, k in all of them; q in its own frame only.
+ */
+qnn_status qnn_linear_attention(const qnn_linear_args *args, void *stream);
+
+/* ---------------------------------------------------------------------------------------------
+ * Label-synchronous decoding: selection over beams and classes, the kept beams' states, labels' rows.
+ * ------------------------------------------------------------------------------------------- */
+
+/*
+ * qnn_beam_select — the n best continuations of each of B utterances' K beams over V classes.
+ *   logits   [B * K x V] of `dtype` (ldl >= V), row b * K + k of utterance b's beam k.
+ *   scores   [B][K] fp32: log probabilities of the beams. finished [B][K], nullable: non-zero for beams that have ended.
+ *   A candidate (k, v) has the score scores[k] + logits[k][v] - log(sum_v exp(logits[k][v])); a finished beam has one candidate
+ *   (k, eos) of its own score, its logits are not read. A candidate whose score is minus infinity or not a number is none (a
+ *   class masked by minus infinity, a beam of score minus infinity); a beam with a NaN or plus infinity among its logits, or with
+ *   minus infinity alone, has none.
+ *   scores_out, parents, tokens  [B][n] out, best first: score, beam and class. Of equal scores the lowest beam, then the lowest
+ *   class comes first; a slot without a candidate has score minus infinity, beam 0 and class eos. scores_out may be
+ *   scores if n = K.
+ * Scores are formed and compared in 64 bits and rounded once for scores_out. The sums of exponentials are of fp32 terms, right to
+ * about 2^-26 (each row of a call in the same order, so that equal rows have equal sums): candidates of different beams
+ * that are closer may come in either order. Within a beam the order is that of the logits. 1 <= K, n <= 128; K V < 2^31; 0 <= eos < V.
+ */
+qnn_status qnn_beam_select(const void *logits, int64_t ldl, int dtype, const float *scores, const uint8_t *finished, int64_t B,
+                           int64_t K, int64_t V, int32_t n, int32_t eos, float *scores_out, int32_t *parents, int32_t *tokens,
+                           void *stream);
+
+/* A carried state: in [outer][B * K] rows of row_bytes, out [outer][B * n]. out may be in if n = K; otherwise outputs overlap
+ * nothing. */
+typedef struct {
+    const void *in;
+    void *out;
+    int64_t outer, row_bytes;
+} qnn_beam_state;
+
+/*
+ * qnn_beam_reorder — states of the beams that were kept: row b * n + j of out is row b * K + parents[b][j] of in, for each of
+ * `count` states (a host array, read before the call returns) of any types. parents [B][n] int32, as qnn_beam_select gives them. A
+ * row whose parent is outside 0 .. K - 1 is left as it is and QNN_ERR_INVALID_ARG is recorded. 1 <= K, n <= 128.
+ */
+qnn_status qnn_beam_reorder(const qnn_beam_state *states, int32_t count, const int32_t *parents, int64_t B, int64_t K, int64_t n,
+                            void *stream);
+
+/*
+ * qnn_embedding — rows of a table by label: out[i] = scale table[ids[i]], rounded once to out_dtype.
+ *   ids [n] int32 or int64 (id_bytes 4 or 8); table [V x D] of `dtype` (ldt >= D); out [n x D] (ldo >= D).
+ *   A label below 0 is padding: a row of zeros. One of V or more is that too, and QNN_ERR_INVALID_ARG is recorded.
+ */
+qnn_status qnn_embedding(const void *ids, int id_bytes, int64_t n, const void *table, int64_t ldt, int dtype, int64_t V, int64_t D,
+                         float scale, void *out, int64_t ldo, int out_dtype, void *stream);
+
+/*
+ * qnn_embedding_grad — its gradient: out[r] = scale sum of grad[i] over the i with ids[i] = r (plus out[r] where `add` is not 0), in
+ * fp32, rounded once to out_dtype.
+ *   grad [n x D] of `dtype` (ldg >= D), out [V x D] (ldo >= D). Labels outside 0 .. V - 1 have no part in it.
+ *   The sums are taken in an order that depends on the sizes and labels only (positions sorted by label), so that the same inputs
+ *   give the same bits. Takes scratch of about 16 n + n D / 4 bytes. n <= 2^30.
+ */
+qnn_status qnn_embedding_grad(const void *grad, int64_t ldg, int dtype, const void *ids, int id_bytes, int64_t n, int64_t V,
+                              int64_t D, float scale, int add, void *out, int64_t ldo, int out_dtype, void *stream);
+
 /* ---------------------------------------------------------------------------------------------
  * Kernel timing (diagnostics and benchmarks; no counterpart in the paper).
  * ------------------------------------------------------------------------------------------- */

@@ -77,3 +77,32 @@ class QuantLinear(torch.nn.Module):
 
     def forward(self, x):
         return _QuantizedLinear.apply(x, self.weight, self.bias, self.n_blocks)
+
+
+class _Embedding(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, table, ids, scale, dtype):
+        ctx.save_for_backward(ids)
+        ctx.rows, ctx.scale, ctx.dtype = table.shape[0], scale, table.dtype
+        return qnn.qnn_embedding(ids, table.detach(), scale=scale, dtype=dtype)
+
+    @staticmethod
+    def backward(ctx, gy):
+        ids, = ctx.saved_tensors
+        return qnn.qnn_embedding_grad(gy.contiguous(), ids, ctx.rows, scale=ctx.scale, dtype=ctx.dtype), None, None, None
+
+
+class Embedding(torch.nn.Module):
+    """Labels' rows of a trained table, times scale: the
+    input of layers that take labels, a full-precision layer in Algorithm 1's sense. Labels below 0 are padding: rows of zeros, no
+    gradient. The gradient is dense, its rows summed in an order that depends on the labels only."""
+
+    def __init__(self, rows: int, dim: int, scale: float = 1.0, dtype: torch.dtype = torch.float32, device="cuda"):
+        super().__init__()
+        self.weight = torch.nn.Parameter(torch.empty(rows, dim, dtype=dtype, device=device))
+        self.scale = scale
+        torch.nn.init.normal_(self.weight)
+
+    def forward(self, ids, dtype: torch.dtype | None = None):
+        """ids int32 or int64 of any shape; the result is of the table's type unless `dtype` is given."""
+        return _Embedding.apply(self.weight, ids.contiguous(), self.scale, dtype)

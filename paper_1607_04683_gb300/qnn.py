@@ -37,12 +37,15 @@ EXPORTS = ("qnn_status_string", "qnn_device_status", "qnn_quantize", "qnn_qmatmu
            "qnn_profile_enable", "qnn_profile_read", "qnn_measure_peak", "qnn_quantize_matrix_static",
            "qnn_selftest_s64_to_f32", "qnn_stack_frames", "qnn_selftest_wait_timeout", "qnn_selftest_pair_functions", "qnn_lstm_stream_open",
            "qnn_lstm_stream_push", "qnn_lstm_stream_pull", "qnn_lstm_stream_close", "qnn_measure_exchange_floor",
-           "qnn_rmsnorm_quantize", "qnn_quantize4", "qnn_qmatmul4", "qnn_causal_conv", "qnn_ssm_scan")
+           "qnn_rmsnorm_quantize", "qnn_quantize4", "qnn_qmatmul4", "qnn_causal_conv", "qnn_ssm_scan",
+           "qnn_linear_attention", "qnn_beam_select", "qnn_beam_reorder", "qnn_embedding", "qnn_embedding_grad")
 
 _DTYPES = {}  # qnn_dtype of a torch type
 _MOST_SUMMED = (2 ** 31 - 1) // 255  # values of a row whose codes' sum has 32 bits
 # qnn_ssm_args as it lies in memory
 _SSM_ARGS = struct.Struct("=3q4i" + 6 * "Q2q" + "6Q")
+# qnn_linear_args
+_LINEAR_ARGS = struct.Struct("=2q7if" + 4 * "Q2q" + "4Q")
 
 
 class QnnError(RuntimeError):
@@ -135,6 +138,16 @@ def lib():
         L.qnn_causal_conv.restype = i32
         L.qnn_ssm_scan.argtypes = [P, P]
         L.qnn_ssm_scan.restype = i32
+        L.qnn_linear_attention.argtypes = [P, P]
+        L.qnn_linear_attention.restype = i32
+        L.qnn_beam_select.argtypes = [P, i64, i32, P, P, i64, i64, i64, C.c_int32, C.c_int32, P, P, P, P]
+        L.qnn_beam_select.restype = i32
+        L.qnn_beam_reorder.argtypes = [P, C.c_int32, P, i64, i64, i64, P]
+        L.qnn_beam_reorder.restype = i32
+        L.qnn_embedding.argtypes = [P, i32, i64, P, i64, i32, i64, i64, C.c_float, P, i64, i32, P]
+        L.qnn_embedding.restype = i32
+        L.qnn_embedding_grad.argtypes = [P, i64, i32, P, i32, i64, i64, i64, C.c_float, i32, P, i64, i32, P]
+        L.qnn_embedding_grad.restype = i32
         _lib = L
     return _lib
 
@@ -321,6 +334,9 @@ def _frames(t, what: str, dtype, shape):
     if t.dtype is not dtype or t.shape != shape:
         _bad(what + ":", dtype, shape)
     st = t.stride()
+    if not t.numel():  # (the strides of nothing are anything)
+        width = shape[2] if len(shape) == 3 else shape[2] * shape[3]
+        return t.data_ptr(), max(shape[1], 1) * width, width
     if (st[-1] != 1 and shape[-1] > 1) or (len(st) == 4 and st[2] != shape[3] and shape[2] > 1):
         _bad(what + ": frames of contiguous values")
     return t.data_ptr(), st[0], st[1]
@@ -507,6 +523,170 @@ def qnn_ssm_scan(u, dt, A, B, C, D=None, z=None, dt_bias=None, softplus=True, st
     if st:
         _check(st, "qnn_ssm_scan")
     return y
+
+
+def qnn_linear_attention(q, k, v, log_decay, scale=None, state_in=None, state_out=None, lengths=None, out=None, stream=None):
+    """Linear attention with a decay for each head: q [B, T, heads, dk], k [B, T, heads, dk] and v [B, T, heads, dv] (fp32, bf16
+    or fp16, all of one type; frames may be slices of wider ones), log_decay [H] fp32 (above 0 counts as 0), where each has a number
+    of heads that divides H; states [B, H, dk, dv] fp32 (state_out may be state_in), lengths int32 [B]; scale is 1 / sqrt(dk)
+    unless given. Returns out, [B, T, H, dv]; without an out given, the frames behind a sequence's end hold nothing in
+    particular."""
+    torch, L = _libs()
+    if q.dim() != 4 or k.dim() != 4 or v.dim() != 4 or log_decay.dim() != 1 or not q.is_cuda:
+        _bad("q, k, v: CUDA [B, T, heads, d]; log_decay: [H]")
+    ty, f32, kind = q.dtype, torch.float32, _dtype(q, "q")
+    B, T, hq, dk = q.shape
+    hk, (hv, dv), H = k.shape[2], v.shape[2:], log_decay.shape[0]
+    y = out if out is not None else _result(torch, (B, T, H, dv), ty, q, stream)
+    state = (B, H, dk, dv)
+    args = _LINEAR_ARGS.pack(B, T, H, hq, hk, hv, dk, dv, kind, dk ** -0.5 if scale is None else scale,
+                             *_frames(q, "q", ty, (B, T, hq, dk)), *_frames(k, "k", ty, (B, T, hk, dk)),
+                             *_frames(v, "v", ty, (B, T, hv, dv)), *_frames(y, "out", ty, (B, T, H, dv)),
+                             _flat(log_decay, "log_decay", f32, (H,)), _flat(state_in, "state_in", f32, state),
+                             _flat(state_out, "state_out", f32, state), _flat(lengths, "lengths", torch.int32, (B,)))
+    if stream is not None:
+        _used(stream, q, k, v, log_decay, state_in, state_out, lengths, out)
+    st = L.qnn_linear_attention(args, _here(torch) if stream is None else stream.cuda_stream)
+    if st:
+        _check(st, "qnn_linear_attention")
+    return y
+
+
+def qnn_beam_select(logits, scores, n=None, finished=None, eos=0, stream=None):
+    """The n best continuations of each utterance's beams: logits [B, K, V] (fp32, bf16 or fp16; rows equally far apart), scores
+    fp32 [B, K], finished bool or uint8 [B, K]; n is K unless given. A candidate's score is its beam's plus the class's log
+    softmax, a finished beam has its own with class eos only; ties go to the lowest beam, then class. Returns (scores fp32, parents
+    int32, tokens int32), each [B, n], best first; slots without a candidate hold (-inf, 0, eos)."""
+    torch, L = _libs()
+    if logits.dim() != 3 or not logits.is_cuda:
+        _bad("logits: CUDA [B, K, V]")
+    B, K, V = shape = logits.shape
+    dt = _dtype(logits, "logits")
+    s0, s1, s2 = logits.stride()
+    if K == 1:
+        s1 = s0 if B > 1 else V
+    if (s2 != 1 and V > 1) or (B > 1 and s0 != K * s1) or (s1 < V and B * K > 1):
+        _bad("logits: rows of contiguous values, equally far apart", shape)
+    n = K if n is None else n
+    ended = 0
+    if finished is not None:
+        ended = _flat(finished, "finished", torch.uint8 if finished.dtype is torch.uint8 else torch.bool, (B, K))
+    score = _flat(scores, "scores", torch.float32, (B, K))
+    best = _result(torch, (B, n), torch.float32, logits, stream)
+    parents = _result(torch, (B, n), torch.int32, logits, stream)
+    tokens = _result(torch, (B, n), torch.int32, logits, stream)
+    if stream is not None:
+        _used(stream, logits, scores, finished)
+    st = L.qnn_beam_select(logits.data_ptr(), max(s1, V), dt, score, ended, B, K, V, n, eos, best.data_ptr(), parents.data_ptr(),
+                           tokens.data_ptr(), _here(torch) if stream is None else stream.cuda_stream)
+    if st:
+        _check(st, "qnn_beam_select")
+    return best, parents, tokens
+
+
+def qnn_beam_reorder(states, parents, dims=None, out=None, stream=None):
+    """States of the beams that were kept: each of the contiguous tensors `states` (of any type) has B * K rows in dimension 0, or
+    the one `dims` names; row b * n + j of the result is its row b * K + parents[b, j], parents int32 [B, n]. `out`: a list of as many
+    tensors, each of which may be the state itself (n = K); new ones unless given. Returns the list."""
+    torch, L = _libs()
+    if parents.dim() != 2 or not parents.is_cuda:
+        _bad("parents: CUDA [B, n]")
+    B, n = parents.shape
+    kept = _flat(parents, "parents", torch.int32, (B, n))
+    count = len(states)
+    if (dims is not None and len(dims) != count) or (out is not None and len(out) != count):
+        _bad("dims and out: as many as states")
+    K, results, args = 1, [], []
+    for i, s in enumerate(states):
+        d = 0 if dims is None else dims[i]
+        shape = s.shape
+        if not s.is_cuda or not s.is_contiguous() or not 0 <= d < len(shape) or (B and shape[d] % B):
+            _bad("states: contiguous CUDA tensors of B * K rows", shape)
+        rows = shape[d] // B if B else K
+        if i and rows != K:
+            _bad("states: as many beams each", shape)
+        K = rows
+        o = _result(torch, (*shape[:d], B * n, *shape[d + 1:]), s.dtype, s, stream) if out is None else out[i]
+        if o.dtype is not s.dtype or o.shape != (*shape[:d], B * n, *shape[d + 1:]) or not o.is_contiguous():
+            _bad("out: contiguous tensors of the states' types and B * n rows", tuple(o.shape))
+        results.append(o)
+        outer = 1
+        for v in shape[:d]:
+            outer *= v
+        row = s.element_size()
+        for v in shape[d + 1:]:
+            row *= v
+        args += [s.data_ptr(), o.data_ptr(), outer, row]
+    if stream is not None:
+        _used(stream, parents, *states, *results)
+    st = L.qnn_beam_reorder(struct.pack("=" + count * "2Q2q", *args), count, kept, B, K, n,
+                            _here(torch) if stream is None else stream.cuda_stream)
+    if st:
+        _check(st, "qnn_beam_reorder")
+    return results
+
+
+def _ids(torch, ids) -> int:
+    """Bytes of a label."""
+    if ids.dtype is not torch.int32 and ids.dtype is not torch.int64 or not ids.is_contiguous():
+        _bad("ids: contiguous int32 or int64")
+    return 4 if ids.dtype is torch.int32 else 8
+
+
+def _by_label(t, what: str, dtype, lead, D: int) -> int:
+    """Leading dimension of [*lead, D] values: rows apart where lead is one dimension, contiguous otherwise."""
+    if len(lead) == 1:
+        return _rows(t, what, dtype, (*lead, D))
+    _flat(t, what, dtype, (*lead, D))
+    return D
+
+
+def qnn_embedding(ids, table, scale: float = 1.0, dtype=None, out=None, stream=None):
+    """Rows of table [V, D] (fp32, bf16 or fp16) by label, times scale: ids CUDA int32 or int64 of any shape, labels below 0 give
+    zeros. Returns out, [*ids.shape, D] of `dtype` (the table's unless given)."""
+    torch, L = _libs()
+    if table.dim() != 2 or not table.is_cuda or not ids.is_cuda:
+        _bad("ids and table: CUDA tensors, the table a matrix")
+    V, D = table.shape
+    ty = out.dtype if out is not None else table.dtype if dtype is None else dtype
+    if dtype is not None and ty is not dtype:
+        _bad("out:", dtype)
+    lead, size = tuple(ids.shape), _ids(torch, ids)
+    y = out if out is not None else _result(torch, (*lead, D), ty, table, stream)
+    ldt, ldo = _rows(table, "table", table.dtype, (V, D)), _by_label(y, "out", ty, lead, D)
+    if stream is not None:
+        _used(stream, ids, table, out)
+    st = L.qnn_embedding(ids.data_ptr(), size, ids.numel(), table.data_ptr(), ldt, _dtype(table, "table"), V, D, scale, y.data_ptr(),
+                         ldo, _dtype(y, "out"), _here(torch) if stream is None else stream.cuda_stream)
+    if st:
+        _check(st, "qnn_embedding")
+    return y
+
+
+def qnn_embedding_grad(grad, ids, rows: int, scale: float = 1.0, dtype=None, out=None, accumulate: bool = False, stream=None):
+    """Gradient of qnn_embedding for its table of `rows` rows: grad [*ids.shape, D] (fp32, bf16 or fp16). Returns out, [rows, D] of
+    `dtype` (fp32 unless given), to which the gradient is added if accumulate. The same inputs give the same bits."""
+    torch, L = _libs()
+    lead = tuple(ids.shape)
+    if grad.dim() != len(lead) + 1 or not grad.is_cuda or not ids.is_cuda:
+        _bad("grad: CUDA [*ids.shape, D]")
+    D, size = grad.shape[-1], _ids(torch, ids)
+    ldg = _by_label(grad, "grad", grad.dtype, lead, D)
+    ty = out.dtype if out is not None else torch.float32 if dtype is None else dtype
+    if dtype is not None and ty is not dtype:
+        _bad("out:", dtype)
+    if accumulate and out is None:
+        _bad("accumulate: needs an out")
+    G = out if out is not None else _result(torch, (rows, D), ty, grad, stream)
+    ldo = _rows(G, "out", ty, (rows, D))
+    if stream is not None:
+        _used(stream, grad, ids, out)
+    st = L.qnn_embedding_grad(grad.data_ptr(), ldg, _dtype(grad, "grad"), ids.data_ptr(), size, ids.numel(), rows, D, scale,
+                              1 if accumulate else 0, G.data_ptr(), ldo, _dtype(G, "out"),
+                              _here(torch) if stream is None else stream.cuda_stream)
+    if st:
+        _check(st, "qnn_embedding_grad")
+    return G
 
 
 def lstm_desc(num_layers, input_dim, hidden, proj=0, num_classes=0, output_mode=None, stack=0,
