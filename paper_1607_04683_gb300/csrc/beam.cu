@@ -19,7 +19,7 @@ constexpr int kMostKept = 128, kMostBeams = 128;
 // A candidate: larger ones first, 0 none. The value in an order-preserving form, above it the index's complement, so that
 // of equal values the lowest index is the largest candidate and no two are equal.
 using Logit = unsigned long long;  // 32 bits of a logit, 32 of ~index
-struct Cand {                      // a score in 64 bits
+struct Cand {                      // a score in two fp32 terms, 32 bits each
     unsigned long long v;
     unsigned index;
 };
@@ -29,69 +29,98 @@ __device__ __forceinline__ bool some(Logit a) { return a != 0; }
 __device__ __forceinline__ bool some(const Cand &a) { return a.v != 0; }
 __device__ __forceinline__ Logit none_of(Logit) { return 0; }
 __device__ __forceinline__ Cand none_of(Cand) { return {0, 0xffffffffu}; }
+__device__ __forceinline__ Logit from_lane(Logit a, int lane) { return __shfl_sync(0xffffffffu, a, lane); }
+__device__ __forceinline__ Cand from_lane(const Cand &a, int lane) {
+    return {__shfl_sync(0xffffffffu, a.v, lane), __shfl_sync(0xffffffffu, a.index, lane)};
+}
+__device__ __forceinline__ Logit across(Logit a, int mask) { return __shfl_xor_sync(0xffffffffu, a, mask); }
+__device__ __forceinline__ Cand across(const Cand &a, int mask) {
+    return {__shfl_xor_sync(0xffffffffu, a.v, mask), __shfl_xor_sync(0xffffffffu, a.index, mask)};
+}
 
-__device__ __forceinline__ Logit logit_key(float v, unsigned index) {
+__device__ __forceinline__ uint32_t ordered(float v) {
     const uint32_t b = __float_as_uint(__fadd_rn(v, 0.0f));  // (-0 is 0)
-    const uint32_t o = b ^ ((int32_t)b < 0 ? 0xffffffffu : 0x80000000u);
-    return v > -INFINITY ? (Logit)o << 32 | (uint32_t)~index : 0;  // (a NaN is none either)
+    return b ^ ((int32_t)b < 0 ? 0xffffffffu : 0x80000000u);
 }
-__device__ __forceinline__ float logit_of(Logit k) {
-    const uint32_t o = (uint32_t)(k >> 32);
-    return __uint_as_float(o ^ ((int32_t)o < 0 ? 0x80000000u : 0xffffffffu));
-}
-__device__ __forceinline__ Cand cand_key(double v, unsigned index) {
-    if (!(v > -INFINITY)) return none_of(Cand());
-    const unsigned long long b = (unsigned long long)__double_as_longlong(v + 0.0);
-    return {b ^ ((long long)b < 0 ? ~0ull : 1ull << 63), index};
-}
-__device__ __forceinline__ double cand_of(const Cand &c) {
-    return __longlong_as_double((long long)(c.v ^ ((long long)c.v < 0 ? 1ull << 63 : ~0ull)));
+__device__ __forceinline__ float unordered(uint32_t o) { return __uint_as_float(o ^ ((int32_t)o < 0 ? 0x80000000u : 0xffffffffu)); }
+__device__ __forceinline__ Logit logit_key(float v, unsigned index) {
+    return v > -INFINITY ? (Logit)ordered(v) << 32 | (uint32_t)~index : 0;  // (a NaN is none either)
 }
 
-// The n best candidates so far, best first. A block of kThreads threads brings kEach candidates a thread at a time. Only those
-// better than the n-th best so far count, and where more than n threads have one, those no worse than the n-th best of the
-// threads' bests: n threads at most, so that n kEach + n are ever ranked. A candidate's rank is the number of better ones,
-// counted by one thread: no order of arrival shows in the result.
-constexpr int kThreads = 256, kEach = 8;
-template <typename K>
+// A value as the sum of two fp32 terms, hi the sum rounded: 48 bits or so. (This part's units for 64 bits are few: a logarithm and
+// some sums in 64 bits took a block 15 us.)
+struct Two {
+    float hi, lo;
+};
+__device__ __forceinline__ Two two_sum(float a, float b) {
+    const float s = __fadd_rn(a, b), t = __fsub_rn(s, a);
+    return {s, __fadd_rn(__fsub_rn(a, __fsub_rn(s, t)), __fsub_rn(b, t))};
+}
+__device__ __forceinline__ Two add(Two a, Two b) {
+    Two s = two_sum(a.hi, b.hi);
+    s.lo = __fadd_rn(s.lo, __fadd_rn(a.lo, b.lo));
+    return two_sum(s.hi, s.lo);
+}
+__device__ __forceinline__ Two mul(Two a, Two b) {
+    const float p = __fmul_rn(a.hi, b.hi), e = __fmaf_rn(a.hi, b.hi, -p);
+    return two_sum(p, __fmaf_rn(a.hi, b.lo, __fmaf_rn(a.lo, b.hi, e)));
+}
+// ln 2 in parts of 15 bits (whose product with an exponent is exact), 24, and the rest.
+constexpr float kLn2Head = 0.693145751953125f, kLn2Mid = 1.428606765330187e-06f, kLn2Rest = 5.497923e-14f;
+// exp(x), |x| <= 80, to about 2^-40: x = n ln 2 + 8 r, exp(r) - 1 = r + r^2 / 2 + r^3 / 6 + ... (the first two terms in two fp32 terms
+// each; r^3 <= 10^-4), its square taken three times by p -> 2 p + p^2.
+__device__ __forceinline__ Two exp_two(Two x) {
+    const float n = rintf(__fmul_rn(x.hi, kLog2e));
+    Two r = two_sum(__fmaf_rn(-n, kLn2Head, x.hi), __fmul_rn(-n, kLn2Mid));
+    r.lo = __fadd_rn(r.lo, __fadd_rn(__fmaf_rn(-n, kLn2Mid, -__fmul_rn(-n, kLn2Mid)), __fmaf_rn(-n, kLn2Rest, x.lo)));
+    r = two_sum(__fmul_rn(r.hi, 0.125f), __fmul_rn(r.lo, 0.125f));
+    const Two q = mul(r, r);
+    float c = __fmaf_rn(r.hi, 1.0f / 720, 1.0f / 120);
+    c = __fmaf_rn(c, r.hi, 1.0f / 24);
+    c = __fmaf_rn(c, r.hi, 1.0f / 6);
+    Two p = add(r, {__fmul_rn(q.hi, 0.5f), __fmaf_rn(__fmul_rn(q.hi, r.hi), c, __fmul_rn(q.lo, 0.5f))});
+#pragma unroll
+    for (int i = 0; i < 3; ++i) p = add({__fmul_rn(2.0f, p.hi), __fmul_rn(2.0f, p.lo)}, mul(p, p));
+    p = add({1.0f, 0.0f}, p);
+    const float scale = __int_as_float((int)(n + 127.0f) << 23);
+    return {__fmul_rn(p.hi, scale), __fmul_rn(p.lo, scale)};
+}
+// log(x), 2^-10 <= x < 2^64, to about 2^-40: a first value in fp32, and the logarithm of what x exp(-value) is off 1.
+__device__ __forceinline__ Two log_two(Two x) {
+    const float y = logf(x.hi);
+    const Two e = exp_two({-y, 0.0f});
+    const Two d = add(mul(x, e), {-1.0f, 0.0f});
+    return two_sum(y, __fmaf_rn(__fmul_rn(-0.5f, d.hi), d.hi, __fadd_rn(d.hi, d.lo)));
+}
+// score + (logit - lse), none where that is minus infinity or not a number.
+__device__ __forceinline__ Cand cand_key(float score, float logit, Two lse, unsigned index) {
+    const Two a = two_sum(logit, -lse.hi), b = two_sum(score, a.hi);
+    Two s = two_sum(b.hi, __fadd_rn(b.lo, __fsub_rn(a.lo, lse.lo)));
+    if (!(fabsf(b.hi) < INFINITY)) s = {b.hi, 0.0f};
+    if (!(s.hi > -INFINITY)) return none_of(Cand());
+    return {(unsigned long long)ordered(s.hi) << 32 | ordered(s.lo), index};
+}
+
+// The n best candidates so far, best first. A block of kThreads threads brings EACH candidates a thread at a time. Only those
+// better than the n-th best so far count, and of them those no worse than the n-th best of the bests of G groups of threads, G >= 2 n:
+// of candidates in no order 1.4 n at most are expected, n groups' at worst. A candidate's rank is the number of better
+// ones, counted by one thread: no order of arrival shows in the result.
+constexpr int kThreads = 256, kWarps = kThreads / 32;
+template <typename K, int EACH>
 struct Best {
-    K list[kMostKept * (kEach + 1)];
+    static constexpr int kMost = kThreads * EACH / 2 + kMostKept;
+    K list[kMost];
     K ranked[kMostKept];
     K bests[kThreads];
     K last;  // the n-th best, or none
-    K least;
-    int count, held;
+    int count, held, wanted;
 
     __device__ __forceinline__ void start() {
         if (threadIdx.x == 0) count = 0, held = 0, last = none_of(K());
         __syncthreads();
     }
-    // mine: the best of key[]. All threads call it; ends behind a barrier.
-    __device__ __forceinline__ void take(const K (&key)[kEach], const K &mine, int n) {
-        const K bar = last;
-        const bool pass = before(mine, bar);
-        const int threads = __syncthreads_count(pass);
-        if (threads == 0) return;
-        K from = bar;
-        bool with = false;  // `from` itself counts
-        if (threads > n) {
-            bests[threadIdx.x] = pass ? mine : none_of(K());
-            __syncthreads();
-            if (pass) {
-                int better = 0;
-#pragma unroll 8
-                for (int i = 0; i < kThreads; ++i) better += before(bests[i], mine);
-                if (better == n - 1) least = mine;
-            }
-            __syncthreads();
-            from = least, with = true;
-        }
-        if (pass && (with ? !before(from, mine) : true)) {
-#pragma unroll
-            for (int e = 0; e < kEach; ++e)
-                if (some(key[e]) && (with ? !before(from, key[e]) : before(key[e], from))) list[atomicAdd(&count, 1)] = key[e];
-        }
-        __syncthreads();
+    // What is in list[0 .. count), ranked: the best n of it, in order. Ends behind a barrier.
+    __device__ __forceinline__ void rank(int n) {
         const int m = count;
         for (int i = threadIdx.x; i < m; i += kThreads) {
             const K k = list[i];
@@ -108,6 +137,40 @@ struct Best {
             if (h == n) last = ranked[n - 1];
         }
         __syncthreads();
+    }
+    // key(e), e < EACH: the thread's candidates, mine the best of them. All threads call it; ends behind a barrier.
+    template <typename F>
+    __device__ __forceinline__ void take(F key, K mine, int n) {
+        const K bar = last;
+        if (!before(mine, bar)) mine = none_of(K());
+        if (__syncthreads_or(some(mine)) == 0) return;
+        // the groups' bests, and of them the n-th: every warp for itself
+        const int lane = threadIdx.x % 32, groups = n <= 16 ? 32 : n <= 32 ? 64 : n <= 64 ? 128 : 256, size = kThreads / groups;
+        K top = mine;
+        for (int m = 1; m < size; m <<= 1) {
+            const K other = across(top, m);
+            if (before(other, top)) top = other;
+        }
+        if (threadIdx.x % size == 0) bests[threadIdx.x / size] = top;
+        __syncthreads();
+        K from = none_of(K());
+        for (int i = lane; i < groups; i += 32) {
+            const K k = bests[i];
+            int better = 0;
+#pragma unroll 8
+            for (int j = 0; j < groups; ++j) better += before(bests[j], k);
+            const unsigned hit = __ballot_sync(0xffffffffu, some(k) && better == n - 1);
+            if (hit) from = from_lane(k, __ffs(hit) - 1);
+        }
+        if (some(mine) && !before(from, mine)) {
+#pragma unroll
+            for (int e = 0; e < EACH; ++e) {
+                const K k = key(e);
+                if (before(k, bar) && !before(from, k)) list[atomicAdd(&count, 1)] = k;
+            }
+        }
+        __syncthreads();
+        rank(n);
     }
 };
 
@@ -142,63 +205,125 @@ struct SelectArgs {
 constexpr float kLog2eRest = 1.925963033500e-08f, kBias = 2e-8f;
 __device__ __forceinline__ float exp_term(float d) { return exp2_hw(__fmaf_rn(d, kLog2eRest, __fmaf_rn(d, kLog2e, kBias))); }
 
-template <typename T, bool VEC>
-__device__ __forceinline__ void load_tile(const T *row, int64_t base, int64_t end, float (&v)[kEach]) {
-    if constexpr (VEC) {
-        const int64_t at = base + (int64_t)threadIdx.x * kEach;
-        Run<T, kEach> r;
-        if (at + kEach <= end) {
-            r.load(row + at);
-        } else {
-            r.load_some(row + at, at < end ? (int)(end - at) : 0);
-        }
+// A tile of a row: with VEC runs of eight values a thread, else neighbouring values by neighbouring threads.
+constexpr int kRun = 8;
+template <bool VEC>
+__device__ __forceinline__ int64_t place(int64_t base, int e) {
+    return base + (VEC ? (e / kRun * kThreads + (int)threadIdx.x) * kRun + e % kRun : e * kThreads + (int)threadIdx.x);
+}
+template <typename T, bool VEC, int EACH>
+__device__ __forceinline__ void load_tile(const T *row, int64_t base, int64_t end, float (&v)[EACH]) {
+    if (base + kThreads * EACH <= end) {  // whole
+        if constexpr (VEC) {
 #pragma unroll
-        for (int e = 0; e < kEach; ++e) v[e] = at + e < end ? r.get(e) : -INFINITY;
+            for (int r = 0; r < EACH / kRun; ++r) {
+                Run<T, kRun> x;
+                x.load(row + place<VEC>(base, r * kRun));
+#pragma unroll
+                for (int e = 0; e < kRun; ++e) v[r * kRun + e] = x.get(e);
+            }
+        } else {
+#pragma unroll
+            for (int e = 0; e < EACH; ++e) v[e] = to_f32(row[place<VEC>(base, e)]);
+        }
+    } else if constexpr (VEC) {
+#pragma unroll
+        for (int r = 0; r < EACH / kRun; ++r) {
+            const int64_t at = place<VEC>(base, r * kRun);
+            Run<T, kRun> x;
+            if (at + kRun <= end) x.load(row + at);
+            else x.load_some(row + at, at < end ? (int)(end - at) : 0);
+#pragma unroll
+            for (int e = 0; e < kRun; ++e) v[r * kRun + e] = at + e < end ? x.get(e) : -INFINITY;
+        }
     } else {
 #pragma unroll
-        for (int e = 0; e < kEach; ++e) {
-            const int64_t at = base + threadIdx.x + (int64_t)e * kThreads;
+        for (int e = 0; e < EACH; ++e) {
+            const int64_t at = place<VEC>(base, e);
             v[e] = at < end ? to_f32(row[at]) : -INFINITY;
         }
     }
 }
 
-// One part of a beam's row: its sum of exponentials and its n best classes in one pass over it, each thread's running maximum
-// and sum in registers. Within a beam the order of the logits is that of the scores, so that no score is formed here.
-template <typename T, bool VEC>
-__global__ void __launch_bounds__(kThreads) beam_rows_kernel(const SelectArgs a) {
-    __shared__ Best<Logit> best;
-    __shared__ float warp_most[kThreads / 32];
-    __shared__ unsigned long long warp_sum[kThreads / 32];
+// Best::take for a tile of a row, by values alone: candidates are those no less than the n-th best of the groups' largest values (and
+// above the n-th best so far, which comes from lower classes). False, with nothing taken, where so many are equal to it that
+// they need to be told apart by their classes first. One 32-bit comparison a value instead of keys of 64: 128 x 8 x 8192
+// bf16 11 us less.
+constexpr int kFewCands = 512;
+template <bool VEC, int EACH>
+__device__ __forceinline__ bool take_values(Best<Logit, EACH> &s, const float (&v)[EACH], float top, int64_t base, int n) {
+    const float bar = s.held == n ? unordered((uint32_t)(s.last >> 32)) : -INFINITY;
+    const bool pass = top > bar;
+    if (__syncthreads_or(pass) == 0) return true;
+    const int lane = threadIdx.x % 32, groups = n <= 16 ? 32 : n <= 32 ? 64 : n <= 64 ? 128 : 256, size = kThreads / groups;
+    float most = pass ? top : -INFINITY;
+    for (int m = 1; m < size; m <<= 1) most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, m));
+    float *bests = reinterpret_cast<float *>(s.bests);
+    if (threadIdx.x % size == 0) bests[threadIdx.x / size] = most;
+    if (threadIdx.x == 0) s.wanted = s.held;
+    __syncthreads();
+    float from = -INFINITY;  // the n-th largest, if there are as many
+    for (int i = lane; i < groups; i += 32) {
+        const float mine = bests[i];
+        int better = 0;
+#pragma unroll 8
+        for (int j = 0; j < groups; ++j) better += bests[j] > mine;
+        // (of equal ones all have the same count: the n-th has less than n better ones, and n or more with its equals)
+        float least = better < n ? mine : INFINITY;
+#pragma unroll
+        for (int o = 16; o > 0; o >>= 1) least = fminf(least, __shfl_xor_sync(0xffffffffu, least, o));
+        from = i == lane ? least : fminf(from, least);
+    }
+    int mine = 0;
+    if (pass && top >= from)
+#pragma unroll
+        for (int e = 0; e < EACH; ++e) mine += v[e] >= from && v[e] > bar;
+    int at = 0;
+    if (mine) at = atomicAdd(&s.wanted, mine);
+    __syncthreads();
+    if (s.wanted > kFewCands) return false;
+    if (mine)
+#pragma unroll
+        for (int e = 0; e < EACH; ++e)
+            if (v[e] >= from && v[e] > bar) s.list[at++] = logit_key(v[e], (unsigned)place<VEC>(base, e));
+    if (threadIdx.x == 0) s.count = s.wanted;
+    __syncthreads();
+    s.rank(n);
+    return true;
+}
+
+// One part of a beam's row: its sum of exponentials and its n best classes in one pass over it, tiles of kThreads EACH values
+// in registers. Within a beam the order of the logits is that of the scores, so that no score is formed here.
+template <typename T, bool VEC, int EACH>
+__global__ void __launch_bounds__(kThreads, EACH == 8 ? 4 : 3) beam_rows_kernel(const SelectArgs a) {
+    __shared__ Best<Logit, EACH> best;
+    __shared__ float warp_most[kWarps];
+    __shared__ unsigned long long warp_sum[kWarps];
     const int64_t row = blockIdx.x / (unsigned)a.parts;
     const int part = blockIdx.x % (unsigned)a.parts;
-    RowPart *out = a.parts_of + row * a.parts + part;
-    const float score = a.scores[row];
-    if ((a.finished && a.finished[row]) || !(score > -INFINITY)) return;  // (nothing of this row is looked at)
     const T *x = static_cast<const T *>(a.logits) + row * a.ldl;
     const int64_t lo = part * a.per, hi = lo + a.per < a.V ? lo + a.per : a.V;
-    float v[kEach], most = -INFINITY, sum = 0.0f;
-    load_tile<T, VEC>(x, lo, hi, v);
+    float v[EACH], most = -INFINITY, sum = 0.0f;
+    const float score = a.scores[row];
+    if ((a.finished && a.finished[row]) || !(score > -INFINITY)) return;  // (nothing of this row is looked at)
+    load_tile<T, VEC, EACH>(x, lo, hi, v);
     best.start();
-    for (int64_t base = lo; base < hi; base += kThreads * kEach) {
-        float next[kEach];
-        if (base + kThreads * kEach < hi) load_tile<T, VEC>(x, base + kThreads * kEach, hi, next);
+    for (int64_t base = lo; base < hi; base += kThreads * EACH) {
+        if (base > lo) load_tile<T, VEC, EACH>(x, base, hi, v);
         float top = v[0];
 #pragma unroll
-        for (int e = 1; e < kEach; ++e) top = fmaxf(top, v[e]);
+        for (int e = 1; e < EACH; ++e) top = fmaxf(top, v[e]);
         if (top > most) sum = __fmul_rn(sum, exp_term(__fsub_rn(most, top))), most = top;
         const float from = most > -INFINITY ? most : 0.0f;
 #pragma unroll
-        for (int e = 0; e < kEach; ++e) sum = __fadd_rn(sum, exp_term(__fsub_rn(v[e], from)));
-        Logit key[kEach], mine = 0;
+        for (int e = 0; e < EACH; ++e) sum = __fadd_rn(sum, exp_term(__fsub_rn(v[e], from)));
+        if (!take_values<VEC, EACH>(best, v, top, base, a.n)) {
+            unsigned first = 0;
 #pragma unroll
-        for (int e = 0; e < kEach; ++e) {
-            key[e] = logit_key(v[e], (unsigned)(VEC ? base + threadIdx.x * kEach + e : base + threadIdx.x + e * kThreads));
-            mine = key[e] > mine ? key[e] : mine;
+            for (int e = EACH - 1; e >= 0; --e)
+                if (v[e] == top) first = (unsigned)place<VEC>(base, e);
+            best.take([&](int e) { return logit_key(v[e], (unsigned)place<VEC>(base, e)); }, logit_key(top, first), a.n);
         }
-        best.take(key, mine, a.n);
-#pragma unroll
-        for (int e = 0; e < kEach; ++e) v[e] = next[e];
     }
     // the block's maximum, then the sums' parts of it
     const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
@@ -207,7 +332,7 @@ __global__ void __launch_bounds__(kThreads) beam_rows_kernel(const SelectArgs a)
     __syncthreads();
     m = warp_most[0];
 #pragma unroll
-    for (int i = 1; i < kThreads / 32; ++i) m = fmaxf(m, warp_most[i]);
+    for (int i = 1; i < kWarps; ++i) m = fmaxf(m, warp_most[i]);
     const float share = most > -INFINITY ? __fmul_rn(sum, exp_term(__fsub_rn(most, m))) : sum;  // (NaNs pass through)
     const bool bad = !(share >= 0.0f && share < INFINITY);
     unsigned long long s = bad ? 0 : __float2ull_rn(__fmul_rn(share, 4294967296.0f));
@@ -220,41 +345,64 @@ __global__ void __launch_bounds__(kThreads) beam_rows_kernel(const SelectArgs a)
     for (int i = threadIdx.x; i < held; i += kThreads) keys[i] = best.list[i];
     if (threadIdx.x == 0) {
         s = 0;
-        for (int i = 0; i < kThreads / 32; ++i) s += warp_sum[i];
-        *out = {any_bad ? ~0ull : s, m, held};
+        for (int i = 0; i < kWarps; ++i) s += warp_sum[i];
+        a.parts_of[row * a.parts + part] = {any_bad ? ~0ull : s, m, held};
     }
-    grid_dependents_launch();
 }
 
-// A batch row's continuations: each beam's log of its sum in 64 bits from its parts, then the n best of the parts' lists.
+// A batch row's continuations: each beam's log of its sum from its parts, then the n best of the parts' lists.
+// EACH: 1 while a block's threads hold all candidates one each (code that is not in a cache yet is most of a short kernel's time), else 8.
+template <int EACH>
 __global__ void __launch_bounds__(kThreads) beam_merge_kernel(const SelectArgs a) {
-    __shared__ Best<Cand> best;
-    __shared__ double lse[kMostBeams];
+    __shared__ Best<Cand, EACH> best;
+    __shared__ Two lse[kMostBeams];
     __shared__ unsigned char state[kMostBeams];  // 0: no candidates, 1: its parts' lists, 2: finished
     __shared__ float score[kMostBeams];
     const int64_t b = blockIdx.x;
     const int K = (int)a.K;
+    const int64_t total = (int64_t)K * a.parts * a.n;
+    // a candidate's beam, and its logit where its list has one (whatever is in memory for a row that nothing was looked for in)
+    auto candidate = [&](int64_t at, int &k, Logit &logit) {
+        const unsigned list = (unsigned)at / (unsigned)a.n, i = (unsigned)at % (unsigned)a.n;
+        k = (int)(list / (unsigned)a.parts);
+        const int64_t of = b * K * a.parts + list;
+        const int held = a.parts_of[of].held;
+        logit = a.keys[of * a.n + i];
+        if ((int)i >= held) logit = 0;
+        return list == (unsigned)k * (unsigned)a.parts && i == 0;  // the beam's first
+    };
     grid_dependency_wait();
+    int first_k = 0;
+    Logit first_logit = 0;
+    bool first_first = false;
+    if (EACH == 1 && threadIdx.x < total) first_first = candidate(threadIdx.x, first_k, first_logit);
     for (int k = threadIdx.x; k < K; k += kThreads) {
         const int64_t row = b * K + k;
         const float sc = a.scores[row];
+        const RowPart part0 = a.parts_of[row * a.parts];
         int st = 0;
-        double l = 0.0;
+        Two l = {0.0f, 0.0f};
         if (sc > -INFINITY) {
             if (a.finished && a.finished[row]) {
                 st = 2;
             } else {
                 const RowPart *p = a.parts_of + row * a.parts;
-                float m = -INFINITY;
-                bool bad = false;
-                for (int i = 0; i < a.parts; ++i) m = fmaxf(m, p[i].most), bad |= p[i].sum == ~0ull;
-                double s = 0.0;
+                float m = part0.most;
+                bool bad = part0.sum == ~0ull;
+                for (int i = 1; i < a.parts; ++i) m = fmaxf(m, p[i].most), bad |= p[i].sum == ~0ull;
                 if (!bad && m > -INFINITY && m < INFINITY) {
+                    Two s = {0.0f, 0.0f};
                     for (int i = 0; i < a.parts; ++i) {
-                        const double share = (double)p[i].sum * 0x1p-32;
-                        if (p[i].most > -INFINITY) s += p[i].most == m ? share : share * exp((double)p[i].most - (double)m);
+                        const RowPart of = i == 0 ? part0 : p[i];
+                        const float d = __fsub_rn(of.most, m);  // (below -80 a part counts for nothing)
+                        if (d < -80.0f) continue;
+                        const unsigned long long whole = of.sum;
+                        const float hi = __ull2float_rn(whole);
+                        const Two share = {__fmul_rn(hi, 0x1p-32f),
+                                           __fmul_rn(__ll2float_rn((long long)(whole - (unsigned long long)hi)), 0x1p-32f)};
+                        s = add(s, d == 0.0f ? share : mul(share, exp_two(two_sum(of.most, -m))));
                     }
-                    l = (double)m + log(s);
+                    l = add({m, 0.0f}, log_two(s));
                     st = 1;
                 }
             }
@@ -262,34 +410,32 @@ __global__ void __launch_bounds__(kThreads) beam_merge_kernel(const SelectArgs a
         lse[k] = l, state[k] = (unsigned char)st, score[k] = sc;
     }
     best.start();
-    const int64_t lists = (int64_t)K * a.parts, total = lists * a.n;
-    for (int64_t base = 0; base < total; base += kThreads * kEach) {
-        Cand key[kEach], mine = none_of(Cand());
+    for (int64_t base = 0; base < total; base += kThreads * EACH) {
+        Cand key[EACH], mine = none_of(Cand());
 #pragma unroll
-        for (int e = 0; e < kEach; ++e) {
+        for (int e = 0; e < EACH; ++e) {
             const int64_t at = base + threadIdx.x + (int64_t)e * kThreads;
             key[e] = none_of(Cand());
             if (at < total) {
-                const unsigned list = (unsigned)at / (unsigned)a.n, i = (unsigned)at % (unsigned)a.n;
-                const int k = (int)(list / (unsigned)a.parts), part = (int)(list % (unsigned)a.parts);
-                const int64_t row = b * K + k;
+                int k = first_k;
+                Logit l = first_logit;
+                const bool first = EACH == 1 ? first_first : candidate(at, k, l);
                 if (state[k] == 2) {
-                    if (part == 0 && i == 0) key[e] = cand_key((double)score[k], (unsigned)(k * a.V + a.eos));
-                } else if (state[k] == 1 && (int)i < a.parts_of[row * a.parts + part].held) {
-                    const Logit l = a.keys[(row * a.parts + part) * a.n + i];
-                    key[e] = cand_key((double)score[k] + ((double)logit_of(l) - lse[k]), (unsigned)(k * a.V + (unsigned)~(uint32_t)l));
+                    if (first) key[e] = cand_key(score[k], 0.0f, {0.0f, 0.0f}, (unsigned)(k * a.V + a.eos));
+                } else if (state[k] == 1 && l) {
+                    key[e] = cand_key(score[k], unordered((uint32_t)(l >> 32)), lse[k], (unsigned)(k * a.V + (unsigned)~(uint32_t)l));
                 }
             }
             if (before(key[e], mine)) mine = key[e];
         }
-        best.take(key, mine, a.n);
+        best.take([&](int e) { return key[e]; }, mine, a.n);
     }
     const int held = best.held;
     for (int i = threadIdx.x; i < a.n; i += kThreads) {
         const int64_t o = b * a.n + i;
         if (i < held) {
             const Cand c = best.list[i];
-            a.scores_out[o] = (float)cand_of(c);
+            a.scores_out[o] = unordered((uint32_t)(c.v >> 32));
             a.parents[o] = (int32_t)(c.index / (unsigned)a.V);
             a.tokens[o] = (int32_t)(c.index % (unsigned)a.V);
         } else {
@@ -300,11 +446,18 @@ __global__ void __launch_bounds__(kThreads) beam_merge_kernel(const SelectArgs a
     }
 }
 
-template <typename T>
-qnn_status launch_select(SelectArgs a, int64_t rows, int64_t B, cudaStream_t st) {
+template <typename T, int EACH>
+qnn_status launch_rows(const SelectArgs &a, int64_t rows, cudaStream_t st) {
     const bool vec = reinterpret_cast<uintptr_t>(a.logits) % 16 == 0 && a.ldl * (int64_t)sizeof(T) % 16 == 0;
-    const auto kern = vec ? beam_rows_kernel<T, true> : beam_rows_kernel<T, false>;
+    const auto kern = vec ? beam_rows_kernel<T, true, EACH> : beam_rows_kernel<T, false, EACH>;
     kern<<<(unsigned)(rows * a.parts), kThreads, 0, st>>>(a);
+    QNN_CUDA_TRY(cudaGetLastError());
+    return QNN_OK;
+}
+
+template <typename T>
+qnn_status launch_select(const SelectArgs &a, int each, int64_t rows, int64_t B, cudaStream_t st) {
+    QNN_TRY(each == 8 ? (launch_rows<T, 8>(a, rows, st)) : (launch_rows<T, 32>(a, rows, st)));
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3((unsigned)B);
     cfg.blockDim = dim3(kThreads);
@@ -314,8 +467,7 @@ qnn_status launch_select(SelectArgs a, int64_t rows, int64_t B, cudaStream_t st)
     attr[0].val.programmaticStreamSerializationAllowed = 1;
     cfg.attrs = attr;
     cfg.numAttrs = 1;
-    QNN_CUDA_TRY(cudaGetLastError());
-    QNN_CUDA_TRY(cudaLaunchKernelEx(&cfg, beam_merge_kernel, a));
+    QNN_CUDA_TRY(a.K * a.parts * a.n <= kThreads ? cudaLaunchKernelEx(&cfg, beam_merge_kernel<1>, a) : cudaLaunchKernelEx(&cfg, beam_merge_kernel<8>, a));
     return QNN_OK;
 }
 
@@ -419,9 +571,12 @@ extern "C" qnn_status qnn_beam_select(const void *logits, int64_t ldl, int dtype
     SelectArgs a;
     a.logits = logits, a.ldl = ldl, a.scores = scores, a.finished = finished, a.scores_out = scores_out, a.parents = parents;
     a.tokens = tokens, a.K = K, a.V = V, a.n = n, a.eos = eos;
-    // parts of a row: two tiles or more, while the SMs have fewer than four blocks each
-    const int64_t rows = B * K, tile = kThreads * kEach, tiles = (V + tile - 1) / tile;
-    int64_t parts = std::max<int64_t>(1, std::min<int64_t>({4 * (int64_t)sm_count() / rows, (tiles + 1) / 2, 32}));
+    // Tiles of 8192 classes where those alone give the SMs two blocks each, else of 2048; a part of a row is as many tiles as leave
+    // four blocks an SM (one, while there are fewer).
+    const int64_t rows = B * K;
+    const int each = rows * (V / (32 * kThreads)) >= 2 * (int64_t)sm_count() ? 32 : 8;
+    const int64_t tile = each * kThreads, tiles = (V + tile - 1) / tile;
+    int64_t parts = std::max<int64_t>(1, std::min<int64_t>({4 * (int64_t)sm_count() / rows, tiles, 32}));
     const int64_t per = (tiles + parts - 1) / parts;
     parts = (tiles + per - 1) / per;
     if (rows * parts > INT32_MAX) return QNN_ERR_INVALID_ARG;
@@ -433,7 +588,7 @@ extern "C" qnn_status qnn_beam_select(const void *logits, int64_t ldl, int dtype
     a.keys = static_cast<Logit *>(scratch.ptr());
     a.parts_of = reinterpret_cast<RowPart *>(static_cast<char *>(scratch.ptr()) + keys);
     ProfScope prof("beam_select", st);
-    QNN_TRY(with_type(dtype, [&](auto t) { return launch_select<decltype(t)>(a, rows, B, st); }));
+    QNN_TRY(with_type(dtype, [&](auto t) { return launch_select<decltype(t)>(a, each, rows, B, st); }));
     QNN_CUDA_TRY(cudaGetLastError());
     return QNN_OK;
 }

@@ -94,7 +94,12 @@ __device__ __forceinline__ Tf tf_in(float x) {
 __device__ __forceinline__ float2 two(const float *p) { return *reinterpret_cast<const float2 *>(p); }
 __device__ __forceinline__ float2 two(const __half *p) { return __half22float2(*reinterpret_cast<const __half2 *>(p)); }
 
-// d^i for i = 0 .. count - 1.
+// exp(rate n), rate <= 0: the product's rounding is put back in. (No arithmetic in 64 bits: this part's units for it are few, and a
+// table of these by exp() in 64 bits took 20 us of a launch.)
+__device__ __forceinline__ float power(float rate, float n) {
+    const float x = __fmul_rn(rate, n), e = expf(x);
+    return __fmaf_rn(e, __fmaf_rn(rate, n, -x), e);
+}
 __device__ __forceinline__ float head_rate(const float *log_decay, int h) {
     const float g = __ldg(log_decay + h);
     // (rates below -200 leave nothing of a state after one frame, as infinite ones do; a NaN stays one)
@@ -160,7 +165,7 @@ __global__ void __launch_bounds__(kLinThreads) linear_chunk_kernel(const LinearA
     // (a part's state is needed by those behind it that have frames; a part without frames has nothing to do but part 0)
     if (STATES ? lo + a.per >= n : part > 0 && lo >= n) return;
     const float rate = head_rate(a.log_decay, h);
-    for (int i = threadIdx.x; i <= C; i += kLinThreads) powers[i] = (float)exp((double)rate * i);
+    for (int i = threadIdx.x; i <= C; i += kLinThreads) powers[i] = power(rate, (float)i);
 
     const int col0 = tile * kLinCols, cols = a.dv - col0 < kLinCols ? a.dv - col0 : kLinCols, wcol = warp * 16;
     const bool works = wcol < cols;
@@ -199,7 +204,7 @@ __global__ void __launch_bounds__(kLinThreads) linear_chunk_kernel(const LinearA
         const float *p = n > a.per ? a.partial + unit * a.parts * size : a.state_in ? a.state_in + unit * size : nullptr;
         if (p) each_state([&](float &s, int64_t i) { s = p[i]; });
         if (part > 0) {
-            const float over = (float)exp((double)rate * (double)a.per);
+            const float over = power(rate, (float)a.per);
             for (int j = 0; j < part; ++j) {
                 p += size;
                 each_state([&](float &s, int64_t i) { s = __fmaf_rn(s, over, p[i]); });

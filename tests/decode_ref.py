@@ -62,7 +62,7 @@ def select(logits, scores, n, finished=None, eos=0):
             m = x.max()
             if np.isfinite(m):
                 with np.errstate(invalid="ignore"):
-                    cand[k] = s + (x - (m + np.log(np.exp(x - m).sum())))
+                    cand[k] = s + ((x - m) - np.log(np.exp(x - m).sum()))  # (m + log would lose the log beside a mask of -3e38)
         cand = cand.ravel()
         cand[np.isnan(cand)] = -np.inf
         order = np.argsort(-cand, kind="stable")[:n]
