@@ -144,7 +144,7 @@ int copy_unit(const void *p, int64_t B, int64_t T, int64_t heads, int64_t width,
 
 }  // namespace
 
-int linear_chunk(int dtype, int dk) { return (dtype == QNN_F32 ? 32 : 64) / (dk > 128 ? 2 : 1); }
+int linear_chunk(int dtype, int dk) { return (dtype == QNN_BF16 ? 64 : 32) / (dk > 128 ? 2 : 1); }
 
 }  // namespace qnn
 
@@ -201,7 +201,7 @@ extern "C" qnn_status qnn_linear_attention(const qnn_linear_args *args, void *st
     // parts of a sequence: while the SMs have less than two blocks each, but no fewer than two chunks a part
     const int chunk = linear_chunk(p.dtype, p.dk);
     const int64_t units = B * p.H * a.tiles, chunks = (T + chunk - 1) / chunk;
-    int64_t parts = std::max<int64_t>(1, std::min<int64_t>({2 * (int64_t)sm_count() / units, chunks / 2, 16}));
+    int64_t parts = std::max<int64_t>(1, std::min<int64_t>({2 * (int64_t)sm_count() / units, chunks / 2, 64}));
     const int64_t per = (chunks + parts - 1) / parts;
     a.parts = (int)((chunks + per - 1) / per);
     a.per = per * chunk;

@@ -7,10 +7,12 @@
 // copied while this one is multiplied. The state never leaves the registers: its transpose S^T [16 columns][dk] is the
 // accumulator of the last product, and lies in a lane as the first operand of q S wants it.
 //
-// Numbers. bf16 inputs are operands of bf16 products as they are, and what is held in fp32 is put in as a sum of bf16 pieces of 8
-// bits: scores and state in two (2^-17 of each, far below the output's rounding), the scaled v in three (2^-25: the state is kept
-// in fp32 and is an output). fp16 and fp32 inputs take products of tf32 (11 bits), where an fp16 value is one piece and an fp32
-// one is two, high and low; low times low (2^-22) is left out. All sums are fp32.
+// Numbers. All products are of bf16 pieces of 8 bits with fp32 sums: a bf16 input is one piece, an fp16 input two, an fp32 input
+// three (all exact). What is formed in fp32 is put in as a sum of such pieces: scores and state in two (2^-17 of each, far below a
+// 16-bit output's rounding; fp32: three), the scaled v in three (2^-25: the state is kept in fp32 and is an output). Of the products of
+// pieces those are taken that the shorter of the two sides' precisions needs: one to three for bf16, three to five for fp16, six for fp32
+// (2^-23). (tf32 instructions for fp16 and fp32 took as many, and three times the instructions around them to split operands in
+// every warp: 1 x 4000 x 8 x 64 fp32 125 us.)
 #pragma once
 
 #include <algorithm>
@@ -18,6 +20,7 @@
 
 #include "elem.cuh"
 #include "linattn.h"
+#include "qnn_device.cuh"
 #include "tc_ptx.cuh"
 
 namespace qnn {
@@ -26,14 +29,9 @@ namespace {
 constexpr int kLinThreads = 128, kLinCols = 64;
 
 __device__ __forceinline__ void mma_bf16(float (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
-    asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
-                 : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
-                 : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
-}
-__device__ __forceinline__ void mma_tf32(float (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
-    asm volatile("mma.sync.aligned.m16n8k8.row.col.f32.tf32.tf32.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
-                 : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
-                 : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+    asm("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+        : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
+        : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
 }
 __device__ __forceinline__ void ld_matrix(uint32_t (&r)[4], uint32_t addr) {
     asm volatile("ldmatrix.sync.aligned.m8n8.x4.shared.b16 {%0,%1,%2,%3}, [%4];"
@@ -60,39 +58,28 @@ __device__ __forceinline__ uint32_t rounded_pair(float x, float y) {
     const __nv_bfloat162 p = __floats2bfloat162_rn(x, y);
     return *reinterpret_cast<const uint32_t *>(&p);
 }
-__device__ __forceinline__ void pieces2(float x, float y, uint32_t &hi, uint32_t &lo) {
-    hi = high_halves(x, y);
-    lo = rounded_pair(below_high(x), below_high(y));
+// Two values as N pieces each, a pair of the first, second, ... of them a word; the last piece is rounded.
+template <int N>
+__device__ __forceinline__ void split_pair(float x, float y, uint32_t (&p)[N]) {
+#pragma unroll
+    for (int i = 0; i + 1 < N; ++i) {
+        p[i] = high_halves(x, y);
+        x = below_high(x), y = below_high(y);
+    }
+    p[N - 1] = rounded_pair(x, y);
 }
-__device__ __forceinline__ void pieces3(float x, float y, uint32_t &hi, uint32_t &mid, uint32_t &lo) {
-    hi = high_halves(x, y);
-    const float rx = below_high(x), ry = below_high(y);
-    mid = high_halves(rx, ry);
-    lo = rounded_pair(below_high(rx), below_high(ry));
+__device__ __forceinline__ float low_of(uint32_t w) { return __uint_as_float(w << 16); }
+__device__ __forceinline__ float high_of(uint32_t w) { return __uint_as_float(w & 0xffff0000u); }
+// The products (i, j) of A's and B's pieces that count, the smallest first: i + j below the larger number of pieces.
+template <int A, int B, typename F>
+__device__ __forceinline__ void each_product(F f) {
+    constexpr int kMost = A > B ? A : B;
+#pragma unroll
+    for (int sum = kMost - 1; sum >= 0; --sum)
+#pragma unroll
+        for (int i = 0; i <= sum; ++i)
+            if (i < A && sum - i < B) f(i, sum - i);
 }
-__device__ __forceinline__ uint32_t tf32_of(float x) {
-    uint32_t r;
-    asm("cvt.rna.tf32.f32 %0, %1;" : "=r"(r) : "f"(x));
-    return r;
-}
-// An operand in tf32: the value itself where it is exact, else its two pieces.
-struct Tf {
-    uint32_t hi, lo;
-};
-__device__ __forceinline__ Tf tf_split(float x) {
-    Tf r;
-    r.hi = tf32_of(x);
-    r.lo = tf32_of(__fsub_rn(x, __uint_as_float(r.hi)));
-    return r;
-}
-template <bool EXACT>
-__device__ __forceinline__ Tf tf_in(float x) {
-    if constexpr (EXACT) return {__float_as_uint(x), 0};
-    else return tf_split(x);
-}
-
-__device__ __forceinline__ float2 two(const float *p) { return *reinterpret_cast<const float2 *>(p); }
-__device__ __forceinline__ float2 two(const __half *p) { return __half22float2(*reinterpret_cast<const __half2 *>(p)); }
 
 // exp(rate n), rate <= 0: the product's rounding is put back in. (No arithmetic in 64 bits: this part's units for it are few, and a
 // table of these by exp() in 64 bits took 20 us of a launch.)
@@ -108,11 +95,15 @@ __device__ __forceinline__ float head_rate(const float *log_decay, int h) {
 
 template <typename T, int DKP, int C, bool STATES>
 struct ChunkShape {
-    static constexpr bool kBf16 = std::is_same<T, __nv_bfloat16>::value;
-    static constexpr int E = sizeof(T), QS = DKP + 8, VS = kLinCols + 8, PS = kBf16 ? C + 8 : C + 4;
-    static constexpr int kStage = (C * QS * (STATES ? 1 : 2) + C * VS) * E;
-    static constexpr int kScores = STATES ? 0 : kBf16 ? 2 * C * PS * 2 : C * PS * 4;
-    static constexpr int kBytes = 2 * kStage + kScores + (C + 1) * 4;
+    static constexpr int kPieces = std::is_same<T, __nv_bfloat16>::value ? 1 : sizeof(T) == 2 ? 2 : 3;
+    static constexpr int kHeld = kPieces == 3 ? 3 : 2;  // of a score and of the state
+    static constexpr int QS = DKP + 8, VS = kLinCols + 8, PS = C + 8;
+    static constexpr int kRows = STATES ? 1 : 2;                                   // q and k, or k
+    static constexpr int kPlane = C * (QS * kRows + VS) * 2;                       // a piece of q, k and v
+    static constexpr int kRaw = kPieces == 1 ? 0 : C * (DKP * kRows + kLinCols) * (int)sizeof(T);  // them as they were loaded
+    static constexpr int kOperands = kPieces == 1 ? 2 * kPlane : kPieces * kPlane + kRaw;
+    static constexpr int kScores = STATES ? 0 : kHeld * C * PS * 2;
+    static constexpr int kBytes = kOperands + kScores + (C + 1) * 4;
 };
 
 // `rows` rows of `cols` values from global memory into rows of WIDTH in shared memory, zeros beyond both.
@@ -142,15 +133,36 @@ __device__ __forceinline__ void copy_rows(T *dst, const T *src, int64_t frame, i
         }
     }
 }
+// Rows of WIDTH loaded values to N planes of pieces.
+template <typename T, int C, int WIDTH, int STRIDE, int N>
+__device__ __forceinline__ void split_rows(const T *raw, __nv_bfloat16 *planes, int plane) {
+#pragma unroll 2
+    for (int i = threadIdx.x; i < C * WIDTH / 8; i += kLinThreads) {
+        Run<T, 8> v;
+        v.load(raw + i * 8);
+        uint32_t w[N][4];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            uint32_t p[N];
+            split_pair<N>(v.get(2 * e), v.get(2 * e + 1), p);
+#pragma unroll
+            for (int n = 0; n < N; ++n) w[n][e] = p[n];
+        }
+        const int to = i * 8 / WIDTH * STRIDE + i * 8 % WIDTH;
+#pragma unroll
+        for (int n = 0; n < N; ++n) *reinterpret_cast<uint4 *>(planes + n * plane + to) = make_uint4(w[n][0], w[n][1], w[n][2], w[n][3]);
+    }
+}
 
 template <typename T, int DKP, int C, bool STATES>
 __global__ void __launch_bounds__(kLinThreads) linear_chunk_kernel(const LinearArgs a) {
     using Sh = ChunkShape<T, DKP, C, STATES>;
-    constexpr bool BF = Sh::kBf16, EXACT = sizeof(T) == 2;
-    constexpr int QS = Sh::QS, VS = Sh::VS, PS = Sh::PS, MT = C / 16;
+    using P16 = __nv_bfloat16;
+    constexpr int NP = Sh::kPieces, NH = Sh::kHeld;
+    constexpr int QS = Sh::QS, VS = Sh::VS, PS = Sh::PS, MT = C / 16, PLANE = Sh::kPlane / 2;
     extern __shared__ __align__(16) unsigned char smem[];
-    T *const stage0 = reinterpret_cast<T *>(smem);
-    unsigned char *const scores = smem + 2 * Sh::kStage;
+    P16 *const planes = reinterpret_cast<P16 *>(smem);
+    unsigned char *const scores = smem + Sh::kOperands;
     float *const powers = reinterpret_cast<float *>(scores + Sh::kScores);
     const int warp = threadIdx.x / 32, lane = threadIdx.x % 32, g = lane / 4, t = lane % 4;
 
@@ -164,8 +176,6 @@ __global__ void __launch_bounds__(kLinThreads) linear_chunk_kernel(const LinearA
     const int64_t n = frames_of(a.lengths, b, a.T), lo = part * a.per, hi = lo + a.per < n ? lo + a.per : n;
     // (a part's state is needed by those behind it that have frames; a part without frames has nothing to do but part 0)
     if (STATES ? lo + a.per >= n : part > 0 && lo >= n) return;
-    const float rate = head_rate(a.log_decay, h);
-    for (int i = threadIdx.x; i <= C; i += kLinThreads) powers[i] = power(rate, (float)i);
 
     const int col0 = tile * kLinCols, cols = a.dv - col0 < kLinCols ? a.dv - col0 : kLinCols, wcol = warp * 16;
     const bool works = wcol < cols;
@@ -173,17 +183,26 @@ __global__ void __launch_bounds__(kLinThreads) linear_chunk_kernel(const LinearA
     const T *const k = static_cast<const T *>(a.k) + b * a.k_seq + (int64_t)(h / a.k_share) * a.dk;
     const T *const v = static_cast<const T *>(a.v) + b * a.v_seq + (int64_t)(h / a.v_share) * a.dv + col0;
 
-    auto qs = [&](int s) { return stage0 + s * (Sh::kStage / Sh::E); };
-    auto ks = [&](int s) { return qs(s) + (STATES ? 0 : C * QS); };
-    auto vs = [&](int s) { return ks(s) + C * QS; };
+    // bf16: two stages of operands, copied as they are; others: one stage of what was loaded, from which the pieces are made
+    constexpr int kVRow = Sh::kRows * C * QS;  // of a plane
     auto fetch = [&](int64_t at, int s) {
         const int rows = hi - at < C ? (int)(hi - at) : C;
-        if constexpr (!STATES) copy_rows<T, C, DKP, QS>(qs(s), q + at * a.q_frame, a.q_frame, rows, a.dk, a.q_copy);
-        copy_rows<T, C, DKP, QS>(ks(s), k + at * a.k_frame, a.k_frame, rows, a.dk, a.k_copy);
-        copy_rows<T, C, kLinCols, VS>(vs(s), v + at * a.v_frame, a.v_frame, rows, cols, a.v_copy);
+        if constexpr (NP == 1) {
+            P16 *to = planes + s * PLANE;
+            if constexpr (!STATES) copy_rows<T, C, DKP, QS>(to, q + at * a.q_frame, a.q_frame, rows, a.dk, a.q_copy);
+            copy_rows<T, C, DKP, QS>(to + (STATES ? 0 : C * QS), k + at * a.k_frame, a.k_frame, rows, a.dk, a.k_copy);
+            copy_rows<T, C, kLinCols, VS>(to + kVRow, v + at * a.v_frame, a.v_frame, rows, cols, a.v_copy);
+        } else {
+            T *to = reinterpret_cast<T *>(smem + NP * Sh::kPlane);
+            if constexpr (!STATES) copy_rows<T, C, DKP, DKP>(to, q + at * a.q_frame, a.q_frame, rows, a.dk, a.q_copy);
+            copy_rows<T, C, DKP, DKP>(to + (STATES ? 0 : C * DKP), k + at * a.k_frame, a.k_frame, rows, a.dk, a.k_copy);
+            copy_rows<T, C, kLinCols, kLinCols>(to + Sh::kRows * C * DKP, v + at * a.v_frame, a.v_frame, rows, cols, a.v_copy);
+        }
         copy_commit();
     };
     if (lo < hi) fetch(lo, 0);
+    const float rate = head_rate(a.log_decay, h);
+    for (int i = threadIdx.x; i <= C; i += kLinThreads) powers[i] = power(rate, (float)i);
 
     // S^T: rows (columns of v) g and g + 8, values of dk 8 j + 2 t and the next
     float S[DKP / 8][4];
@@ -193,37 +212,35 @@ __global__ void __launch_bounds__(kLinThreads) linear_chunk_kernel(const LinearA
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
                 const int r = 8 * j + 2 * t + (e & 1), c = wcol + g + 8 * (e >> 1);
-                if (r < a.dk && c < cols) f(S[j][e], (int64_t)r * a.dv + col0 + c);
+                if (r < a.dk && c < cols) f(S[j][e], r * a.dv + col0 + c);
             }
     };
 #pragma unroll
     for (int j = 0; j < DKP / 8; ++j) S[j][0] = S[j][1] = S[j][2] = S[j][3] = 0.0f;
     const int64_t size = (int64_t)a.dk * a.dv;
     if constexpr (!STATES) {
-        // (another part may write state_out, which may be state_in: only a sequence of one part reads that here)
-        const float *p = n > a.per ? a.partial + unit * a.parts * size : a.state_in ? a.state_in + unit * size : nullptr;
-        if (p) each_state([&](float &s, int64_t i) { s = p[i]; });
-        if (part > 0) {
-            const float over = power(rate, (float)a.per);
-            for (int j = 0; j < part; ++j) {
-                p += size;
-                each_state([&](float &s, int64_t i) { s = __fmaf_rn(s, over, p[i]); });
-            }
-        }
-    } else if (part == 0) {
-        float *p = a.partial + unit * a.parts * size;
-        const float *in = a.state_in + unit * size;
-        each_state([&](float &, int64_t i) { p[i] = a.state_in ? in[i] : 0.0f; });
+        // (with parts, the state each begins with: another part may write state_out, which may be state_in)
+        if (a.parts > 1) grid_dependency_wait();
+        const float *p = a.parts > 1 ? a.partial + (unit * a.parts + part) * size : a.state_in ? a.state_in + unit * size : nullptr;
+        if (p) each_state([&](float &s, int i) { s = p[i]; });
     }
 
     int s = 0;
-    for (int64_t base = lo; base < hi; base += C, s ^= 1) {
+    for (int64_t base = lo; base < hi; base += C, s ^= NP == 1) {
         copy_wait();
         __syncthreads();
-        if (base + C < hi) fetch(base + C, s ^ 1);
+        if constexpr (NP == 1) {
+            if (base + C < hi) fetch(base + C, s ^ 1);
+        } else {
+            const T *raw = reinterpret_cast<const T *>(smem + NP * Sh::kPlane);
+            split_rows<T, C * Sh::kRows, DKP, QS, NP>(raw, planes, PLANE);
+            split_rows<T, C, kLinCols, VS, NP>(raw + Sh::kRows * C * DKP, planes + kVRow, PLANE);
+            __syncthreads();
+            if (base + C < hi) fetch(base + C, 0);
+        }
         const int rows = hi - base < C ? (int)(hi - base) : C;
-        const T *const Q = qs(s), *const K = ks(s), *const V = vs(s);
-        const uint32_t Qa = su32(Q), Ka = su32(K), Va = su32(V);
+        const P16 *const Qp = planes + (NP == 1 ? s * PLANE : 0), *const Kp = Qp + (STATES ? 0 : C * QS), *const Vp = Qp + kVRow;
+        const uint32_t Qa = su32(Qp), Ka = su32(Kp), Va = su32(Vp);
 
         // scores of pairs of 16 frames, those of later frames on earlier ones 0, times the decay between them
         if constexpr (!STATES) {
@@ -231,124 +248,82 @@ __global__ void __launch_bounds__(kLinThreads) linear_chunk_kernel(const LinearA
                 int r0 = 0, c0 = block;
                 while (c0 > r0) c0 -= ++r0;
                 r0 *= 16, c0 *= 16;
-                float acc[2][4] = {}, rest[2][4] = {};
-                if constexpr (BF) {
+                float acc[2][2][4] = {};  // (two sums of each, of every other step: a sum's instructions wait for one another)
+                const uint32_t qa = Qa + ((r0 + lane % 16) * QS + lane / 16 * 8) * 2;
+                const uint32_t ka = Ka + ((c0 + lane % 8 + lane / 16 * 8) * QS + lane / 8 % 2 * 8) * 2;
 #pragma unroll
-                    for (int k0 = 0; k0 < DKP; k0 += 16) {
-                        if (k0 < a.dk) {
-                            uint32_t x[4], y[4];
-                            ld_matrix(x, Qa + ((r0 + lane % 16) * QS + k0 + lane / 16 * 8) * 2);
-                            ld_matrix(y, Ka + ((c0 + lane % 8 + lane / 16 * 8) * QS + k0 + lane / 8 % 2 * 8) * 2);
-                            mma_bf16(acc[0], x, y[0], y[1]);
-                            mma_bf16(acc[1], x, y[2], y[3]);
+                for (int k0 = 0; k0 < DKP; k0 += 16) {
+                    if (k0 < a.dk) {
+                        uint32_t x[NP][4], y[NP][4];
+#pragma unroll
+                        for (int p = 0; p < NP; ++p) {
+                            ld_matrix(x[p], qa + (p * PLANE + k0) * 2);
+                            ld_matrix(y[p], ka + (p * PLANE + k0) * 2);
                         }
+                        each_product<NP, NP>([&](int i, int j) {
+                            float(&to)[2][4] = acc[NP == 1 ? k0 / 16 & 1 : i + j > 0];
+                            mma_bf16(to[0], x[i], y[j][0], y[j][1]);
+                            mma_bf16(to[1], x[i], y[j][2], y[j][3]);
+                        });
                     }
-                } else {
-#pragma unroll 4
-                    for (int k0 = 0; k0 < DKP; k0 += 8) {
-                        if (k0 < a.dk) {
-                            const float2 x0 = two(Q + (r0 + g) * QS + k0 + 2 * t), x1 = two(Q + (r0 + g + 8) * QS + k0 + 2 * t);
-                            const Tf a0 = tf_in<EXACT>(x0.x), a1 = tf_in<EXACT>(x1.x), a2 = tf_in<EXACT>(x0.y), a3 = tf_in<EXACT>(x1.y);
-                            const uint32_t hi4[4] = {a0.hi, a1.hi, a2.hi, a3.hi}, lo4[4] = {a0.lo, a1.lo, a2.lo, a3.lo};
-#pragma unroll
-                            for (int nt = 0; nt < 2; ++nt) {
-                                const float2 y = two(K + (c0 + nt * 8 + g) * QS + k0 + 2 * t);
-                                const Tf b0 = tf_in<EXACT>(y.x), b1 = tf_in<EXACT>(y.y);
-                                if constexpr (!EXACT) {
-                                    mma_tf32(rest[nt], lo4, b0.hi, b1.hi);
-                                    mma_tf32(rest[nt], hi4, b0.lo, b1.lo);
-                                }
-                                mma_tf32(acc[nt], hi4, b0.hi, b1.hi);
-                            }
-                        }
-                    }
-                }
-                if constexpr (!EXACT) {
-#pragma unroll
-                    for (int i = 0; i < 8; ++i) acc[i / 4][i % 4] = __fadd_rn(acc[i / 4][i % 4], rest[i / 4][i % 4]);
                 }
 #pragma unroll
                 for (int nt = 0; nt < 2; ++nt)
 #pragma unroll
                     for (int half = 0; half < 2; ++half) {
                         const int i = r0 + g + 8 * half, j = c0 + nt * 8 + 2 * t;
-                        const float x = i >= j ? __fmul_rn(acc[nt][2 * half], powers[i >= j ? i - j : 0]) : 0.0f;
-                        const float y = i > j ? __fmul_rn(acc[nt][2 * half + 1], powers[i > j ? i - j - 1 : 0]) : 0.0f;
-                        if constexpr (BF) {
-                            uint32_t *hi = reinterpret_cast<uint32_t *>(scores) + (i * PS + j) / 2, *lo = hi + C * PS / 2;
-                            pieces2(x, y, *hi, *lo);
-                        } else {
-                            *reinterpret_cast<float2 *>(reinterpret_cast<float *>(scores) + i * PS + j) = make_float2(x, y);
-                        }
+                        const float u = __fadd_rn(acc[0][nt][2 * half], acc[1][nt][2 * half]);
+                        const float w = __fadd_rn(acc[0][nt][2 * half + 1], acc[1][nt][2 * half + 1]);
+                        const float x = i >= j ? __fmul_rn(u, powers[i >= j ? i - j : 0]) : 0.0f;
+                        const float y = i > j ? __fmul_rn(w, powers[i > j ? i - j - 1 : 0]) : 0.0f;
+                        uint32_t p[NH];
+                        split_pair<NH>(x, y, p);
+                        uint32_t *to = reinterpret_cast<uint32_t *>(scores) + (i * PS + j) / 2;
+#pragma unroll
+                        for (int m = 0; m < NH; ++m) to[m * (C * PS / 2)] = p[m];
                     }
             }
             __syncthreads();
         }
         if (!works) continue;
 
-        // the warp's columns of v, a pair of frames of one column a register (bf16)
-        uint32_t vf[MT][4];
-        bool finite = true;
-        if constexpr (BF) {
-            uint32_t zero = 0;
+        // the warp's columns of v: registers 0 .. 3 of frames 2 t, 2 t + 8 (pairs), and again for 8 columns on
+        uint32_t vf[NP][MT][4];
+        uint32_t zero = 0;
+#pragma unroll
+        for (int p = 0; p < NP; ++p)
 #pragma unroll
             for (int m = 0; m < MT; ++m) {
-                ld_matrix_t(vf[m], Va + ((m * 16 + lane % 16) * VS + wcol + lane / 16 * 8) * 2);
+                ld_matrix_t(vf[p][m], Va + (p * PLANE + (m * 16 + lane % 16) * VS + wcol + lane / 16 * 8) * 2);
 #pragma unroll
-                for (int e = 0; e < 4; ++e) asm("fma.rn.bf16x2 %0, %1, %2, %0;" : "+r"(zero) : "r"(vf[m][e]), "r"(0u));
+                for (int e = 0; e < 4; ++e) asm("fma.rn.bf16x2 %0, %1, %2, %0;" : "+r"(zero) : "r"(vf[p][m][e]), "r"(0u));
             }
-            finite = (zero & 0x7fff7fffu) == 0;
-        } else {
-            float zero = 0.0f;
-            for (int i = lane; i < C * 16; i += 32) zero = __fmaf_rn(to_f32(V[i / 16 * VS + wcol + i % 16]), 0.0f, zero);
-            finite = zero == 0.0f;
-        }
-        finite = __all_sync(0xffffffffu, finite);
+        const bool finite = __all_sync(0xffffffffu, (zero & 0x7fff7fffu) == 0);
 
         if constexpr (!STATES) {
-            float y[MT][2][4] = {}, rest[MT][2][4] = {};  // (fp32: products with low pieces apart, see the state)
+            float y[MT][2][4] = {};
             // q S
-            if constexpr (BF) {
+            const uint32_t qa = Qa + (lane % 16 * QS + lane / 16 * 8) * 2;
 #pragma unroll
-                for (int k0 = 0; k0 < DKP; k0 += 16) {
-                    if (k0 < a.dk) {
-                        const int j = k0 / 8;
-                        uint32_t hi[4], lo[4];
-                        pieces2(S[j][0], S[j][1], hi[0], lo[0]);
-                        pieces2(S[j + 1][0], S[j + 1][1], hi[1], lo[1]);
-                        pieces2(S[j][2], S[j][3], hi[2], lo[2]);
-                        pieces2(S[j + 1][2], S[j + 1][3], hi[3], lo[3]);
+            for (int k0 = 0; k0 < DKP; k0 += 16) {
+                if (k0 < a.dk) {
+                    const int j = k0 / 8;
+                    uint32_t sp[4][NH], x[MT][NP][4];
+                    split_pair<NH>(S[j][0], S[j][1], sp[0]);
+                    split_pair<NH>(S[j + 1][0], S[j + 1][1], sp[1]);
+                    split_pair<NH>(S[j][2], S[j][3], sp[2]);
+                    split_pair<NH>(S[j + 1][2], S[j + 1][3], sp[3]);
 #pragma unroll
-                        for (int m = 0; m < MT; ++m) {
-                            uint32_t x[4];
-                            ld_matrix(x, Qa + ((m * 16 + lane % 16) * QS + k0 + lane / 16 * 8) * 2);
-                            mma_bf16(y[m][0], x, lo[0], lo[1]);
-                            mma_bf16(y[m][1], x, lo[2], lo[3]);
-                            mma_bf16(y[m][0], x, hi[0], hi[1]);
-                            mma_bf16(y[m][1], x, hi[2], hi[3]);
-                        }
-                    }
-                }
-            } else {
+                    for (int m = 0; m < MT; ++m)
 #pragma unroll
-                for (int k0 = 0; k0 < DKP; k0 += 8) {
-                    if (k0 < a.dk) {
-                        Tf sp[4];
-#pragma unroll
-                        for (int e = 0; e < 4; ++e) sp[e] = tf_split(S[k0 / 8][e]);
+                        for (int p = 0; p < NP; ++p) ld_matrix(x[m][p], qa + (p * PLANE + m * 16 * QS + k0) * 2);
+                    each_product<NP, NH>([&](int i, int j) {
 #pragma unroll
                         for (int m = 0; m < MT; ++m) {
-                            const float2 x0 = two(Q + (m * 16 + g) * QS + k0 + 2 * t), x1 = two(Q + (m * 16 + g + 8) * QS + k0 + 2 * t);
-                            const Tf a0 = tf_in<EXACT>(x0.x), a1 = tf_in<EXACT>(x1.x), a2 = tf_in<EXACT>(x0.y), a3 = tf_in<EXACT>(x1.y);
-                            const uint32_t hi4[4] = {a0.hi, a1.hi, a2.hi, a3.hi}, lo4[4] = {a0.lo, a1.lo, a2.lo, a3.lo};
-#pragma unroll
-                            for (int nt = 0; nt < 2; ++nt) {
-                                if constexpr (!EXACT) mma_tf32(rest[m][nt], lo4, sp[2 * nt].hi, sp[2 * nt + 1].hi);
-                                mma_tf32(EXACT ? y[m][nt] : rest[m][nt], hi4, sp[2 * nt].lo, sp[2 * nt + 1].lo);
-                                mma_tf32(y[m][nt], hi4, sp[2 * nt].hi, sp[2 * nt + 1].hi);
-                            }
+                            mma_bf16(y[m][0], x[m][i], sp[0][j], sp[1][j]);
+                            mma_bf16(y[m][1], x[m][i], sp[2][j], sp[3][j]);
                         }
-                    }
+                    });
                 }
             }
 #pragma unroll
@@ -356,13 +331,11 @@ __global__ void __launch_bounds__(kLinThreads) linear_chunk_kernel(const LinearA
 #pragma unroll
                 for (int nt = 0; nt < 2; ++nt)
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) {
-                        if constexpr (!EXACT) y[m][nt][e] = __fadd_rn(y[m][nt][e], rest[m][nt][e]), rest[m][nt][e] = 0.0f;
-                        y[m][nt][e] = __fmul_rn(y[m][nt][e], powers[m * 16 + g + 8 * (e >> 1) + 1]);
-                    }
+                    for (int e = 0; e < 4; ++e) y[m][nt][e] = __fmul_rn(y[m][nt][e], powers[m * 16 + g + 8 * (e >> 1) + 1]);
             // scores v. A later frame's score is 0, whose product with an infinity would be a NaN in an earlier frame's output:
             // where a column holds one, the sums are formed frame by frame.
             if (!finite) {
+                const P16 *p = reinterpret_cast<const P16 *>(scores);
 #pragma unroll
                 for (int m = 0; m < MT; ++m)
 #pragma unroll
@@ -372,77 +345,50 @@ __global__ void __launch_bounds__(kLinThreads) linear_chunk_kernel(const LinearA
                             const int i = m * 16 + g + 8 * (e >> 1), c = wcol + nt * 8 + 2 * t + (e & 1);
                             float sum = y[m][nt][e];
                             for (int j = 0; j <= i; ++j) {
-                                float p;
-                                if constexpr (BF) {
-                                    const __nv_bfloat16 *hi = reinterpret_cast<const __nv_bfloat16 *>(scores) + i * PS + j;
-                                    p = __fadd_rn(to_f32(hi[0]), to_f32(hi[C * PS]));
-                                } else {
-                                    p = reinterpret_cast<const float *>(scores)[i * PS + j];
-                                }
-                                sum = __fmaf_rn(p, to_f32(V[j * VS + c]), sum);
+                                float u = 0.0f, w = 0.0f;
+                                for (int r = NH - 1; r >= 0; --r) u = __fadd_rn(u, to_f32(p[r * C * PS + i * PS + j]));
+                                for (int r = NP - 1; r >= 0; --r) w = __fadd_rn(w, to_f32(Vp[r * PLANE + j * VS + c]));
+                                sum = __fmaf_rn(u, w, sum);
                             }
                             y[m][nt][e] = sum;
                         }
-            } else if constexpr (BF) {
-                const uint32_t P = su32(scores);
-#pragma unroll
-                for (int m = 0; m < MT; ++m)
-#pragma unroll
-                    for (int j = 0; j <= m; ++j) {
-                        uint32_t hi[4], lo[4];
-                        const uint32_t p = P + ((m * 16 + lane % 16) * PS + j * 16 + lane / 16 * 8) * 2;
-                        ld_matrix(lo, p + C * PS * 2);
-                        ld_matrix(hi, p);
-                        mma_bf16(y[m][0], lo, vf[j][0], vf[j][1]);
-                        mma_bf16(y[m][1], lo, vf[j][2], vf[j][3]);
-                        mma_bf16(y[m][0], hi, vf[j][0], vf[j][1]);
-                        mma_bf16(y[m][1], hi, vf[j][2], vf[j][3]);
-                    }
             } else {
-                const float *P = reinterpret_cast<const float *>(scores);
+                const uint32_t pa = su32(scores) + (lane % 16 * PS + lane / 16 * 8) * 2;
 #pragma unroll
-                for (int j = 0; j < C; j += 8) {
-                    Tf vp[2][2];
+                for (int j = 0; j < MT; ++j) {
+                    uint32_t x[MT][NH][4];
 #pragma unroll
-                    for (int nt = 0; nt < 2; ++nt)
+                    for (int m = j; m < MT; ++m)
 #pragma unroll
-                        for (int e = 0; e < 2; ++e) vp[nt][e] = tf_in<EXACT>(to_f32(V[(j + t + 4 * e) * VS + wcol + nt * 8 + g]));
+                        for (int p = 0; p < NH; ++p) ld_matrix(x[m][p], pa + (p * C * PS + m * 16 * PS + j * 16) * 2);
+                    each_product<NH, NP>([&](int i, int p) {
 #pragma unroll
-                    for (int m = j / 16; m < MT; ++m) {
-                        const float *p = P + (m * 16 + g) * PS + j + t;
-                        const Tf a0 = tf_split(p[0]), a1 = tf_split(p[8 * PS]), a2 = tf_split(p[4]), a3 = tf_split(p[8 * PS + 4]);
-                        const uint32_t hi4[4] = {a0.hi, a1.hi, a2.hi, a3.hi}, lo4[4] = {a0.lo, a1.lo, a2.lo, a3.lo};
-#pragma unroll
-                        for (int nt = 0; nt < 2; ++nt) {
-                            mma_tf32(EXACT ? y[m][nt] : rest[m][nt], lo4, vp[nt][0].hi, vp[nt][1].hi);
-                            if constexpr (!EXACT) mma_tf32(rest[m][nt], hi4, vp[nt][0].lo, vp[nt][1].lo);
-                            mma_tf32(y[m][nt], hi4, vp[nt][0].hi, vp[nt][1].hi);
+                        for (int m = j; m < MT; ++m) {
+                            mma_bf16(y[m][0], x[m][i], vf[p][j][0], vf[p][j][1]);
+                            mma_bf16(y[m][1], x[m][i], vf[p][j][2], vf[p][j][3]);
                         }
-                    }
-                }
-                if constexpr (!EXACT) {
-#pragma unroll
-                    for (int i = 0; i < MT * 8; ++i) y[i / 8][i / 4 % 2][i % 4] = __fadd_rn(y[i / 8][i / 4 % 2][i % 4], rest[i / 8][i / 4 % 2][i % 4]);
+                    });
                 }
             }
+            T *const out = static_cast<T *>(a.y) + b * a.y_seq + (base + g) * a.y_frame + (int64_t)h * a.dv + col0;
 #pragma unroll
             for (int m = 0; m < MT; ++m)
 #pragma unroll
                 for (int half = 0; half < 2; ++half) {
-                    const int i = m * 16 + g + 8 * half;
-                    if (i < rows) {
-                        T *out = static_cast<T *>(a.y) + b * a.y_seq + (base + i) * a.y_frame + (int64_t)h * a.dv + col0;
+                    const int i = m * 16 + 8 * half;
+                    if (i + g < rows) {
+                        T *o = out + i * a.y_frame;
 #pragma unroll
                         for (int nt = 0; nt < 2; ++nt) {
                             const int c = wcol + nt * 8 + 2 * t;
                             const float f[2] = {__fmul_rn(y[m][nt][2 * half], a.scale), __fmul_rn(y[m][nt][2 * half + 1], a.scale)};
                             if (a.pairs && c + 1 < cols) {
-                                Run<T, 2> o;
-                                o.set(f);
-                                o.store(out + c);
+                                Run<T, 2> r;
+                                r.set(f);
+                                r.store(o + c);
                             } else {
-                                if (c < cols) out[c] = from_f32<T>(f[0]);
-                                if (c + 1 < cols) out[c + 1] = from_f32<T>(f[1]);
+                                if (c < cols) o[c] = from_f32<T>(f[0]);
+                                if (c + 1 < cols) o[c + 1] = from_f32<T>(f[1]);
                             }
                         }
                     }
@@ -454,76 +400,89 @@ __global__ void __launch_bounds__(kLinThreads) linear_chunk_kernel(const LinearA
         // came out 1e-6 low.
         const float decay = powers[rows];
         auto weight = [&](int frame) { return powers[rows - 1 - frame > 0 ? rows - 1 - frame : 0]; };  // (frames past the last are zeros)
-        auto add = [&](int j, const float (&sum)[4]) {
+        uint32_t vp[MT][3][4];
 #pragma unroll
-            for (int e = 0; e < 4; ++e) S[j][e] = __fmaf_rn(S[j][e], decay, sum[e]);
-        };
-        if constexpr (BF) {
-            uint32_t hi[MT][4], mid[MT][4], lo[MT][4];
+        for (int m = 0; m < MT; ++m)
 #pragma unroll
-            for (int m = 0; m < MT; ++m)
+            for (int e = 0; e < 4; ++e) {
+                const int frame = m * 16 + 2 * t + 8 * (e & 1);
+                float x = low_of(vf[NP - 1][m][e]), z = high_of(vf[NP - 1][m][e]);
 #pragma unroll
-                for (int e = 0; e < 4; ++e) {  // registers 0 .. 3: frames 2 t, 2 t + 8, and again for 8 columns on
-                    const int frame = m * 16 + 2 * t + 8 * (e & 1);
-                    const float x = __fmul_rn(__uint_as_float(vf[m][e] << 16), weight(frame));
-                    const float z = __fmul_rn(__uint_as_float(vf[m][e] & 0xffff0000u), weight(frame + 1));
-                    const int to = e == 1 ? 2 : e == 2 ? 1 : e;  // (operand order: columns before frames)
-                    pieces3(x, z, hi[m][to], mid[m][to], lo[m][to]);
-                }
-#pragma unroll
-            for (int n0 = 0; n0 < DKP; n0 += 16) {
-                if (n0 < a.dk) {
-                    float sum[2][4] = {};
-#pragma unroll
-                    for (int m = 0; m < MT; ++m) {
-                        uint32_t x[4];
-                        ld_matrix_t(x, Ka + ((m * 16 + lane % 16) * QS + n0 + lane / 16 * 8) * 2);
-                        mma_bf16(sum[0], lo[m], x[0], x[1]);
-                        mma_bf16(sum[1], lo[m], x[2], x[3]);
-                        mma_bf16(sum[0], mid[m], x[0], x[1]);
-                        mma_bf16(sum[1], mid[m], x[2], x[3]);
-                        mma_bf16(sum[0], hi[m], x[0], x[1]);
-                        mma_bf16(sum[1], hi[m], x[2], x[3]);
-                    }
-                    add(n0 / 8, sum[0]);
-                    add(n0 / 8 + 1, sum[1]);
-                }
+                for (int p = NP - 2; p >= 0; --p) x = __fadd_rn(x, low_of(vf[p][m][e])), z = __fadd_rn(z, high_of(vf[p][m][e]));
+                uint32_t p3[3];
+                split_pair<3>(__fmul_rn(x, weight(frame)), __fmul_rn(z, weight(frame + 1)), p3);
+                const int to = e == 1 ? 2 : e == 2 ? 1 : e;  // (operand order: columns before frames)
+                vp[m][0][to] = p3[0], vp[m][1][to] = p3[1], vp[m][2][to] = p3[2];
             }
-        } else {
-            Tf x[C / 8][4];
+        const uint32_t ka = Ka + (lane % 16 * QS + lane / 16 * 8) * 2;
 #pragma unroll
-            for (int j = 0; j < C; j += 8) {
-                const T *p = V + (j + t) * VS + wcol + g;
-                const float w0 = weight(j + t), w1 = weight(j + t + 4);
-                x[j / 8][0] = tf_split(__fmul_rn(to_f32(p[0]), w0)), x[j / 8][1] = tf_split(__fmul_rn(to_f32(p[8]), w0));
-                x[j / 8][2] = tf_split(__fmul_rn(to_f32(p[4 * VS]), w1)), x[j / 8][3] = tf_split(__fmul_rn(to_f32(p[4 * VS + 8]), w1));
-            }
+        for (int n0 = 0; n0 < DKP; n0 += 32) {
+            if (n0 < a.dk) {
+                float sum[4][4] = {};
 #pragma unroll
-            for (int n0 = 0; n0 < DKP; n0 += 8) {
-                if (n0 < a.dk) {
-                    float sum[4] = {}, rest[4] = {};
+                for (int m = 0; m < MT; ++m) {
+                    uint32_t x[NP][2][4];
 #pragma unroll
-                    for (int j = 0; j < C; j += 8) {
-                        const Tf(&v4)[4] = x[j / 8];
-                        const uint32_t hi4[4] = {v4[0].hi, v4[1].hi, v4[2].hi, v4[3].hi}, lo4[4] = {v4[0].lo, v4[1].lo, v4[2].lo, v4[3].lo};
-                        const Tf b0 = tf_in<EXACT>(to_f32(K[(j + t) * QS + n0 + g])), b1 = tf_in<EXACT>(to_f32(K[(j + t + 4) * QS + n0 + g]));
-                        mma_tf32(rest, lo4, b0.hi, b1.hi);
-                        if constexpr (!EXACT) mma_tf32(rest, hi4, b0.lo, b1.lo);
-                        mma_tf32(sum, hi4, b0.hi, b1.hi);
+                    for (int p = 0; p < NP; ++p) {
+                        ld_matrix_t(x[p][0], ka + (p * PLANE + m * 16 * QS + n0) * 2);
+                        ld_matrix_t(x[p][1], ka + (p * PLANE + m * 16 * QS + n0 + 16) * 2);
                     }
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) sum[e] = __fadd_rn(sum[e], rest[e]);
-                    add(n0 / 8, sum);
+                    each_product<3, NP>([&](int i, int p) {
+                        mma_bf16(sum[0], vp[m][i], x[p][0][0], x[p][0][1]);
+                        mma_bf16(sum[1], vp[m][i], x[p][0][2], x[p][0][3]);
+                        mma_bf16(sum[2], vp[m][i], x[p][1][0], x[p][1][1]);
+                        mma_bf16(sum[3], vp[m][i], x[p][1][2], x[p][1][3]);
+                    });
                 }
+#pragma unroll
+                for (int j = 0; j < 4; ++j)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) S[n0 / 8 + j][e] = __fmaf_rn(S[n0 / 8 + j][e], decay, sum[j][e]);
             }
         }
     }
     if constexpr (STATES) {
-        float *p = a.partial + (unit * a.parts + part + 1) * size;
-        each_state([&](float &s, int64_t i) { p[i] = s; });
+        float *p = a.partial + (unit * a.parts + part) * size;
+        each_state([&](float &s, int i) { p[i] = s; });
     } else {
         // the part with the sequence's last frame (the first one, for none) has its state
-        if (a.state_out && (hi == n || n == 0)) each_state([&](float &s, int64_t i) { a.state_out[unit * size + i] = s; });
+        if (a.state_out && (hi == n || n == 0)) {
+            float *p = a.state_out + unit * size;
+            each_state([&](float &s, int i) { p[i] = s; });
+        }
+    }
+}
+
+// From the states that the parts of a sequence end with from zeros, those that they begin with, in their place: a thread an element,
+// eight parts loaded at a time. (Of parts without frames nothing is used.)
+constexpr int kPrefixThreads = 256;
+template <bool VEC>
+__global__ void __launch_bounds__(kPrefixThreads) linear_prefix_kernel(const LinearArgs a) {
+    using W = typename std::conditional<VEC, float4, float>::type;
+    const int64_t size = (int64_t)a.dk * a.dv / (VEC ? 4 : 1), at = (int64_t)blockIdx.x * kPrefixThreads + threadIdx.x;
+    const int64_t unit = at / size, i = at % size;
+    if (unit >= a.B * a.H) return;
+    const float over = power(head_rate(a.log_decay, (int)(unit % a.H)), (float)a.per);
+    W run = {};
+    if (a.state_in) run = reinterpret_cast<const W *>(a.state_in)[unit * size + i];
+    grid_dependency_wait();
+    W *p = reinterpret_cast<W *>(a.partial) + unit * a.parts * size + i;
+    for (int j0 = 0; j0 < a.parts; j0 += 8) {
+        W v[8];
+#pragma unroll
+        for (int j = 0; j < 8; ++j)
+            if (j0 + j + 1 < a.parts) v[j] = p[(j0 + j) * size];
+#pragma unroll
+        for (int j = 0; j < 8; ++j)
+            if (j0 + j < a.parts) {
+                p[(j0 + j) * size] = run;
+                if constexpr (VEC) {
+                    run.x = __fmaf_rn(run.x, over, v[j].x), run.y = __fmaf_rn(run.y, over, v[j].y);
+                    run.z = __fmaf_rn(run.z, over, v[j].z), run.w = __fmaf_rn(run.w, over, v[j].w);
+                } else {
+                    run = __fmaf_rn(run, over, v[j]);
+                }
+            }
     }
 }
 
@@ -535,14 +494,37 @@ qnn_status launch_chunk(const LinearArgs &a, cudaStream_t st) {
     QNN_CUDA_TRY(cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, Sh::kBytes));
     const int64_t blocks = a.B * a.H * a.tiles * (STATES ? a.parts - 1 : a.parts);
     if (blocks > INT32_MAX) return QNN_FAIL(QNN_ERR_INVALID_ARG);
-    kern<<<(unsigned)blocks, kLinThreads, Sh::kBytes, st>>>(a);
-    QNN_CUDA_TRY(cudaGetLastError());
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3((unsigned)blocks);
+    cfg.blockDim = dim3(kLinThreads);
+    cfg.dynamicSmemBytes = Sh::kBytes;
+    cfg.stream = st;
+    cudaLaunchAttribute attr;
+    attr.id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr.val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = &attr;
+    cfg.numAttrs = !STATES && a.parts > 1 ? 1 : 0;
+    QNN_CUDA_TRY(cudaLaunchKernelEx(&cfg, kern, a));
     return QNN_OK;
 }
 
 template <typename T, int DKP, int C>
 qnn_status launch_parts(const LinearArgs &a, cudaStream_t st) {
-    if (a.parts > 1) QNN_TRY((launch_chunk<T, DKP, C, true>(a, st)));
+    if (a.parts > 1) {
+        QNN_TRY((launch_chunk<T, DKP, C, true>(a, st)));
+        const bool vec = (int64_t)a.dk * a.dv % 4 == 0 && reinterpret_cast<uintptr_t>(a.state_in) % 16 == 0;
+        const int64_t blocks = (a.B * a.H * a.dk * a.dv / (vec ? 4 : 1) + kPrefixThreads - 1) / kPrefixThreads;
+        cudaLaunchConfig_t cfg = {};
+        cfg.gridDim = dim3((unsigned)blocks);
+        cfg.blockDim = dim3(kPrefixThreads);
+        cfg.stream = st;
+        cudaLaunchAttribute attr;
+        attr.id = cudaLaunchAttributeProgrammaticStreamSerialization;
+        attr.val.programmaticStreamSerializationAllowed = 1;
+        cfg.attrs = &attr;
+        cfg.numAttrs = 1;
+        QNN_CUDA_TRY(vec ? cudaLaunchKernelEx(&cfg, linear_prefix_kernel<true>, a) : cudaLaunchKernelEx(&cfg, linear_prefix_kernel<false>, a));
+    }
     return launch_chunk<T, DKP, C, false>(a, st);
 }
 
@@ -550,7 +532,7 @@ qnn_status launch_parts(const LinearArgs &a, cudaStream_t st) {
 
 template <typename T>
 qnn_status launch_linear_chunks(const LinearArgs &a, cudaStream_t st) {
-    constexpr int C = sizeof(T) == 4 ? 32 : 64;
+    constexpr int C = std::is_same<T, __nv_bfloat16>::value ? 64 : 32;
     if (a.dk <= 64) return launch_parts<T, 64, C>(a, st);
     if (a.dk <= 128) return launch_parts<T, 128, C>(a, st);
     return launch_parts<T, 256, C / 2>(a, st);

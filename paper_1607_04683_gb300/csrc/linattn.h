@@ -9,7 +9,7 @@ struct LinearArgs {
     const void *q, *k, *v;
     void *y;
     const float *log_decay, *state_in;
-    float *state_out, *partial;  // partial: [B H][parts][dk][dv], state_in and what each part but the last would end with from zeros
+    float *state_out, *partial;  // partial: [B H][parts][dk][dv], what each part but the last ends with from zeros, then what each begins with
     const int32_t *lengths;
     int64_t q_seq, q_frame, k_seq, k_frame, v_seq, v_frame, y_seq, y_frame, B, T;
     int64_t per;  // frames of a part
