@@ -1,5 +1,7 @@
 // linattn.cu — linear attention with a decay for each head on sm_103a: the call, and its recurrent kernel for few frames.
 #include <algorithm>
+#include <cstdlib>
+#include <cstring>
 
 #include "elem.cuh"
 #include "linattn.h"
@@ -142,6 +144,22 @@ int copy_unit(const void *p, int64_t B, int64_t T, int64_t heads, int64_t width,
     return bits % 16 == 0 ? 16 : bits % 8 == 0 ? 8 : bits % 4 == 0 ? 4 : 0;
 }
 
+// Which of the two kernels takes a bf16 sequence, by what they took (us; dk = dv, sequences x heads): the tcgen05 one a chunk
+// of 128 frames in 3.3 and a sequence in 5 more, one block an SM; the other a chunk of 64 frames in 5 to 7, two blocks an SM, or with
+// the sequence in parts 6 to 9 for both passes. Of 128: T 64 10.4 / 10.3, 1 x 1000 33 / 29, 76 x 1000 39 / 88, 16 x 4000 111 / 85,
+// 38 x 4000 114 / 182; of 64: 38 x 1000 33 / 27, 152 x 1000 37 / 64; of 32: 304 x 128 16.5 / 14.5.
+bool prefers_tc(const LinearArgs &a, int chunk, int64_t chunks) {
+    if (const char *e = std::getenv("QNN_LINEAR")) {  // one of them always (tests)
+        if (std::strcmp(e, "tc") == 0) return true;
+        if (std::strcmp(e, "chunks") == 0) return false;
+    }
+    const int64_t blocks = a.B * a.H * a.tiles, sms = sm_count();
+    const double tc = 2.0 + (5.0 + 3.3 * (double)((a.T + 127) / 128)) * (double)((blocks + sms - 1) / sms);
+    const double per = (double)(a.parts > 1 ? a.per / chunk : chunks);
+    return tc < (a.parts > 1 ? 17.0 + (a.dk > 64 ? 9.0 : 6.0) * per
+                             : 6.0 + (a.dk > 64 ? 7.2 : 4.6) * per * (double)((blocks + 2 * sms - 1) / (2 * sms)));
+}
+
 }  // namespace
 
 int linear_chunk(int dtype, int dk) { return (dtype == QNN_BF16 ? 64 : 32) / (dk > 128 ? 2 : 1); }
@@ -196,6 +214,7 @@ extern "C" qnn_status qnn_linear_attention(const qnn_linear_args *args, void *st
     a.q_copy = copy_unit(p.q, B, T, p.q_heads, p.dk, p.q_seq, p.q_frame, e);
     a.k_copy = copy_unit(p.k, B, T, p.k_heads, p.dk, p.k_seq, p.k_frame, e);
     a.v_copy = copy_unit(p.v, B, T, p.v_heads, p.dv, p.v_seq, p.v_frame, e);
+    a.y_copy = copy_unit(p.y, B, T, p.H, p.dv, p.y_seq, p.y_frame, e);
     const uintptr_t ybits = reinterpret_cast<uintptr_t>(p.y) | (uintptr_t)((B > 1 ? p.y_seq * e : 0) | p.y_frame * e | (int64_t)p.dv * e);
     a.pairs = ybits % (2 * e) == 0;
     // parts of a sequence: while the SMs have less than two blocks each, but no fewer than two chunks a part
@@ -205,6 +224,10 @@ extern "C" qnn_status qnn_linear_attention(const qnn_linear_args *args, void *st
     const int64_t per = (chunks + parts - 1) / parts;
     a.parts = (int)((chunks + per - 1) / per);
     a.per = per * chunk;
+    if (p.dtype == QNN_BF16 && linear_tc_fits(a) && prefers_tc(a, chunk, chunks)) {
+        ProfScope prof("linear_attention", st);
+        return launch_linear_tc(a, st);
+    }
     Scratch scratch;
     if (a.parts > 1) {
         QNN_TRY(scratch.take((size_t)(B * p.H * a.parts) * p.dk * p.dv * sizeof(float), st));

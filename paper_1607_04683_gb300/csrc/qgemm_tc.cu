@@ -1602,6 +1602,22 @@ qnn_status tc_map_f16(CUtensorMap *map, const __half *base, int64_t rows, int64_
     return make_map(map, base, rows, ld, box_rows);
 }
 
+qnn_status tc_map_heads(CUtensorMap *map, const void *base, int d, int heads, int64_t T, int64_t B, int64_t frame, int64_t seq, int box_rows) {
+    PFN_cuTensorMapEncodeTiled_v12000 enc = nullptr;
+    QNN_TRY(get_encode(&enc));
+    const cuuint64_t most = (cuuint64_t)1 << 40;
+    cuuint64_t dims[4] = {(cuuint64_t)d, (cuuint64_t)heads, (cuuint64_t)T, (cuuint64_t)B};
+    // (the strides of dimensions of one are any legal ones)
+    cuuint64_t strides[3] = {(cuuint64_t)(heads > 1 ? d : 64) * 2, (cuuint64_t)frame * 2, (cuuint64_t)(B > 1 ? seq : 64) * 2};
+    if (strides[0] % 16 || strides[1] % 16 || strides[2] % 16 || strides[1] >= most || strides[2] >= most || !strides[1] || !strides[2])
+        return QNN_ERR_INVALID_ARG;
+    cuuint32_t box[4] = {64, 1, (cuuint32_t)box_rows, 1}, estr[4] = {1, 1, 1, 1};
+    const CUresult r = enc(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 4, const_cast<void *>(base), dims, strides, box, estr,
+                           CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+                           CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+    return r == CUDA_SUCCESS ? QNN_OK : QNN_FAIL(QNN_ERR_CUDA);
+}
+
 qnn_status tc_map_kblocks(CUtensorMap *map, const __half *base, int64_t rows, int64_t ld, int box_rows, int box_kb) {
     PFN_cuTensorMapEncodeTiled_v12000 enc = nullptr;
     QNN_TRY(get_encode(&enc));

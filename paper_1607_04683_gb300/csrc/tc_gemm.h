@@ -35,6 +35,9 @@ qnn_status tc_map_f16(CUtensorMap *map, const __half *base, int64_t rows, int64_
 // The same matrix as [ld / 64 k-blocks][rows][64], in boxes of box_kb k-blocks x box_rows x 64: one load
 // brings box_kb consecutive k-blocks of the rows, each a swizzled tile of its own.
 qnn_status tc_map_kblocks(CUtensorMap *map, const __half *base, int64_t rows, int64_t ld, int box_rows, int box_kb);
+// bf16 values [B][T][heads][d] (strides of frames and sequences in elements, multiples of 8, as is d where there are heads), in boxes of
+// 64 values x one head x box_rows frames of one sequence, 128-byte swizzle.
+qnn_status tc_map_heads(CUtensorMap *map, const void *base, int d, int heads, int64_t T, int64_t B, int64_t frame, int64_t seq, int box_rows);
 // Default tile width of a linear product (QNN_TC_BN overrides).
 int tc_pick_bn(int64_t M, int64_t N, int64_t kp);
 // Of the candidate tile widths (widest first), the widest whose share of busy SMs over the last

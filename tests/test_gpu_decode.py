@@ -252,6 +252,71 @@ def test_linear_far_strides(qnn):
     within(host(out), y, bound)
 
 
+@pytest.fixture(params=["tc", "chunks"])
+def kernel(request, monkeypatch):
+    """One of the kernels of long bf16 sequences, whichever would be taken."""
+    monkeypatch.setenv("QNN_LINEAR", request.param)
+    return request.param
+
+
+@pytest.mark.parametrize("B,T,H,dk,dv", [(1, 9, 1, 8, 8), (1, 64, 2, 64, 64), (2, 127, 1, 16, 24), (1, 128, 3, 128, 128), (2, 129, 2, 72, 64),
+                                         (1, 255, 1, 128, 200), (1, 256, 2, 64, 72), (1, 257, 1, 48, 256), (1, 384, 1, 128, 64),
+                                         (3, 385, 2, 120, 136), (1, 1000, 2, 128, 128), (40, 140, 8, 64, 64), (5, 300, 33, 32, 128)])
+def test_linear_kernels_of_long_sequences(qnn, kernel, B, T, H, dk, dv):
+    q, k, v, decay, state = linear_inputs(B * 1000 + T * 7 + dk, B, T, H, dk, dv, "bf16")
+    a = check_linear(qnn, q, k, v, decay, state)
+    b = check_linear(qnn, q, k, v, decay, state, inplace=True)
+    assert torch.equal(a[0], b[0]) and torch.equal(a[1], b[1])
+    check_linear(qnn, q, k, v, decay)
+    check_linear(qnn, q, k, v, decay, state, padded=(8, 8))
+
+
+@pytest.mark.parametrize("heads", [(1, 1, 6), (6, 1, 1), (2, 3, 6), (1, 1, 1)])
+def test_linear_kernels_with_shared_heads(qnn, kernel, heads):
+    q, k, v, decay, state = linear_inputs(5, 2, 200, 6, 64, 128, "bf16", *heads)
+    check_linear(qnn, q, k, v, decay, state)
+
+
+@pytest.mark.parametrize("B,T", [(9, 128), (12, 300), (300, 150), (257, 20)])
+def test_linear_kernels_with_lengths(qnn, kernel, B, T):
+    """Sequences of all lengths, more of them than are sorted and than there are SMs, with anything behind their ends."""
+    g = rng(B)
+    lengths = g.integers(-3, T + 5, B)
+    lengths[:4] = [0, T, 1, T - 1]
+    q, k, v, decay, state = linear_inputs(B, B, T, 2, 32, 64, "bf16")
+    n = gpu(lengths.astype(np.int32))
+    a = check_linear(qnn, q, k, v, decay, state, lengths=n)
+    for i, x in enumerate((q, k, v)):
+        for b, m in enumerate(np.clip(lengths, 0, T)):
+            x[b, m:] = (float("nan"), float("inf"), -float("inf"))[i]
+    out, end = torch.full_like(a[0], 7.0), torch.empty_like(a[1])
+    qnn.qnn_linear_attention(q, k, v, decay, state_in=state, state_out=end, lengths=n, out=out)
+    assert torch.equal(out, a[0]) and torch.equal(end, a[1])
+
+
+@pytest.mark.parametrize("T,at", [(128, 40), (130, 129), (400, 200)])
+@pytest.mark.parametrize("bad", [float("nan"), float("inf"), -float("inf")])
+def test_linear_kernels_with_values_that_are_not_finite(qnn, kernel, T, at, bad):
+    test_linear_values_that_are_not_finite(qnn, T, at, bad, "bf16")
+
+
+def test_linear_kernels_with_decays_at_their_ends(qnn, kernel):
+    for T in (100, 300):
+        test_linear_decays_at_their_ends(qnn, T, "bf16")
+
+
+def test_linear_kernels_give_the_same_bits_again(qnn, kernel):
+    q, k, v, decay, state = linear_inputs(8, 3, 700, 60, 128, 128, "bf16")
+    lengths = gpu(np.array([700, 300, 5], np.int32))
+    outs = []
+    for _ in range(4):
+        end = torch.empty_like(state)
+        y = torch.zeros_like(v)
+        qnn.qnn_linear_attention(q, k, v, decay, state_in=state, state_out=end, lengths=lengths, out=y)
+        outs.append((y, end))
+    assert all(torch.equal(y, outs[0][0]) and torch.equal(e, outs[0][1]) for y, e in outs)
+
+
 # ------------------------------------------------------------------------------------- selection
 
 def check_select(qnn, logits, scores, n, finished=None, eos=0, alike=0.0):
