@@ -299,6 +299,7 @@ __global__ void __launch_bounds__(kThreads, EACH == 8 ? 4 : 3) beam_rows_kernel(
     __shared__ Best<Logit, EACH> best;
     __shared__ float warp_most[kWarps];
     __shared__ unsigned long long warp_sum[kWarps];
+    grid_dependents_launch();  // (the merge waits for all of this before it reads any of it)
     const int64_t row = blockIdx.x / (unsigned)a.parts;
     const int part = blockIdx.x % (unsigned)a.parts;
     const T *x = static_cast<const T *>(a.logits) + row * a.ldl;
@@ -351,7 +352,9 @@ __global__ void __launch_bounds__(kThreads, EACH == 8 ? 4 : 3) beam_rows_kernel(
 }
 
 // A batch row's continuations: each beam's log of its sum from its parts, then the n best of the parts' lists.
-// EACH: 1 while a block's threads hold all candidates one each (code that is not in a cache yet is most of a short kernel's time), else 8.
+// EACH: 1 while a block's threads hold all candidates one each, else 8. With one each a candidate's rank is counted over all of them by
+// as many threads as there are for it; a list's candidates lie in order and lists by beam and classes, so that of equal scores the first is
+// the one with the lowest index. (Code that is not in a cache yet is most of a short kernel's time.)
 template <int EACH>
 __global__ void __launch_bounds__(kThreads) beam_merge_kernel(const SelectArgs a) {
     __shared__ Best<Cand, EACH> best;
@@ -409,32 +412,52 @@ __global__ void __launch_bounds__(kThreads) beam_merge_kernel(const SelectArgs a
         }
         lse[k] = l, state[k] = (unsigned char)st, score[k] = sc;
     }
-    best.start();
-    for (int64_t base = 0; base < total; base += kThreads * EACH) {
-        Cand key[EACH], mine = none_of(Cand());
+    auto scored = [&](int k, Logit l, bool first) {
+        if (state[k] == 2 && first) return cand_key(score[k], 0.0f, {0.0f, 0.0f}, (unsigned)(k * a.V + a.eos));
+        if (state[k] == 1 && l) return cand_key(score[k], unordered((uint32_t)(l >> 32)), lse[k], (unsigned)(k * a.V + (unsigned)~(uint32_t)l));
+        return none_of(Cand());
+    };
+    if constexpr (EACH == 1) {
+        __syncthreads();
+        Cand *const all = best.list;
+        all[threadIdx.x] = threadIdx.x < total ? scored(first_k, first_logit, first_first) : none_of(Cand());
+        int share = 1;  // threads a candidate
+        while (share < 32 && 2 * share * total <= kThreads) share *= 2;
+        __syncthreads();
+        const int i = threadIdx.x / share, part = threadIdx.x % share;
+        const unsigned long long mine = i < total ? all[i].v : 0;
+        int better = 0;
+#pragma unroll 4
+        for (int j = part; j < total; j += share) better += all[j].v >= mine + (j >= i);
+        for (int m = 1; m < share; m <<= 1) better += __shfl_xor_sync(0xffffffffu, better, m);
+        const int there = __syncthreads_count(part == 0 && mine);
+        if (part == 0 && mine && better < a.n) best.ranked[better] = all[i];
+        if (threadIdx.x == 0) best.held = there < a.n ? there : a.n;
+        __syncthreads();
+    } else {
+        best.start();
+        for (int64_t base = 0; base < total; base += kThreads * EACH) {
+            Cand key[EACH], mine = none_of(Cand());
 #pragma unroll
-        for (int e = 0; e < EACH; ++e) {
-            const int64_t at = base + threadIdx.x + (int64_t)e * kThreads;
-            key[e] = none_of(Cand());
-            if (at < total) {
-                int k = first_k;
-                Logit l = first_logit;
-                const bool first = EACH == 1 ? first_first : candidate(at, k, l);
-                if (state[k] == 2) {
-                    if (first) key[e] = cand_key(score[k], 0.0f, {0.0f, 0.0f}, (unsigned)(k * a.V + a.eos));
-                } else if (state[k] == 1 && l) {
-                    key[e] = cand_key(score[k], unordered((uint32_t)(l >> 32)), lse[k], (unsigned)(k * a.V + (unsigned)~(uint32_t)l));
+            for (int e = 0; e < EACH; ++e) {
+                const int64_t at = base + threadIdx.x + (int64_t)e * kThreads;
+                key[e] = none_of(Cand());
+                if (at < total) {
+                    int k;
+                    Logit l;
+                    const bool first = candidate(at, k, l);
+                    key[e] = scored(k, l, first);
                 }
+                if (before(key[e], mine)) mine = key[e];
             }
-            if (before(key[e], mine)) mine = key[e];
+            best.take([&](int e) { return key[e]; }, mine, a.n);
         }
-        best.take([&](int e) { return key[e]; }, mine, a.n);
     }
     const int held = best.held;
     for (int i = threadIdx.x; i < a.n; i += kThreads) {
         const int64_t o = b * a.n + i;
         if (i < held) {
-            const Cand c = best.list[i];
+            const Cand c = EACH == 1 ? best.ranked[i] : best.list[i];
             a.scores_out[o] = unordered((uint32_t)(c.v >> 32));
             a.parents[o] = (int32_t)(c.index / (unsigned)a.V);
             a.tokens[o] = (int32_t)(c.index % (unsigned)a.V);

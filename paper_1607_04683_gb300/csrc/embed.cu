@@ -155,6 +155,7 @@ template <typename I>
 __global__ void __launch_bounds__(kSortThreads) sort_count_kernel(const SortArgs a) {
     __shared__ uint32_t count[kMostBins];
     const int bins = 1 << a.bits;
+    grid_dependents_launch();
     for (int i = threadIdx.x; i < bins; i += kSortThreads) count[i] = 0;
     for (int64_t i = (int64_t)blockIdx.x * kSortThreads + threadIdx.x; i < a.clear; i += (int64_t)gridDim.x * kSortThreads) a.next[i] = 0;
     __syncthreads();
@@ -170,6 +171,7 @@ __global__ void __launch_bounds__(kSortThreads) sort_place_kernel(const SortArgs
     __shared__ uint32_t place[kSortWarps][kMostBins];
     __shared__ uint32_t warp_total[kSortWarps];
     const int bins = 1 << a.bits, warp = threadIdx.x / 32, lane = threadIdx.x % 32;
+    grid_dependents_launch();
     if ((int)blockIdx.x >= a.tiles) return clear_rows(a.rows, (int)blockIdx.x - a.tiles);
     for (int i = threadIdx.x; i < kSortWarps * bins; i += kSortThreads) place[i / bins][i % bins] = 0;
     grid_dependency_wait();
@@ -273,6 +275,7 @@ template <typename I>
 __global__ void __launch_bounds__(kOneThreads, 1) sort_cluster_kernel(const SortArgs a, int passes) {
     extern __shared__ __align__(16) unsigned char raw[];
     OneShared &s = *reinterpret_cast<OneShared *>(raw);
+    grid_dependents_launch();
     const int bins = 1 << a.bits, warp = threadIdx.x / 32, lane = threadIdx.x % 32;
     const int rank = (int)cluster_rank(), blocks = a.tiles, tile = a.tile;
     if ((int)blockIdx.x >= blocks) return clear_rows(a.rows, (int)blockIdx.x - blocks);  // (whole clusters)
@@ -416,6 +419,7 @@ constexpr int kRows = 8;  // (16: 16000 x 2048 bf16 46 us, so 30)
 template <typename T, typename O, int W>
 __global__ void __launch_bounds__(kGradThreads) grad_sum_kernel(const GradArgs a) {
     const int lane = threadIdx.x % 32;
+    grid_dependents_launch();  // (each kernel of the call waits for all of the one before)
     grid_dependency_wait();
     const int64_t warp = (int64_t)blockIdx.x * (kGradThreads / 32) + threadIdx.x / 32;
     const Split s = split(warp, a.cols);

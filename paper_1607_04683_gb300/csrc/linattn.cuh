@@ -165,6 +165,7 @@ __global__ void __launch_bounds__(kLinThreads) linear_chunk_kernel(const LinearA
     unsigned char *const scores = smem + Sh::kOperands;
     float *const powers = reinterpret_cast<float *>(scores + Sh::kScores);
     const int warp = threadIdx.x / 32, lane = threadIdx.x % 32, g = lane / 4, t = lane % 4;
+    grid_dependents_launch();  // (what follows in the call waits for all of this before it reads any of it)
 
     int64_t at = blockIdx.x;
     const int tile = (int)(at % a.tiles);
@@ -301,7 +302,7 @@ __global__ void __launch_bounds__(kLinThreads) linear_chunk_kernel(const LinearA
         const bool finite = __all_sync(0xffffffffu, (zero & 0x7fff7fffu) == 0);
 
         if constexpr (!STATES) {
-            float y[MT][2][4] = {};
+            float y[MT][2][4] = {}, rest[NP == 3 ? MT : 1][2][4] = {};  // (fp32: products of second and third pieces apart, see the state)
             // q S
             const uint32_t qa = Qa + (lane % 16 * QS + lane / 16 * 8) * 2;
 #pragma unroll
@@ -320,8 +321,9 @@ __global__ void __launch_bounds__(kLinThreads) linear_chunk_kernel(const LinearA
                     each_product<NP, NH>([&](int i, int j) {
 #pragma unroll
                         for (int m = 0; m < MT; ++m) {
-                            mma_bf16(y[m][0], x[m][i], sp[0][j], sp[1][j]);
-                            mma_bf16(y[m][1], x[m][i], sp[2][j], sp[3][j]);
+                            float(&to)[2][4] = NP == 3 && i + j > 0 ? rest[NP == 3 ? m : 0] : y[m];
+                            mma_bf16(to[0], x[m][i], sp[0][j], sp[1][j]);
+                            mma_bf16(to[1], x[m][i], sp[2][j], sp[3][j]);
                         }
                     });
                 }
@@ -331,7 +333,10 @@ __global__ void __launch_bounds__(kLinThreads) linear_chunk_kernel(const LinearA
 #pragma unroll
                 for (int nt = 0; nt < 2; ++nt)
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) y[m][nt][e] = __fmul_rn(y[m][nt][e], powers[m * 16 + g + 8 * (e >> 1) + 1]);
+                    for (int e = 0; e < 4; ++e) {
+                        if constexpr (NP == 3) y[m][nt][e] = __fadd_rn(y[m][nt][e], rest[m][nt][e]), rest[m][nt][e] = 0.0f;
+                        y[m][nt][e] = __fmul_rn(y[m][nt][e], powers[m * 16 + g + 8 * (e >> 1) + 1]);
+                    }
             // scores v. A later frame's score is 0, whose product with an infinity would be a NaN in an earlier frame's output:
             // where a column holds one, the sums are formed frame by frame.
             if (!finite) {
@@ -364,10 +369,17 @@ __global__ void __launch_bounds__(kLinThreads) linear_chunk_kernel(const LinearA
                     each_product<NH, NP>([&](int i, int p) {
 #pragma unroll
                         for (int m = j; m < MT; ++m) {
-                            mma_bf16(y[m][0], x[m][i], vf[p][j][0], vf[p][j][1]);
-                            mma_bf16(y[m][1], x[m][i], vf[p][j][2], vf[p][j][3]);
+                            float(&to)[2][4] = NP == 3 && i + p > 0 ? rest[NP == 3 ? m : 0] : y[m];
+                            mma_bf16(to[0], x[m][i], vf[p][j][0], vf[p][j][1]);
+                            mma_bf16(to[1], x[m][i], vf[p][j][2], vf[p][j][3]);
                         }
                     });
+                }
+                if constexpr (NP == 3) {
+#pragma unroll
+                    for (int m = 0; m < MT; ++m)
+#pragma unroll
+                        for (int e = 0; e < 8; ++e) y[m][e / 4][e % 4] = __fadd_rn(y[m][e / 4][e % 4], rest[m][e / 4][e % 4]);
                 }
             }
             T *const out = static_cast<T *>(a.y) + b * a.y_seq + (base + g) * a.y_frame + (int64_t)h * a.dv + col0;
@@ -397,7 +409,7 @@ __global__ void __launch_bounds__(kLinThreads) linear_chunk_kernel(const LinearA
 
         // The state after the chunk. A chunk's products are added up from zero and then to the state: the matrix instruction cuts its
         // sums off (2^-24 of the largest term, always downwards), and a state that went through all of them as their accumulator
-        // came out 1e-6 low.
+        // came out 1e-6 low. For the same reason products of small pieces have a sum of their own.
         const float decay = powers[rows];
         auto weight = [&](int frame) { return powers[rows - 1 - frame > 0 ? rows - 1 - frame : 0]; };  // (frames past the last are zeros)
         uint32_t vp[MT][3][4];
@@ -418,7 +430,7 @@ __global__ void __launch_bounds__(kLinThreads) linear_chunk_kernel(const LinearA
 #pragma unroll
         for (int n0 = 0; n0 < DKP; n0 += 32) {
             if (n0 < a.dk) {
-                float sum[4][4] = {};
+                float sum[4][4] = {}, rest[NP > 1 ? 4 : 1][4] = {};
 #pragma unroll
                 for (int m = 0; m < MT; ++m) {
                     uint32_t x[NP][2][4];
@@ -428,11 +440,16 @@ __global__ void __launch_bounds__(kLinThreads) linear_chunk_kernel(const LinearA
                         ld_matrix_t(x[p][1], ka + (p * PLANE + m * 16 * QS + n0 + 16) * 2);
                     }
                     each_product<3, NP>([&](int i, int p) {
-                        mma_bf16(sum[0], vp[m][i], x[p][0][0], x[p][0][1]);
-                        mma_bf16(sum[1], vp[m][i], x[p][0][2], x[p][0][3]);
-                        mma_bf16(sum[2], vp[m][i], x[p][1][0], x[p][1][1]);
-                        mma_bf16(sum[3], vp[m][i], x[p][1][2], x[p][1][3]);
+                        const bool small = NP > 1 && i + p > 0;
+                        mma_bf16(small ? rest[0] : sum[0], vp[m][i], x[p][0][0], x[p][0][1]);
+                        mma_bf16(small ? rest[NP > 1 ? 1 : 0] : sum[1], vp[m][i], x[p][0][2], x[p][0][3]);
+                        mma_bf16(small ? rest[NP > 1 ? 2 : 0] : sum[2], vp[m][i], x[p][1][0], x[p][1][1]);
+                        mma_bf16(small ? rest[NP > 1 ? 3 : 0] : sum[3], vp[m][i], x[p][1][2], x[p][1][3]);
                     });
+                }
+                if constexpr (NP > 1) {
+#pragma unroll
+                    for (int e = 0; e < 16; ++e) sum[e / 4][e % 4] = __fadd_rn(sum[e / 4][e % 4], rest[e / 4][e % 4]);
                 }
 #pragma unroll
                 for (int j = 0; j < 4; ++j)
@@ -454,34 +471,27 @@ __global__ void __launch_bounds__(kLinThreads) linear_chunk_kernel(const LinearA
 }
 
 // From the states that the parts of a sequence end with from zeros, those that they begin with, in their place: a thread an element,
-// eight parts loaded at a time. (Of parts without frames nothing is used.)
-constexpr int kPrefixThreads = 256;
-template <bool VEC>
+// kAhead parts loaded at a time. (Of parts without frames nothing is used.)
+constexpr int kPrefixThreads = 256, kAhead = 16;
 __global__ void __launch_bounds__(kPrefixThreads) linear_prefix_kernel(const LinearArgs a) {
-    using W = typename std::conditional<VEC, float4, float>::type;
-    const int64_t size = (int64_t)a.dk * a.dv / (VEC ? 4 : 1), at = (int64_t)blockIdx.x * kPrefixThreads + threadIdx.x;
-    const int64_t unit = at / size, i = at % size;
+    grid_dependents_launch();
+    const int64_t size = (int64_t)a.dk * a.dv;
+    const Split at = split((int64_t)blockIdx.x * kPrefixThreads + threadIdx.x, size);
+    const int64_t unit = at.quot;
     if (unit >= a.B * a.H) return;
     const float over = power(head_rate(a.log_decay, (int)(unit % a.H)), (float)a.per);
-    W run = {};
-    if (a.state_in) run = reinterpret_cast<const W *>(a.state_in)[unit * size + i];
+    float run = a.state_in ? a.state_in[unit * size + at.rem] : 0.0f;
+    float *p = a.partial + unit * a.parts * size + at.rem;
     grid_dependency_wait();
-    W *p = reinterpret_cast<W *>(a.partial) + unit * a.parts * size + i;
-    for (int j0 = 0; j0 < a.parts; j0 += 8) {
-        W v[8];
+    for (int j0 = 0; j0 < a.parts; j0 += kAhead) {
+        float v[kAhead];
 #pragma unroll
-        for (int j = 0; j < 8; ++j)
-            if (j0 + j + 1 < a.parts) v[j] = p[(j0 + j) * size];
+        for (int j = 0; j < kAhead; ++j) v[j] = j0 + j + 1 < a.parts ? p[(j0 + j) * size] : 0.0f;
 #pragma unroll
-        for (int j = 0; j < 8; ++j)
+        for (int j = 0; j < kAhead; ++j)
             if (j0 + j < a.parts) {
                 p[(j0 + j) * size] = run;
-                if constexpr (VEC) {
-                    run.x = __fmaf_rn(run.x, over, v[j].x), run.y = __fmaf_rn(run.y, over, v[j].y);
-                    run.z = __fmaf_rn(run.z, over, v[j].z), run.w = __fmaf_rn(run.w, over, v[j].w);
-                } else {
-                    run = __fmaf_rn(run, over, v[j]);
-                }
+                run = __fmaf_rn(run, over, v[j]);
             }
     }
 }
@@ -512,8 +522,7 @@ template <typename T, int DKP, int C>
 qnn_status launch_parts(const LinearArgs &a, cudaStream_t st) {
     if (a.parts > 1) {
         QNN_TRY((launch_chunk<T, DKP, C, true>(a, st)));
-        const bool vec = (int64_t)a.dk * a.dv % 4 == 0 && reinterpret_cast<uintptr_t>(a.state_in) % 16 == 0;
-        const int64_t blocks = (a.B * a.H * a.dk * a.dv / (vec ? 4 : 1) + kPrefixThreads - 1) / kPrefixThreads;
+        const int64_t blocks = (a.B * a.H * a.dk * a.dv + kPrefixThreads - 1) / kPrefixThreads;
         cudaLaunchConfig_t cfg = {};
         cfg.gridDim = dim3((unsigned)blocks);
         cfg.blockDim = dim3(kPrefixThreads);
@@ -523,7 +532,7 @@ qnn_status launch_parts(const LinearArgs &a, cudaStream_t st) {
         attr.val.programmaticStreamSerializationAllowed = 1;
         cfg.attrs = &attr;
         cfg.numAttrs = 1;
-        QNN_CUDA_TRY(vec ? cudaLaunchKernelEx(&cfg, linear_prefix_kernel<true>, a) : cudaLaunchKernelEx(&cfg, linear_prefix_kernel<false>, a));
+        QNN_CUDA_TRY(cudaLaunchKernelEx(&cfg, linear_prefix_kernel, a));
     }
     return launch_chunk<T, DKP, C, false>(a, st);
 }
