@@ -295,7 +295,7 @@ __device__ __forceinline__ bool take_values(Best<Logit, EACH> &s, const float (&
 // One part of a beam's row: its sum of exponentials and its n best classes in one pass over it, tiles of kThreads EACH values
 // in registers. Within a beam the order of the logits is that of the scores, so that no score is formed here.
 template <typename T, bool VEC, int EACH>
-__global__ void __launch_bounds__(kThreads, EACH == 8 ? 4 : 3) beam_rows_kernel(const SelectArgs a) {
+__global__ void __launch_bounds__(kThreads, 4) beam_rows_kernel(const SelectArgs a) {
     __shared__ Best<Logit, EACH> best;
     __shared__ float warp_most[kWarps];
     __shared__ unsigned long long warp_sum[kWarps];

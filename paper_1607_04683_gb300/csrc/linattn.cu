@@ -217,10 +217,10 @@ extern "C" qnn_status qnn_linear_attention(const qnn_linear_args *args, void *st
     a.y_copy = copy_unit(p.y, B, T, p.H, p.dv, p.y_seq, p.y_frame, e);
     const uintptr_t ybits = reinterpret_cast<uintptr_t>(p.y) | (uintptr_t)((B > 1 ? p.y_seq * e : 0) | p.y_frame * e | (int64_t)p.dv * e);
     a.pairs = ybits % (2 * e) == 0;
-    // parts of a sequence: while the SMs have less than two blocks each, but no fewer than two chunks a part
+    // parts of a sequence: as many blocks as the SMs hold at once, but no fewer than two chunks a part
     const int chunk = linear_chunk(p.dtype, p.dk);
     const int64_t units = B * p.H * a.tiles, chunks = (T + chunk - 1) / chunk;
-    int64_t parts = std::max<int64_t>(1, std::min<int64_t>({2 * (int64_t)sm_count() / units, chunks / 2, 64}));
+    int64_t parts = std::max<int64_t>(1, std::min<int64_t>({(p.dk <= 64 ? 3 : 2) * (int64_t)sm_count() / units, chunks / 2, 64}));
     const int64_t per = (chunks + parts - 1) / parts;
     a.parts = (int)((chunks + per - 1) / per);
     a.per = per * chunk;

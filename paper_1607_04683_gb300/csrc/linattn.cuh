@@ -155,7 +155,7 @@ __device__ __forceinline__ void split_rows(const T *raw, __nv_bfloat16 *planes, 
 }
 
 template <typename T, int DKP, int C, bool STATES>
-__global__ void __launch_bounds__(kLinThreads) linear_chunk_kernel(const LinearArgs a) {
+__global__ void __launch_bounds__(kLinThreads, DKP == 64 ? 4 : DKP == 128 ? 2 : 1) linear_chunk_kernel(const LinearArgs a) {
     using Sh = ChunkShape<T, DKP, C, STATES>;
     using P16 = __nv_bfloat16;
     constexpr int NP = Sh::kPieces, NH = Sh::kHeld;
