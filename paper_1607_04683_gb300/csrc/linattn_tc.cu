@@ -584,8 +584,12 @@ qnn_status launch_tc(const LinearArgs &a, cudaStream_t st) {
 
 }  // namespace
 
+// (Tensor maps take no strides of zero, which are the inputs of one sequence or frame for all, nor any of 2^40 bytes.)
 bool linear_tc_fits(const LinearArgs &a) {
     const uintptr_t states = reinterpret_cast<uintptr_t>(a.state_in) | reinterpret_cast<uintptr_t>(a.state_out);
+    const int64_t strides[8] = {a.q_frame, a.k_frame, a.v_frame, a.y_frame, a.q_seq, a.k_seq, a.v_seq, a.y_seq};
+    for (int i = 0; i < (a.B > 1 ? 8 : 4); ++i)
+        if (strides[i] <= 0 || strides[i] >= (int64_t)1 << 39) return false;
     return a.dk <= 128 && a.dv % 8 == 0 && states % 16 == 0 && a.q_copy == 16 && a.k_copy == 16 && a.v_copy == 16 && a.y_copy == 16;
 }
 qnn_status launch_linear_tc(const LinearArgs &a, cudaStream_t st) { return a.dk <= 64 ? launch_tc<1>(a, st) : launch_tc<2>(a, st); }

@@ -305,6 +305,47 @@ def test_linear_kernels_with_decays_at_their_ends(qnn, kernel):
         test_linear_decays_at_their_ends(qnn, T, "bf16")
 
 
+@pytest.mark.parametrize("kind", KINDS)
+@pytest.mark.parametrize("T", [6, 200])
+def test_linear_inputs_in_other_orders(qnn, T, kind):
+    """Inputs of one sequence or of one frame for all, frames before sequences, and frames that overlap as windows of values."""
+    B, H, d = 3, 2, 64
+    q, k, v, decay, state = linear_inputs(T, B, T, H, d, d, kind)
+
+    def check(q, k, v, out=None):
+        y, bound, S, sbound = ref.linear(host(q), host(k), host(v), host(decay), 0.125, kind, host(state))
+        end = torch.empty_like(state)
+        got = qnn.qnn_linear_attention(q, k, v, decay, state_in=state, state_out=end, out=out)
+        within(host(got), y, bound, "y")
+        within(host(end), S, sbound, "state")
+
+    every = (B, T, H, d)
+    check(q[:1].expand(every), k, v)
+    check(q, k[:, :1].expand(every), v)
+    check(q, k, v[:1, :1].expand(every))
+    check(q[:1].expand(every), k[:1, 3:4].expand(every), v[1:2].expand(every))
+    late = [x.transpose(0, 1).contiguous().transpose(0, 1) for x in (q, k, v, v)]
+    check(*late[:3], out=late[3].clone().transpose(0, 1).contiguous().transpose(0, 1))
+    line = gpu(rng(9).normal(0, 1, (B, T * 8 + H * d)), kind)
+    check(line.as_strided(every, (line.shape[1], 8, d, 1)), k, v)
+
+
+@pytest.mark.parametrize("B", [1, 3])
+def test_linear_kernels_with_inputs_in_other_orders(qnn, kernel, B):
+    test_linear_inputs_in_other_orders(qnn, 260, "bf16")
+    q, k, v, decay, state = linear_inputs(B, B, 260, 2, 64, 64, "bf16")
+    out = torch.empty_like(v)
+    want = qnn.qnn_linear_attention(q, k, v, decay, state_in=state)
+    for x in (q, k, v):  # (values that no copy of 16 bytes takes: a frame of another length, a place in the middle)
+        wide = torch.zeros(B, 260, 2 * 64 + 3, dtype=x.dtype, device="cuda")[..., 1:-2]
+        wide.copy_(x.flatten(2))
+        put = [wide.unflatten(2, (2, 64)) if x is z else z for z in (q, k, v)]
+        got = qnn.qnn_linear_attention(*put, decay, state_in=state, out=out)
+        y, bound, _, _ = ref.linear(host(q), host(k), host(v), host(decay), 0.125, "bf16", host(state))
+        within(host(got), y, bound)
+        within(host(want), y, bound)
+
+
 def test_linear_kernels_give_the_same_bits_again(qnn, kernel):
     q, k, v, decay, state = linear_inputs(8, 3, 700, 60, 128, 128, "bf16")
     lengths = gpu(np.array([700, 300, 5], np.int32))
