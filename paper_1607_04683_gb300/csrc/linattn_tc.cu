@@ -15,6 +15,9 @@
 // Numbers. q, k and v are operands as they are. Scores and state go in as two pieces (2^-17), the scaled v as three, each rounded
 // (2^-25; two left the states 2.4e-6 off). The state's sums are fp32 in registers, a chunk's products in tensor memory.
 //
+// Bound: the products' issue and the warps' work between them, not bytes: a chunk's 48 to 64 products of 64 or 128 columns take 45 to 70 cycles
+// each, 3.3 us a chunk in all. 16 x 1000 frames x 16 heads x 128, all there, 147 us (8 chunks of 512 heads' halves on 152 SMs, 1.8 TB/s); with
+// sequences of a third to all of that 98 to 104 us; linattn.cuh's kernel takes 311 and 220.
 #include <algorithm>
 
 #include "linattn.cuh"
@@ -34,7 +37,7 @@ constexpr int kSorted = 256;
 struct TcShared {  // behind the operands
     float powers[2][kChunk + 32];  // d^0 .. from 32 on (what lies before is read for later frames, and not used)
     int bad[4][kLinCols];  // first frame of a chunk at which a column of v is not finite
-    uint64_t full[2], unit[2], k_free[2], qv_free[2], vp, vp2, v_ready, low_done, sc_full, d_full, pv_done, p_ready, s_ready, d_free, o_full[2],
+    uint64_t full[2], unit[2], k_free[2], qv_free[2], vp, vp2, v_ready, low_done, sc_full, d_full, pv_done, p_ready, s_ready, d_free, end, o_full[2],
         o_free[2];
     uint8_t order[kSorted];
     uint32_t tmem;
@@ -124,7 +127,7 @@ __global__ void __launch_bounds__(kTcThreads, 1) linear_tc_kernel(const LinearAr
         for (int i = 0; i < 2; ++i) mb_init(su32(&sh.full[i]), 1), mb_init(su32(&sh.unit[i]), 4), mb_init(su32(&sh.k_free[i]), 1), mb_init(su32(&sh.qv_free[i]), 1);
         mb_init(su32(&sh.vp), 4), mb_init(su32(&sh.vp2), 4), mb_init(su32(&sh.v_ready), 4), mb_init(su32(&sh.low_done), 1);
         mb_init(su32(&sh.sc_full), 1), mb_init(su32(&sh.d_full), 1), mb_init(su32(&sh.pv_done), 1);
-        mb_init(su32(&sh.p_ready), 8), mb_init(su32(&sh.s_ready), 4), mb_init(su32(&sh.d_free), 4);
+        mb_init(su32(&sh.p_ready), 8), mb_init(su32(&sh.s_ready), 4), mb_init(su32(&sh.d_free), 4), mb_init(su32(&sh.end), 1);
         for (int i = 0; i < 2; ++i) mb_init(su32(&sh.o_full[i]), 1), mb_init(su32(&sh.o_free[i]), 8);
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
         fence_async_smem();
@@ -469,7 +472,6 @@ __global__ void __launch_bounds__(kTcThreads, 1) linear_tc_kernel(const LinearAr
             goto done;
         }
         if (warp > 16) goto done;
-        unsigned c = 0;
         const uint32_t vs = operand(base + L::kVs, 1024), st = operand(base + L::kS, 1024);
         u.set(a, list, 0);
         int k = -1;  // chunk of the unit that QK is issued for
@@ -488,7 +490,7 @@ __global__ void __launch_bounds__(kTcThreads, 1) linear_tc_kernel(const LinearAr
             const uint32_t o = tmem + kO + s * 128, q = operand(base + L::kQ + s * KP * kPanel, 1024);
             constexpr uint32_t kv = idesc(64, true, true), pv = idesc(64, false, true), qk = idesc(128, false, false);
             if (x > 0) {
-                c = x - 1;
+                const unsigned c = x - 1;
                 if (!all_wait(vp, c & 1) || (c > 0 && !all_wait(d_free, (c - 1) & 1))) goto issued;
                 tc_after();
                 uint32_t x0 = kc, x1 = vs;
@@ -547,14 +549,15 @@ __global__ void __launch_bounds__(kTcThreads, 1) linear_tc_kernel(const LinearAr
                     }
                 }
                 if (more) commit_elected(sc_full);
-                if (x > 0) commit_elected(o_full0 + 8 * s), ++c;
+                if (x > 0) commit_elected(o_full0 + 8 * s);
             }
             if (!more) break;
             more = next_chunk();
         }
     issued:
-        // (nothing of this thread's is in flight when the tensor memory is given back)
-        if (c > 0 && !*reinterpret_cast<volatile int *>(&sh.abort)) wait(o_full0 + 8 * ((c - 1) & 1), ((c - 1) >> 1) & 1);
+        // (no product is in flight when the tensor memory is given back, after a wait that gave up neither)
+        commit_elected(su32(&sh.end));
+        mbar_wait_bounded(su32(&sh.end), 0, status, kTcWaitNs);
     }
 done:
     tc_before();

@@ -18,6 +18,7 @@ full-precision parameters, which are quantized again at the next forward pass.
 from __future__ import annotations
 
 import torch
+from torch.autograd.function import once_differentiable
 
 from . import qnn
 
@@ -87,15 +88,16 @@ class _Embedding(torch.autograd.Function):
         return qnn.qnn_embedding(ids, table.detach(), scale=scale, dtype=dtype)
 
     @staticmethod
+    @once_differentiable
     def backward(ctx, gy):
         ids, = ctx.saved_tensors
         return qnn.qnn_embedding_grad(gy.contiguous(), ids, ctx.rows, scale=ctx.scale, dtype=ctx.dtype), None, None, None
 
 
 class Embedding(torch.nn.Module):
-    """Labels' rows of a trained table, times scale: the
-    input of layers that take labels, a full-precision layer in Algorithm 1's sense. Labels below 0 are padding: rows of zeros, no
-    gradient. The gradient is dense, its rows summed in an order that depends on the labels only."""
+    """Labels' rows of a trained table, times scale: the input of layers that take labels, a full-precision layer in Algorithm 1's
+    sense. Labels below 0 are padding: rows of zeros, no gradient. The gradient is dense, its rows summed in an order that
+    depends on the labels only; it has no gradient of its own."""
 
     def __init__(self, rows: int, dim: int, scale: float = 1.0, dtype: torch.dtype = torch.float32, device="cuda"):
         super().__init__()

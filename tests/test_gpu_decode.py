@@ -662,6 +662,15 @@ def test_embedding_module(qnn):
 
 # ------------------------------------------------------------------------------- as they are used
 
+def test_embedding_module_has_no_second_gradient(qnn):
+    from paper_1607_04683_gb300 import qat
+    emb = qat.Embedding(5, 4)
+    y = emb(torch.tensor([1, 2, 1], device="cuda"))
+    grad, = torch.autograd.grad((y ** 3).sum(), emb.weight, create_graph=True)
+    with pytest.raises(RuntimeError):
+        grad.sum().backward()
+
+
 def decoder(qnn, seed, K):
     from paper_1607_04683_gb300 import inputs
     wl = inputs.LstmWorkload(f"decoder_{seed}", seed=seed, num_layers=2, input_dim=24, hidden=32, proj=0, num_classes=50, batch=2,
