@@ -6,6 +6,7 @@
 #include "elem.cuh"
 #include "qnn_device.cuh"
 #include "qnn_host.h"
+#include "tc_ptx.cuh"
 
 namespace qnn {
 namespace {
@@ -293,22 +294,19 @@ __device__ __forceinline__ bool take_values(Best<Logit, EACH> &s, const float (&
 }
 
 // One part of a beam's row: its sum of exponentials and its n best classes in one pass over it, tiles of kThreads EACH values
-// in registers. Within a beam the order of the logits is that of the scores, so that no score is formed here.
+// in registers. Within a beam the order of the logits is that of the scores, so that no score is formed here. The result is thread
+// 0's, the classes lie in best.list.
+template <int EACH>
+struct RowShared {
+    Best<Logit, EACH> best;
+    float warp_most[kWarps];
+    unsigned long long warp_sum[kWarps];
+};
 template <typename T, bool VEC, int EACH>
-__global__ void __launch_bounds__(kThreads, 4) beam_rows_kernel(const SelectArgs a) {
-    __shared__ Best<Logit, EACH> best;
-    __shared__ float warp_most[kWarps];
-    __shared__ unsigned long long warp_sum[kWarps];
-    grid_dependents_launch();  // (the merge waits for all of this before it reads any of it)
-    const int64_t row = blockIdx.x / (unsigned)a.parts;
-    const int part = blockIdx.x % (unsigned)a.parts;
-    const T *x = static_cast<const T *>(a.logits) + row * a.ldl;
-    const int64_t lo = part * a.per, hi = lo + a.per < a.V ? lo + a.per : a.V;
+__device__ __forceinline__ RowPart look_at(const T *x, int64_t lo, int64_t hi, int n, RowShared<EACH> &sh) {
     float v[EACH], most = -INFINITY, sum = 0.0f;
-    const float score = a.scores[row];
-    if ((a.finished && a.finished[row]) || !(score > -INFINITY)) return;  // (nothing of this row is looked at)
     load_tile<T, VEC, EACH>(x, lo, hi, v);
-    best.start();
+    sh.best.start();
     for (int64_t base = lo; base < hi; base += kThreads * EACH) {
         if (base > lo) load_tile<T, VEC, EACH>(x, base, hi, v);
         float top = v[0];
@@ -318,146 +316,106 @@ __global__ void __launch_bounds__(kThreads, 4) beam_rows_kernel(const SelectArgs
         const float from = most > -INFINITY ? most : 0.0f;
 #pragma unroll
         for (int e = 0; e < EACH; ++e) sum = __fadd_rn(sum, exp_term(__fsub_rn(v[e], from)));
-        if (!take_values<VEC, EACH>(best, v, top, base, a.n)) {
+        if (!take_values<VEC, EACH>(sh.best, v, top, base, n)) {
             unsigned first = 0;
 #pragma unroll
             for (int e = EACH - 1; e >= 0; --e)
                 if (v[e] == top) first = (unsigned)place<VEC>(base, e);
-            best.take([&](int e) { return logit_key(v[e], (unsigned)place<VEC>(base, e)); }, logit_key(top, first), a.n);
+            sh.best.take([&](int e) { return logit_key(v[e], (unsigned)place<VEC>(base, e)); }, logit_key(top, first), n);
         }
     }
     // the block's maximum, then the sums' parts of it
     const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
     float m = warp_max(most);
-    if (lane == 0) warp_most[warp] = m;
+    if (lane == 0) sh.warp_most[warp] = m;
     __syncthreads();
-    m = warp_most[0];
+    m = sh.warp_most[0];
 #pragma unroll
-    for (int i = 1; i < kWarps; ++i) m = fmaxf(m, warp_most[i]);
+    for (int i = 1; i < kWarps; ++i) m = fmaxf(m, sh.warp_most[i]);
     const float share = most > -INFINITY ? __fmul_rn(sum, exp_term(__fsub_rn(most, m))) : sum;  // (NaNs pass through)
     const bool bad = !(share >= 0.0f && share < INFINITY);
     unsigned long long s = bad ? 0 : __float2ull_rn(__fmul_rn(share, 4294967296.0f));
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
-    if (lane == 0) warp_sum[warp] = s;
+    if (lane == 0) sh.warp_sum[warp] = s;
     const int any_bad = __syncthreads_or(bad);
-    const int held = best.held;
-    Logit *keys = a.keys + (row * a.parts + part) * a.n;
-    for (int i = threadIdx.x; i < held; i += kThreads) keys[i] = best.list[i];
-    if (threadIdx.x == 0) {
-        s = 0;
-        for (int i = 0; i < kWarps; ++i) s += warp_sum[i];
-        a.parts_of[row * a.parts + part] = {any_bad ? ~0ull : s, m, held};
-    }
+    s = 0;
+    for (int i = 0; i < kWarps; ++i) s += sh.warp_sum[i];
+    return {any_bad ? ~0ull : s, m, sh.best.held};
+}
+// A beam that is not finished and not lost has its logits looked at.
+__device__ __forceinline__ bool looked_at(const SelectArgs &a, int64_t row) {
+    return !(a.finished && a.finished[row]) && a.scores[row] > -INFINITY;
 }
 
-// A batch row's continuations: each beam's log of its sum from its parts, then the n best of the parts' lists.
-// EACH: 1 while a block's threads hold all candidates one each, else 8. With one each a candidate's rank is counted over all of them by
-// as many threads as there are for it; a list's candidates lie in order and lists by beam and classes, so that of equal scores the first is
-// the one with the lowest index. (Code that is not in a cache yet is most of a short kernel's time.)
-template <int EACH>
-__global__ void __launch_bounds__(kThreads) beam_merge_kernel(const SelectArgs a) {
-    __shared__ Best<Cand, EACH> best;
-    __shared__ Two lse[kMostBeams];
-    __shared__ unsigned char state[kMostBeams];  // 0: no candidates, 1: its parts' lists, 2: finished
-    __shared__ float score[kMostBeams];
-    const int64_t b = blockIdx.x;
-    const int K = (int)a.K;
-    const int64_t total = (int64_t)K * a.parts * a.n;
-    // a candidate's beam, and its logit where its list has one (whatever is in memory for a row that nothing was looked for in)
-    auto candidate = [&](int64_t at, int &k, Logit &logit) {
-        const unsigned list = (unsigned)at / (unsigned)a.n, i = (unsigned)at % (unsigned)a.n;
-        k = (int)(list / (unsigned)a.parts);
-        const int64_t of = b * K * a.parts + list;
-        const int held = a.parts_of[of].held;
-        logit = a.keys[of * a.n + i];
-        if ((int)i >= held) logit = 0;
-        return list == (unsigned)k * (unsigned)a.parts && i == 0;  // the beam's first
-    };
-    grid_dependency_wait();
-    int first_k = 0;
-    Logit first_logit = 0;
-    bool first_first = false;
-    if (EACH == 1 && threadIdx.x < total) first_first = candidate(threadIdx.x, first_k, first_logit);
-    for (int k = threadIdx.x; k < K; k += kThreads) {
-        const int64_t row = b * K + k;
-        const float sc = a.scores[row];
-        const RowPart part0 = a.parts_of[row * a.parts];
-        int st = 0;
-        Two l = {0.0f, 0.0f};
-        if (sc > -INFINITY) {
-            if (a.finished && a.finished[row]) {
-                st = 2;
-            } else {
-                const RowPart *p = a.parts_of + row * a.parts;
-                float m = part0.most;
-                bool bad = part0.sum == ~0ull;
-                for (int i = 1; i < a.parts; ++i) m = fmaxf(m, p[i].most), bad |= p[i].sum == ~0ull;
-                if (!bad && m > -INFINITY && m < INFINITY) {
-                    Two s = {0.0f, 0.0f};
-                    for (int i = 0; i < a.parts; ++i) {
-                        const RowPart of = i == 0 ? part0 : p[i];
-                        const float d = __fsub_rn(of.most, m);  // (below -80 a part counts for nothing)
-                        if (d < -80.0f) continue;
-                        const unsigned long long whole = of.sum;
-                        const float hi = __ull2float_rn(whole);
-                        const Two share = {__fmul_rn(hi, 0x1p-32f),
-                                           __fmul_rn(__ll2float_rn((long long)(whole - (unsigned long long)hi)), 0x1p-32f)};
-                        s = add(s, d == 0.0f ? share : mul(share, exp_two(two_sum(of.most, -m))));
+template <typename T, bool VEC, int EACH>
+__global__ void __launch_bounds__(kThreads, 4) beam_rows_kernel(const SelectArgs a) {
+    __shared__ RowShared<EACH> sh;
+    grid_dependents_launch();  // (the merge waits for all of this before it reads any of it)
+    const int64_t row = blockIdx.x / (unsigned)a.parts;
+    const int part = blockIdx.x % (unsigned)a.parts;
+    if (!looked_at(a, row)) return;
+    const int64_t lo = part * a.per, hi = lo + a.per < a.V ? lo + a.per : a.V;
+    const RowPart of = look_at<T, VEC, EACH>(static_cast<const T *>(a.logits) + row * a.ldl, lo, hi, a.n, sh);
+    Logit *keys = a.keys + (row * a.parts + part) * a.n;
+    for (int i = threadIdx.x; i < of.held; i += kThreads) keys[i] = sh.best.list[i];
+    if (threadIdx.x == 0) a.parts_of[row * a.parts + part] = of;
+}
+
+// A batch row's beams: each one's score and the log of its sum from its parts.
+struct Beams {
+    Two lse[kMostBeams];
+    unsigned char state[kMostBeams];  // 0: no candidates, 1: its parts' lists, 2: finished
+    float score[kMostBeams];
+
+    // parts: those of the batch row's first beam, then of its next (whatever is in memory for a row that nothing was looked for in).
+    // By thread k for beam k; seen behind a barrier.
+    __device__ __forceinline__ void set(const SelectArgs &a, int64_t b, const RowPart *parts) {
+        for (int k = threadIdx.x; k < a.K; k += kThreads) {
+            const int64_t row = b * a.K + k;
+            const float sc = a.scores[row];
+            const RowPart *p = parts + (int64_t)k * a.parts, part0 = p[0];
+            int st = 0;
+            Two l = {0.0f, 0.0f};
+            if (sc > -INFINITY) {
+                if (a.finished && a.finished[row]) {
+                    st = 2;
+                } else {
+                    float m = part0.most;
+                    bool bad = part0.sum == ~0ull;
+                    for (int i = 1; i < a.parts; ++i) m = fmaxf(m, p[i].most), bad |= p[i].sum == ~0ull;
+                    if (!bad && m > -INFINITY && m < INFINITY) {
+                        Two s = {0.0f, 0.0f};
+                        for (int i = 0; i < a.parts; ++i) {
+                            const RowPart of = i == 0 ? part0 : p[i];
+                            const float d = __fsub_rn(of.most, m);  // (below -80 a part counts for nothing)
+                            if (d < -80.0f) continue;
+                            const unsigned long long whole = of.sum;
+                            const float hi = __ull2float_rn(whole);
+                            const Two share = {__fmul_rn(hi, 0x1p-32f),
+                                               __fmul_rn(__ll2float_rn((long long)(whole - (unsigned long long)hi)), 0x1p-32f)};
+                            s = add(s, d == 0.0f ? share : mul(share, exp_two(two_sum(of.most, -m))));
+                        }
+                        l = add({m, 0.0f}, log_two(s));
+                        st = 1;
                     }
-                    l = add({m, 0.0f}, log_two(s));
-                    st = 1;
                 }
             }
+            lse[k] = l, state[k] = (unsigned char)st, score[k] = sc;
         }
-        lse[k] = l, state[k] = (unsigned char)st, score[k] = sc;
     }
-    auto scored = [&](int k, Logit l, bool first) {
+    // The candidate of beam k's logit l (0: none, and the finished beam's own for its first).
+    __device__ __forceinline__ Cand scored(const SelectArgs &a, int k, Logit l, bool first) const {
         if (state[k] == 2 && first) return cand_key(score[k], 0.0f, {0.0f, 0.0f}, (unsigned)(k * a.V + a.eos));
         if (state[k] == 1 && l) return cand_key(score[k], unordered((uint32_t)(l >> 32)), lse[k], (unsigned)(k * a.V + (unsigned)~(uint32_t)l));
         return none_of(Cand());
-    };
-    if constexpr (EACH == 1) {
-        __syncthreads();
-        Cand *const all = best.list;
-        all[threadIdx.x] = threadIdx.x < total ? scored(first_k, first_logit, first_first) : none_of(Cand());
-        int share = 1;  // threads a candidate
-        while (share < 32 && 2 * share * total <= kThreads) share *= 2;
-        __syncthreads();
-        const int i = threadIdx.x / share, part = threadIdx.x % share;
-        const unsigned long long mine = i < total ? all[i].v : 0;
-        int better = 0;
-#pragma unroll 4
-        for (int j = part; j < total; j += share) better += all[j].v >= mine + (j >= i);
-        for (int m = 1; m < share; m <<= 1) better += __shfl_xor_sync(0xffffffffu, better, m);
-        const int there = __syncthreads_count(part == 0 && mine);
-        if (part == 0 && mine && better < a.n) best.ranked[better] = all[i];
-        if (threadIdx.x == 0) best.held = there < a.n ? there : a.n;
-        __syncthreads();
-    } else {
-        best.start();
-        for (int64_t base = 0; base < total; base += kThreads * EACH) {
-            Cand key[EACH], mine = none_of(Cand());
-#pragma unroll
-            for (int e = 0; e < EACH; ++e) {
-                const int64_t at = base + threadIdx.x + (int64_t)e * kThreads;
-                key[e] = none_of(Cand());
-                if (at < total) {
-                    int k;
-                    Logit l;
-                    const bool first = candidate(at, k, l);
-                    key[e] = scored(k, l, first);
-                }
-                if (before(key[e], mine)) mine = key[e];
-            }
-            best.take([&](int e) { return key[e]; }, mine, a.n);
-        }
     }
-    const int held = best.held;
+};
+__device__ __forceinline__ void put_selected(const SelectArgs &a, int64_t b, const Cand *best, int held) {
     for (int i = threadIdx.x; i < a.n; i += kThreads) {
         const int64_t o = b * a.n + i;
         if (i < held) {
-            const Cand c = EACH == 1 ? best.ranked[i] : best.list[i];
+            const Cand c = best[i];
             a.scores_out[o] = unordered((uint32_t)(c.v >> 32));
             a.parents[o] = (int32_t)(c.index / (unsigned)a.V);
             a.tokens[o] = (int32_t)(c.index % (unsigned)a.V);
@@ -468,27 +426,150 @@ __global__ void __launch_bounds__(kThreads) beam_merge_kernel(const SelectArgs a
         }
     }
 }
-
-template <typename T, int EACH>
-qnn_status launch_rows(const SelectArgs &a, int64_t rows, cudaStream_t st) {
-    const bool vec = reinterpret_cast<uintptr_t>(a.logits) % 16 == 0 && a.ldl * (int64_t)sizeof(T) % 16 == 0;
-    const auto kern = vec ? beam_rows_kernel<T, true, EACH> : beam_rows_kernel<T, false, EACH>;
-    kern<<<(unsigned)(rows * a.parts), kThreads, 0, st>>>(a);
-    QNN_CUDA_TRY(cudaGetLastError());
-    return QNN_OK;
+// A batch row's candidate `at`: the beam and, where its list has one, its logit. True for the beam's first.
+__device__ __forceinline__ bool candidate(const SelectArgs &a, const RowPart *parts, const Logit *keys, unsigned at, int &k, Logit &logit) {
+    const unsigned list = at / (unsigned)a.n, i = at % (unsigned)a.n;
+    k = (int)(list / (unsigned)a.parts);
+    const int held = parts[list].held;
+    logit = keys[at];
+    if ((int)i >= held) logit = 0;
+    return list == (unsigned)k * (unsigned)a.parts && i == 0;
 }
 
-template <typename T>
-qnn_status launch_select(const SelectArgs &a, int each, int64_t rows, int64_t B, cudaStream_t st) {
-    QNN_TRY(each == 8 ? (launch_rows<T, 8>(a, rows, st)) : (launch_rows<T, 32>(a, rows, st)));
+// A batch row's continuations, where a block's threads hold all candidates one each: a candidate's rank is counted over all of
+// them by as many threads as there are for it; a list's candidates lie in order and lists by beam and classes, so that of equal scores the
+// first is the one with the lowest index. (Code that is not in a cache yet is most of a short kernel's time.)
+struct FewShared {
+    Beams beams;
+    Cand all[kThreads], ranked[kMostKept];
+};
+__device__ __forceinline__ void select_of_few(const SelectArgs &a, int64_t b, const RowPart *parts, const Logit *keys, FewShared &sh) {
+    const int total = (int)a.K * a.parts * a.n;
+    int k = 0;
+    Logit logit = 0;
+    bool first = false;
+    if ((int)threadIdx.x < total) first = candidate(a, parts, keys, threadIdx.x, k, logit);
+    sh.beams.set(a, b, parts);
+    __syncthreads();
+    sh.all[threadIdx.x] = (int)threadIdx.x < total ? sh.beams.scored(a, k, logit, first) : none_of(Cand());
+    int share = 1;  // threads a candidate
+    while (share < 32 && 2 * share * total <= kThreads) share *= 2;
+    __syncthreads();
+    const int i = threadIdx.x / share, part = threadIdx.x % share;
+    const unsigned long long mine = i < total ? sh.all[i].v : 0;
+    int better = 0;
+#pragma unroll 4
+    for (int j = part; j < total; j += share) better += sh.all[j].v >= mine + (j >= i);
+    for (int m = 1; m < share; m <<= 1) better += __shfl_xor_sync(0xffffffffu, better, m);
+    const int there = __syncthreads_count(part == 0 && mine);
+    if (part == 0 && mine && better < a.n) sh.ranked[better] = sh.all[i];
+    __syncthreads();
+    put_selected(a, b, sh.ranked, there < a.n ? there : a.n);
+}
+
+// The merge of what rows' blocks left in memory. EACH: 1 as above, else a thread takes 8 candidates at a time.
+template <int EACH>
+__global__ void __launch_bounds__(kThreads) beam_merge_kernel(const SelectArgs a) {
+    const int64_t b = blockIdx.x, list0 = b * a.K * a.parts;
+    const RowPart *const parts = a.parts_of + list0;
+    const Logit *const keys = a.keys + list0 * a.n;
+    grid_dependency_wait();
+    if constexpr (EACH == 1) {
+        __shared__ FewShared sh;
+        select_of_few(a, b, parts, keys, sh);
+    } else {
+        __shared__ Best<Cand, EACH> best;
+        __shared__ Beams beams;
+        const int64_t total = a.K * a.parts * a.n;
+        beams.set(a, b, parts);
+        best.start();
+        for (int64_t base = 0; base < total; base += kThreads * EACH) {
+            Cand key[EACH], mine = none_of(Cand());
+#pragma unroll
+            for (int e = 0; e < EACH; ++e) {
+                const int64_t at = base + threadIdx.x + (int64_t)e * kThreads;
+                key[e] = none_of(Cand());
+                if (at < total) {
+                    int k;
+                    Logit l;
+                    const bool first = candidate(a, parts, keys, (unsigned)at, k, l);
+                    key[e] = beams.scored(a, k, l, first);
+                }
+                if (before(key[e], mine)) mine = key[e];
+            }
+            best.take([&](int e) { return key[e]; }, mine, a.n);
+        }
+        put_selected(a, b, best.list, best.held);
+    }
+}
+
+// Both in one launch where a batch row's parts are a cluster of blocks and the candidates few: lists and sums go to the
+// first block's shared memory. 128 x 8 x 8192 bf16 20.5 us a call, by two launches 27; 1 x 4 x 2000 fp32 18.5 and 22 (most of it
+// the call on the host).
+constexpr int kMostCluster = 8;
+template <int EACH>
+struct ClusterShared {
+    RowShared<EACH> row;
+    FewShared few;
+    Logit keys[kThreads];
+    RowPart parts[kMostCluster];
+};
+__device__ __forceinline__ void store_remote64(uint32_t addr, unsigned long long v) {
+    asm volatile("st.shared::cluster.u64 [%0], %1;" ::"r"(addr), "l"(v) : "memory");
+}
+__device__ __forceinline__ void cluster_arrive() { asm volatile("barrier.cluster.arrive.relaxed.aligned;" ::: "memory"); }
+__device__ __forceinline__ void cluster_wait() { asm volatile("barrier.cluster.wait.aligned;" ::: "memory"); }
+template <typename T, bool VEC, int EACH>
+__global__ void __launch_bounds__(kThreads, 4) beam_cluster_kernel(const SelectArgs a) {
+    extern __shared__ __align__(16) unsigned char raw[];
+    ClusterShared<EACH> &sh = *reinterpret_cast<ClusterShared<EACH> *>(raw);
+    const unsigned blocks = (unsigned)a.K * (unsigned)a.parts, rank = blockIdx.x % blocks, part = rank % (unsigned)a.parts;
+    const int64_t b = blockIdx.x / blocks, row = b * a.K + rank / (unsigned)a.parts;
+    cluster_arrive();  // (the first block has to run before the others write into its memory)
+    const bool there = looked_at(a, row);
+    RowPart of;
+    if (there) {
+        const int64_t lo = part * a.per, hi = lo + a.per < a.V ? lo + a.per : a.V;
+        of = look_at<T, VEC, EACH>(static_cast<const T *>(a.logits) + row * a.ldl, lo, hi, a.n, sh.row);
+    }
+    cluster_wait();
+    if (there) {
+        const uint32_t keys = cluster_addr(su32(&sh.keys[rank * a.n]), 0), to = cluster_addr(su32(&sh.parts[rank]), 0);
+        for (int i = threadIdx.x; i < of.held; i += kThreads) store_remote64(keys + 8 * i, sh.row.best.list[i]);
+        if (threadIdx.x == 0) {
+            store_remote64(to, of.sum);
+            store_remote64(to + 8, (unsigned long long)(uint32_t)of.held << 32 | __float_as_uint(of.most));
+        }
+    }
+    cluster_sync();
+    if (rank == 0) select_of_few(a, b, sh.parts, sh.keys, sh.few);
+}
+
+bool in_cluster(const SelectArgs &a) { return a.K * a.parts <= kMostCluster && a.K * a.parts * a.n <= kThreads; }
+
+template <typename T, int EACH>
+qnn_status launch_select(const SelectArgs &a, bool vec, int64_t B, cudaStream_t st) {
+    const int64_t blocks = B * a.K * a.parts;
     cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3((unsigned)B);
+    cfg.gridDim = dim3((unsigned)blocks);
     cfg.blockDim = dim3(kThreads);
     cfg.stream = st;
-    cudaLaunchAttribute attr[1];
-    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-    attr[0].val.programmaticStreamSerializationAllowed = 1;
-    cfg.attrs = attr;
+    cudaLaunchAttribute attr;
+    cfg.attrs = &attr;
+    if (in_cluster(a)) {
+        const auto kern = vec ? beam_cluster_kernel<T, true, EACH> : beam_cluster_kernel<T, false, EACH>;
+        cfg.dynamicSmemBytes = sizeof(ClusterShared<EACH>);
+        static_assert(sizeof(ClusterShared<EACH>) <= 48 * 1024);  // (what a launch has without asking)
+        attr.id = cudaLaunchAttributeClusterDimension;
+        attr.val.clusterDim.x = (unsigned)(a.K * a.parts), attr.val.clusterDim.y = attr.val.clusterDim.z = 1;
+        cfg.numAttrs = 1;
+        QNN_CUDA_TRY(cudaLaunchKernelEx(&cfg, kern, a));
+        return QNN_OK;
+    }
+    QNN_CUDA_TRY(vec ? cudaLaunchKernelEx(&cfg, beam_rows_kernel<T, true, EACH>, a) : cudaLaunchKernelEx(&cfg, beam_rows_kernel<T, false, EACH>, a));
+    attr.id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr.val.programmaticStreamSerializationAllowed = 1;
+    cfg.gridDim = dim3((unsigned)B);
     cfg.numAttrs = 1;
     QNN_CUDA_TRY(a.K * a.parts * a.n <= kThreads ? cudaLaunchKernelEx(&cfg, beam_merge_kernel<1>, a) : cudaLaunchKernelEx(&cfg, beam_merge_kernel<8>, a));
     return QNN_OK;
@@ -591,7 +672,7 @@ extern "C" qnn_status qnn_beam_select(const void *logits, int64_t ldl, int dtype
         for (int j = 0; j < i; ++j)
             if (out[i].meets(out[j])) return QNN_ERR_INVALID_ARG;
     }
-    SelectArgs a;
+    SelectArgs a = {};
     a.logits = logits, a.ldl = ldl, a.scores = scores, a.finished = finished, a.scores_out = scores_out, a.parents = parents;
     a.tokens = tokens, a.K = K, a.V = V, a.n = n, a.eos = eos;
     // Tiles of 8192 classes where those alone give the SMs two blocks each, else of 2048; a part of a row is as many tiles as leave
@@ -606,14 +687,17 @@ extern "C" qnn_status qnn_beam_select(const void *logits, int64_t ldl, int dtype
     a.parts = (int)parts, a.per = per * tile;
     cudaStream_t st = as_stream(stream);
     Scratch scratch;
-    const size_t keys = (size_t)(rows * parts * n) * sizeof(Logit);
-    QNN_TRY(scratch.take(keys + (size_t)(rows * parts) * sizeof(RowPart), st));
-    a.keys = static_cast<Logit *>(scratch.ptr());
-    a.parts_of = reinterpret_cast<RowPart *>(static_cast<char *>(scratch.ptr()) + keys);
+    if (!in_cluster(a)) {
+        const size_t keys = (size_t)(rows * parts * n) * sizeof(Logit);
+        QNN_TRY(scratch.take(keys + (size_t)(rows * parts) * sizeof(RowPart), st));
+        a.keys = static_cast<Logit *>(scratch.ptr());
+        a.parts_of = reinterpret_cast<RowPart *>(static_cast<char *>(scratch.ptr()) + keys);
+    }
+    const bool vec = reinterpret_cast<uintptr_t>(logits) % 16 == 0 && ldl * e % 16 == 0;
     ProfScope prof("beam_select", st);
-    QNN_TRY(with_type(dtype, [&](auto t) { return launch_select<decltype(t)>(a, each, rows, B, st); }));
-    QNN_CUDA_TRY(cudaGetLastError());
-    return QNN_OK;
+    return with_type(dtype, [&](auto t) {
+        return each == 8 ? launch_select<decltype(t), 8>(a, vec, B, st) : launch_select<decltype(t), 32>(a, vec, B, st);
+    });
 }
 
 extern "C" qnn_status qnn_beam_reorder(const qnn_beam_state *states, int32_t count, const int32_t *parents, int64_t B, int64_t K,

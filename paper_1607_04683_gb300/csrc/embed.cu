@@ -415,7 +415,7 @@ __device__ __forceinline__ int64_t bound(const uint32_t *ids, int64_t lo, int64_
 // A warp adds the rows of a chunk of sorted positions, 32 lanes' columns of them, in the order of the positions, kRows loads in
 // flight. A run of one label that lies within the chunk is written out; what began before it or goes on behind it is kept for the
 // second kernel. Rows that no position has were cleared while the labels were sorted.
-constexpr int kRows = 8;  // (16: 16000 x 2048 bf16 46 us, so 30)
+constexpr int kRows = 4;  // (2: 16000 x 2048 bf16 32 us, 8: 35, 16: 46, so 29.5; 60000 x 512 fp32 51, 45, so 44)
 template <typename T, typename O, int W>
 __global__ void __launch_bounds__(kGradThreads) grad_sum_kernel(const GradArgs a) {
     const int lane = threadIdx.x % 32;
@@ -628,18 +628,19 @@ qnn_status launch_sort(const void *ids, int64_t n, int64_t V, const SortPlan &p,
     return QNN_OK;
 }
 
+// The runs over several chunks are joined by W columns a lane, 4 at most.
 template <typename T, typename O, int W>
 qnn_status launch_grad(GradArgs a, cudaStream_t st) {
-    constexpr int kWarps = kGradThreads / 32;
+    constexpr int kWarps = kGradThreads / 32, kJoin = W < 4 ? W : 4;
     a.cols = (a.D / W + 31) / 32;
     const int64_t sums = (a.chunks * a.cols + kWarps - 1) / kWarps;
-    if (a.chunks * a.cols > INT32_MAX) return QNN_FAIL(QNN_ERR_INVALID_ARG);
     cudaLaunchAttribute attr;
     cudaLaunchConfig_t cfg = after(sums, kGradThreads, st, &attr);
     QNN_CUDA_TRY(cudaLaunchKernelEx(&cfg, grad_sum_kernel<T, O, W>, a));
     if (a.chunks > 1) {
+        a.cols = (a.D / kJoin + 31) / 32;
         cfg = after((a.chunks + kJoinWarps - 1) / kJoinWarps * a.cols, 32 * kJoinWarps, st, &attr);
-        QNN_CUDA_TRY(cudaLaunchKernelEx(&cfg, grad_join_kernel<O, W>, a));
+        QNN_CUDA_TRY(cudaLaunchKernelEx(&cfg, grad_join_kernel<O, kJoin>, a));
     }
     return QNN_OK;
 }
@@ -648,6 +649,10 @@ template <typename T, typename O>
 qnn_status launch_grad(const GradArgs &a, cudaStream_t st) {
     const int t = sizeof(T), o = sizeof(O);
     auto whole = [&](int v) { return a.D % v == 0 && runs_ok(a.grad, a.ldg, t, v) && runs_ok(a.out, a.ldo, o, v); };
+    if constexpr (sizeof(T) == 2) {
+        // (16 bytes a load where warps are many all the same: 16000 x 2048 43 us, so 50, 8000 x 1024 27 and 29, 2000 x 2048 29 and 28)
+        if (whole(8) && a.chunks * (a.D / 256) >= 4 * (int64_t)sm_count()) return launch_grad<T, O, 8>(a, st);
+    }
     if (whole(4)) return launch_grad<T, O, 4>(a, st);
     return launch_grad<T, O, 1>(a, st);
 }
@@ -707,6 +712,7 @@ extern "C" qnn_status qnn_embedding_grad(const void *grad, int64_t ldg, int dtyp
     // chunks of 32 positions, of 128 from 2^17 on: a label that most positions have leaves that many sums to join
     a.rounds = n < 1 << 17 ? 1 : 4;
     a.chunks = (n + 32 * a.rounds - 1) / (32 * a.rounds);
+    if (a.chunks > INT32_MAX / ((D + 31) / 32)) return QNN_ERR_INVALID_ARG;
     cudaStream_t st = as_stream(stream);
     ClearArgs clear = {};
     if (!add) {

@@ -6,7 +6,7 @@
 //   warps 0 - 7    scores from tensor memory, times their decays, back into it as pairs of bf16 pieces; outputs;
 //   warps 8 - 11   the state, a row of 64 columns a thread in registers, and its two bf16 pieces for QS;
 //   warps 12 - 15  v times its decays in three pieces (two buffers: the last piece first, and the middle one in its place);
-//   warp 16        one thread issues the products, in the order KV, PV, QS and the next chunk's QK;
+//   warp 16        issues the products, in the order KV, PV, QS and the next chunk's QK;
 //   warp 17        one thread has the operands copied (TMA, two stages).
 // While KV runs, scores are worked on; while PV and QS do, the state and the next v; outputs behind the next scores.
 // k, v, the scaled v and the state lie in rows of 64 values (128 bytes, swizzled): read along rows they are one operand's layout, across
@@ -15,9 +15,9 @@
 // Numbers. q, k and v are operands as they are. Scores and state go in as two pieces (2^-17), the scaled v as three, each rounded
 // (2^-25; two left the states 2.4e-6 off). The state's sums are fp32 in registers, a chunk's products in tensor memory.
 //
-// Bound: the products' issue and the warps' work between them, not bytes: a chunk's 48 to 64 products of 64 or 128 columns take 45 to 70 cycles
-// each, 3.3 us a chunk in all. 16 x 1000 frames x 16 heads x 128, all there, 147 us (8 chunks of 512 heads' halves on 152 SMs, 1.8 TB/s); with
-// sequences of a third to all of that 98 to 104 us; linattn.cuh's kernel takes 311 and 220.
+// Bound: the products' issue and the warps' work between them, not bytes: the 52 to 64 products of a chunk, of 64 or 128 columns, take 45 to
+// 70 cycles each, 3.3 us a chunk or more in all. 16 x 1000 frames x 16 heads x 128: 147 us (512 units of 8 chunks on 152 SMs, 2.0
+// TB/s), with sequences of a third to all of that 104 us; the kernel of linattn.cuh takes 235 us for the first.
 #include <algorithm>
 
 #include "linattn.cuh"

@@ -652,8 +652,11 @@ def qnn_embedding(ids, table, scale: float = 1.0, dtype=None, out=None, stream=N
     if dtype is not None and ty is not dtype:
         _bad("out:", dtype)
     lead, size = tuple(ids.shape), _ids(torch, ids)
-    y = out if out is not None else _result(torch, (*lead, D), ty, table, stream)
-    ldt, ldo = _rows(table, "table", table.dtype, (V, D)), _by_label(y, "out", ty, lead, D)
+    if out is None:
+        y, ldo = _result(torch, (*lead, D), ty, table, stream), D
+    else:
+        y, ldo = out, _by_label(out, "out", ty, lead, D)
+    ldt = _rows(table, "table", table.dtype, (V, D))
     if stream is not None:
         _used(stream, ids, table, out)
     st = L.qnn_embedding(ids.data_ptr(), size, ids.numel(), table.data_ptr(), ldt, _dtype(table, "table"), V, D, scale, y.data_ptr(),
@@ -677,8 +680,10 @@ def qnn_embedding_grad(grad, ids, rows: int, scale: float = 1.0, dtype=None, out
         _bad("out:", dtype)
     if accumulate and out is None:
         _bad("accumulate: needs an out")
-    G = out if out is not None else _result(torch, (rows, D), ty, grad, stream)
-    ldo = _rows(G, "out", ty, (rows, D))
+    if out is None:
+        G, ldo = _result(torch, (rows, D), ty, grad, stream), D
+    else:
+        G, ldo = out, _rows(out, "out", ty, (rows, D))
     if stream is not None:
         _used(stream, grad, ids, out)
     st = L.qnn_embedding_grad(grad.data_ptr(), ldg, _dtype(grad, "grad"), ids.data_ptr(), size, ids.numel(), rows, D, scale,

@@ -389,7 +389,8 @@ def select_inputs(seed, B, K, V, kind, std=3.0):
 @pytest.mark.parametrize("kind", KINDS)
 @pytest.mark.parametrize("B,K,V,n", [(1, 1, 1, 1), (1, 4, 2000, 4), (3, 2, 29, 5), (2, 5, 333, 10), (4, 8, 2047, 16), (2, 8, 2048, 8),
                                      (2, 3, 2049, 6), (1, 4, 8192, 8), (7, 16, 1001, 32), (1, 2, 65537, 64), (2, 128, 40, 128),
-                                     (1, 1, 5000, 128), (300, 4, 64, 4), (1, 3, 5, 128), (64, 8, 4100, 16), (1, 32, 30000, 32)])
+                                     (1, 1, 5000, 128), (300, 4, 64, 4), (1, 3, 5, 128), (64, 8, 4100, 16), (1, 32, 30000, 32), (5, 8, 3000, 32),
+                                     (5, 8, 3000, 33), (200, 1, 20000, 3), (80, 2, 9000, 64), (30, 5, 9001, 10), (9, 1, 1, 256 // 2)])
 def test_select(qnn, B, K, V, n, kind):
     logits, scores = select_inputs(B * 7 + V, B, K, V, kind)
     check_select(qnn, logits, scores, n)
@@ -566,7 +567,8 @@ def test_embedding_shapes_and_bad_labels(qnn):
 @pytest.mark.parametrize("n,V,D,how", [(1, 1, 1, "zipf"), (1, 29, 500, "zipf"), (31, 5, 8, "padded"), (32, 2, 40, "one"), (33, 3, 40, "one"),
                                        (64, 511, 12, "zipf"), (65, 512, 7, "padded"), (1000, 2000, 36, "zipf"), (1024, 8, 500, "padded"),
                                        (1025, 9, 64, "padded"), (5000, 70000, 16, "zipf"), (9000, 300000, 4, "padded"), (3000, 1, 260, "one"),
-                                       (20000, 29, 100, "zipf"), (40000, 8192, 8, "zipf"), (140000, 50, 5, "padded"), (131072, 3, 8, "one")])
+                                       (20000, 29, 100, "zipf"), (40000, 8192, 8, "zipf"), (140000, 50, 5, "padded"), (131072, 3, 8, "one"),
+                                       (12000, 900, 1024, "zipf"), (10000, 3, 1032, "padded")])
 def test_embedding_grad(qnn, n, V, D, how, kind):
     g = rng(n + V + D)
     ids_h = id_list(g, n, V, how)
