@@ -27,7 +27,7 @@ struct EmbedArgs {
 constexpr int kEmbedThreads = 128, kEmbedRuns = 4;
 
 // A warp takes a share of a row, 32 kEmbedRuns runs of W values whose loads are in flight together, and loads the label of the next
-// meanwhile. Bound: HBM for the output; rows that come again are read from L2.
+// meanwhile. Bound: HBM for the output; rows that come again are read from L2. 16000 x 2048 bf16: 12.4 us, with nothing in L2 17.5 (94 MB).
 template <typename T, typename O, typename I, int W>
 __global__ void __launch_bounds__(kEmbedThreads) embed_kernel(const EmbedArgs a) {
     const int lane = threadIdx.x % 32;
@@ -414,7 +414,8 @@ __device__ __forceinline__ int64_t bound(const uint32_t *ids, int64_t lo, int64_
 
 // A warp adds the rows of a chunk of sorted positions, 32 lanes' columns of them, in the order of the positions, kRows loads in
 // flight. A run of one label that lies within the chunk is written out; what began before it or goes on behind it is kept for the
-// second kernel. Rows that no position has were cleared while the labels were sorted.
+// second kernel. Rows that no position has were cleared while the labels were sorted. Bound: memory's latency, with few warps (1200 x 500:
+// 13 us by itself), and its rate: 16000 x 2048 bf16 18 us.
 constexpr int kRows = 4;  // (2: 16000 x 2048 bf16 32 us, 8: 35, 16: 46, so 29.5; 60000 x 512 fp32 51, 45, so 44)
 template <typename T, typename O, int W>
 __global__ void __launch_bounds__(kGradThreads) grad_sum_kernel(const GradArgs a) {
@@ -476,7 +477,8 @@ __global__ void __launch_bounds__(kGradThreads) grad_sum_kernel(const GradArgs a
 
 // Runs over several chunks. A warp looks at one chunk (and 32 lanes' columns): where a run begins in it and goes on, it adds the sums
 // of the chunks that hold the rest, in order. Runs over more than kLongRun chunks are left to all of the block's warps, which
-// add a share of the chunks each, then the shares in order.
+// add a share of the chunks each, then the shares in order. 16000 x 2048: 12 us by itself, the search for a run's end and the sums of up to
+// kLongRun chunks in turn.
 constexpr int kLongRun = 32;
 template <int W>
 __device__ __forceinline__ void add_heads(const GradArgs &a, int64_t from, int64_t to, int64_t col, float (&sum)[W]) {
@@ -628,19 +630,17 @@ qnn_status launch_sort(const void *ids, int64_t n, int64_t V, const SortPlan &p,
     return QNN_OK;
 }
 
-// The runs over several chunks are joined by W columns a lane, 4 at most.
 template <typename T, typename O, int W>
 qnn_status launch_grad(GradArgs a, cudaStream_t st) {
-    constexpr int kWarps = kGradThreads / 32, kJoin = W < 4 ? W : 4;
+    constexpr int kWarps = kGradThreads / 32;
     a.cols = (a.D / W + 31) / 32;
     const int64_t sums = (a.chunks * a.cols + kWarps - 1) / kWarps;
     cudaLaunchAttribute attr;
     cudaLaunchConfig_t cfg = after(sums, kGradThreads, st, &attr);
     QNN_CUDA_TRY(cudaLaunchKernelEx(&cfg, grad_sum_kernel<T, O, W>, a));
     if (a.chunks > 1) {
-        a.cols = (a.D / kJoin + 31) / 32;
         cfg = after((a.chunks + kJoinWarps - 1) / kJoinWarps * a.cols, 32 * kJoinWarps, st, &attr);
-        QNN_CUDA_TRY(cudaLaunchKernelEx(&cfg, grad_join_kernel<O, kJoin>, a));
+        QNN_CUDA_TRY(cudaLaunchKernelEx(&cfg, grad_join_kernel<O, W>, a));
     }
     return QNN_OK;
 }

@@ -15,7 +15,8 @@ constexpr int kMostDim = 256;
 
 // Few frames: the states are most of the traffic, in and out. A block takes 32 columns of one head's state, whose rows lie in
 // runs of 128 bytes; a warp four rows of them at a time, kRows times in flight. A row's part in the outputs is added over the
-// warp's rows by shuffles and over the block's warps in shared memory.
+// warp's rows by shuffles and over the block's warps in shared memory. Bound: HBM for the states; 256 sequences x 16 heads x 128 x 128, one
+// frame, 541 MB: 79.5 us, 6.8 TB/s (the copy's rate).
 constexpr int kStepFrames = 8, kStepThreads = 128, kStepCols = 32, kRows = 8, kBlockRows = kRows * kStepThreads / 8;
 template <typename T, bool VEC, int FRAMES>
 __global__ void __launch_bounds__(kStepThreads) linear_step_kernel(const LinearArgs a) {
