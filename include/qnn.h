@@ -450,8 +450,8 @@ qnn_status qnn_linear_attention(const qnn_linear_args *args, void *stream);
 /* ---------------------------------------------------------------------------------------------
  * Label-synchronous decoding: selection over beams and classes, the kept beams' states, labels' rows.
  * As for the calls above, device pointers belong to the current device and outputs overlap nothing unless a call allows it; any
- * number of calls may run at once, and be captured into a graph after a first one of their kind on the device (which makes the
- * pool of their scratch and the status word). The same holds for qnn_linear_attention.
+ * number of calls may run at once, and be captured into a graph, a first call on the device too. The same holds for
+ * qnn_linear_attention.
  * ------------------------------------------------------------------------------------------- */
 
 /*

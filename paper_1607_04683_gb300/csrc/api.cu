@@ -41,6 +41,29 @@ qnn_status current(int *dev) {
     return QNN_OK;
 }
 
+// While it lives, the calling thread may make the library's own memory although a stream is being captured: a first call may be
+// one that is captured.
+class OutsideCapture {
+  public:
+    OutsideCapture() { cudaThreadExchangeStreamCaptureMode(&mode_); }
+    ~OutsideCapture() { cudaThreadExchangeStreamCaptureMode(&mode_); }
+    OutsideCapture(const OutsideCapture &) = delete;
+    OutsideCapture &operator=(const OutsideCapture &) = delete;
+
+  private:
+    cudaStreamCaptureMode mode_ = cudaStreamCaptureModeRelaxed;
+};
+// Clears memory by a stream of its own, which none that is captured has to do with.
+cudaError_t clear_now(void *p, size_t bytes) {
+    cudaStream_t st;
+    cudaError_t e = cudaStreamCreateWithFlags(&st, cudaStreamNonBlocking);
+    if (e != cudaSuccess) return e;
+    e = cudaMemsetAsync(p, 0, bytes, st);
+    const cudaError_t done = cudaStreamSynchronize(st);
+    cudaStreamDestroy(st);
+    return e == cudaSuccess ? done : e;
+}
+
 }  // namespace
 
 bool is_device_ptr(const void *p) {
@@ -90,11 +113,13 @@ qnn_status Scratch::take(size_t bytes, cudaStream_t st) {
             props.allocType = cudaMemAllocationTypePinned;
             props.location.type = cudaMemLocationTypeDevice;
             props.location.id = dev;
+            const OutsideCapture relaxed;
             QNN_CUDA_TRY(cudaMemPoolCreate(&d.pool, &props));
         }
         const size_t keeps = bytes > (size_t)1 << 30 ? bytes : (size_t)1 << 30;
         if (keeps > d.pool_keeps) {
             unsigned long long v = keeps;
+            const OutsideCapture relaxed;
             QNN_CUDA_TRY(cudaMemPoolSetAttribute(d.pool, cudaMemPoolAttrReleaseThreshold, &v));
             d.pool_keeps = keeps;
         }
@@ -182,8 +207,13 @@ qnn_status status_word(int **out) {
     std::lock_guard<std::mutex> lk(g_mu);
     DeviceState &d = g_dev[dev];
     if (!d.status) {
-        QNN_CUDA_TRY(cudaMalloc(&d.status, sizeof(int)));
-        QNN_CUDA_TRY(cudaMemset(d.status, 0, sizeof(int)));
+        const OutsideCapture relaxed;
+        int *p = nullptr;
+        QNN_CUDA_TRY(cudaMalloc(&p, sizeof(int)));
+        const cudaError_t e = clear_now(p, sizeof(int));
+        if (e != cudaSuccess) cudaFree(p);
+        QNN_CUDA_TRY(e);
+        d.status = p;
     }
     *out = d.status;
     return QNN_OK;

@@ -97,7 +97,8 @@ class _Embedding(torch.autograd.Function):
 class Embedding(torch.nn.Module):
     """Labels' rows of a trained table, times scale: the input of layers that take labels, a full-precision layer in Algorithm 1's
     sense. Labels below 0 are padding: rows of zeros, no gradient. The gradient is dense, its rows summed in an order that
-    depends on the labels only; it has no gradient of its own."""
+    depends on the labels only; it has no gradient of its own. A step is captured into a CUDA graph while no eager graph of the
+    same table lives (torch adds the gradient on the stream that such a graph was made on)."""
 
     def __init__(self, rows: int, dim: int, scale: float = 1.0, dtype: torch.dtype = torch.float32, device="cuda"):
         super().__init__()

@@ -1,6 +1,9 @@
 """Linear attention, beam selection and reordering, embedding and its gradient on the GPU against plain 64-bit references
 (decode_ref.py, which derives the bounds), and a decoder of them as it is used."""
 import ctypes as C
+import os
+import subprocess
+import sys
 
 import numpy as np
 import pytest
@@ -806,6 +809,61 @@ def test_calls_in_graphs(qnn):
         for a, b in zip([*got, eager], [*want, want[0]]):
             for x, y in zip(a, b):
                 assert all(torch.equal(p, r) for p, r in zip(x, y))
+
+
+@pytest.mark.parametrize("kernel,call", [
+    ("tc", "qnn.qnn_linear_attention(q, k, v, decay)"), ("chunks", "qnn.qnn_linear_attention(q, k, v, decay)"),
+    ("", "qnn.qnn_linear_attention(q.float(), k.float(), v.float(), decay)"), ("", "qnn.qnn_linear_attention(q[:, :1], k[:, :1], v[:, :1], decay)"),
+    ("", "torch.stack(qnn.qnn_beam_select(logits, scores)[1:])"), ("", "qnn.qnn_beam_reorder([table[:64]], parents)[0]"),
+    ("", "qnn.qnn_embedding(ids, table)"), ("", "qnn.qnn_embedding_grad(grad, ids, 300)")])
+def test_captured_before_the_first_call(qnn, kernel, call):
+    """In a process of its own: nothing of the library's has been made on the device when the call is captured."""
+    code = f'''
+import os, torch
+os.environ["QNN_LINEAR"] = "{kernel}"
+from paper_1607_04683_gb300 import qnn
+torch.cuda.set_device(0)
+g = torch.Generator(device="cuda").manual_seed(1)
+q, k, v = (torch.rand((1, 900, 2, 64), generator=g, device="cuda").bfloat16() for _ in range(3))
+decay, scores = torch.full((2,), -0.1, device="cuda"), torch.zeros((4, 16), device="cuda")
+logits, table, grad = torch.rand((4, 16, 3000), generator=g, device="cuda"), torch.rand((300, 64), device="cuda"), torch.rand((5000, 64), device="cuda")
+ids, parents = torch.randint(0, 300, (5000,), device="cuda"), torch.ones((4, 16), dtype=torch.int32, device="cuda")
+torch.cuda.synchronize()
+graph = torch.cuda.CUDAGraph()
+with torch.cuda.graph(graph):
+    out = {call}
+graph.replay()
+torch.cuda.synchronize()
+assert qnn.device_status() == qnn.QNN_OK and torch.equal(out, {call}) and out.abs().sum() > 0
+'''
+    root = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+    r = subprocess.run([sys.executable, "-c", code], cwd=root, capture_output=True, text=True, timeout=240)
+    assert r.returncode == 0, r.stderr[-2000:]
+
+
+def test_embedding_module_captured(qnn):
+    """A training step of the module in a graph, replayed on other labels and errors."""
+    from paper_1607_04683_gb300 import qat
+    emb = qat.Embedding(40, 8, scale=0.5)
+    ids, gy = torch.zeros(100, dtype=torch.int64, device="cuda"), torch.zeros(100, 8, device="cuda")
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):  # (nothing of this pass lives when the next is captured)
+        emb(ids).backward(gy)
+    torch.cuda.current_stream().wait_stream(side)
+    emb.weight.grad = None
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        y = emb(ids)
+        y.backward(gy)
+    for seed in range(3):
+        g = rng(seed)
+        ids.copy_(gpu(g.integers(-2, 40, 100)))
+        gy.copy_(gpu(g.normal(0, 1, (100, 8)).astype(np.float32)))
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(y, qnn.qnn_embedding(ids, emb.weight.detach(), scale=0.5))
+        assert torch.equal(emb.weight.grad, qnn.qnn_embedding_grad(gy, ids, 40, scale=0.5))
 
 
 def test_refusals(qnn):
