@@ -465,9 +465,10 @@ qnn_status qnn_linear_attention(const qnn_linear_args *args, void *stream);
  *   scores_out, parents, tokens  [B][n] out, best first: score, beam and class. Of equal scores the lowest beam, then the lowest
  *   class comes first; a slot without a candidate has score minus infinity, beam 0 and class eos. scores_out may be
  *   scores if n = K.
- * Scores are formed and compared in 64 bits and rounded once for scores_out. The sums of exponentials are of fp32 terms, right to
+ * Scores are formed and compared as two fp32 terms (48 bits) and rounded once for scores_out. The sums of exponentials are of fp32 terms, right to
  * about 2^-26 (each row of a call in the same order, so that equal rows have equal sums): candidates of different beams
- * that are closer may come in either order. Within a beam the order is that of the logits. 1 <= K, n <= 128; K V < 2^31; 0 <= eos < V.
+ * that are closer may come in either order. Within a beam the n best are those
+ * of the logits, in their order as far as the scores differ. 1 <= K, n <= 128; K V < 2^31; 0 <= eos < V.
  */
 qnn_status qnn_beam_select(const void *logits, int64_t ldl, int dtype, const float *scores, const uint8_t *finished, int64_t B,
                            int64_t K, int64_t V, int32_t n, int32_t eos, float *scores_out, int32_t *parents, int32_t *tokens,

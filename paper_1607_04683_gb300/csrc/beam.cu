@@ -275,18 +275,17 @@ __device__ __forceinline__ bool take_values(Best<Logit, EACH> &s, const float (&
         for (int o = 16; o > 0; o >>= 1) least = fminf(least, __shfl_xor_sync(0xffffffffu, least, o));
         from = i == lane ? least : fminf(from, least);
     }
-    int mine = 0;
-    if (pass && top >= from)
-#pragma unroll
-        for (int e = 0; e < EACH; ++e) mine += v[e] >= from && v[e] > bar;
-    int at = 0;
-    if (mine) at = atomicAdd(&s.wanted, mine);
-    __syncthreads();
-    if (s.wanted > kFewCands) return false;
-    if (mine)
+    // (one comparison a value: those no less than the n-th, or than the next value above the bar)
+    const float least = from > bar ? from : unordered(ordered(bar) + 1);
+    if (pass && top >= least)
 #pragma unroll
         for (int e = 0; e < EACH; ++e)
-            if (v[e] >= from && v[e] > bar) s.list[at++] = logit_key(v[e], (unsigned)place<VEC>(base, e));
+            if (v[e] >= least) {
+                const int at = atomicAdd(&s.wanted, 1);
+                if (at < kFewCands) s.list[at] = logit_key(v[e], (unsigned)place<VEC>(base, e));
+            }
+    __syncthreads();
+    if (s.wanted > kFewCands) return false;
     if (threadIdx.x == 0) s.count = s.wanted;
     __syncthreads();
     s.rank(n);
