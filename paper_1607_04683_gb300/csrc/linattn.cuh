@@ -230,6 +230,7 @@ __global__ void __launch_bounds__(kLinThreads, DKP == 64 ? 4 : DKP == 128 ? 2 : 
         if (p) each_state([&](float &s, int i) { s = p[i]; });
     }
 
+    const bool keeps = a.state_out && hi == n;
     int s = 0;
     for (int64_t base = lo; base < hi; base += C, s ^= NP == 1) {
         copy_wait();
@@ -411,6 +412,8 @@ __global__ void __launch_bounds__(kLinThreads, DKP == 64 ? 4 : DKP == 128 ? 2 : 
                 }
         }
 
+        if (!STATES && base + C >= hi && !keeps) break;  // (a part's last state is another's first, which the prefix has formed)
+
         // The state after the chunk. A chunk's products are added up from zero and then to the state: the matrix instruction cuts its
         // sums off (2^-24 of the largest term, always downwards), and a state that went through all of them as their accumulator
         // came out 1e-6 low. For the same reason products of small pieces have a sum of their own.
@@ -467,7 +470,7 @@ __global__ void __launch_bounds__(kLinThreads, DKP == 64 ? 4 : DKP == 128 ? 2 : 
         each_state([&](float &s, int i) { p[i] = s; });
     } else {
         // the part with the sequence's last frame (the first one, for none) has its state
-        if (a.state_out && (hi == n || n == 0)) {
+        if (keeps || (a.state_out && n == 0)) {
             float *p = a.state_out + unit * size;
             each_state([&](float &s, int i) { p[i] = s; });
         }
