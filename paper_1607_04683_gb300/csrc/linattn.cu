@@ -1,5 +1,6 @@
 // linattn.cu — linear attention with a decay for each head on sm_103a: the call, and its recurrent kernel for few frames.
 #include <algorithm>
+#include <cmath>
 #include <cstdlib>
 #include <cstring>
 
@@ -145,20 +146,21 @@ int copy_unit(const void *p, int64_t B, int64_t T, int64_t heads, int64_t width,
     return bits % 16 == 0 ? 16 : bits % 8 == 0 ? 8 : bits % 4 == 0 ? 4 : 0;
 }
 
-// Which of the two kernels takes a bf16 sequence, by what they took (us; dk = dv, sequences x heads): the tcgen05 one a chunk
-// of 128 frames in 3.3 and a sequence in 5 more, one block an SM; the other a chunk of 64 frames in 5 to 7, two blocks an SM, or with
-// the sequence in parts 6 to 9 for both passes. Of 128: T 64 10.4 / 10.3, 1 x 1000 33 / 29, 76 x 1000 39 / 88, 16 x 4000 111 / 85,
-// 38 x 4000 114 / 182; of 64: 38 x 1000 33 / 27, 152 x 1000 37 / 64; of 32: 304 x 128 16.5 / 14.5.
+// Which of the two kernels takes a bf16 sequence, by what they took (us): the tcgen05 one a chunk of 128 frames in 3.3 and a unit in
+// 1.7 more, one block an SM; the other a chunk of 64 frames in 4.4 or 5.8, or with the sequence in parts both passes of a part's chunks, that take
+// longer with more blocks an SM, and 9 or 13 for the call. Sequences x frames x heads x dk: 1 x 16 x 8 x 64 10.4 / 8.3, 1 x 128 x 8 x 64 10.4 / 12.6, 1 x 300
+// x 4 x 64 16.6 / 12.6, 8 x 300 x 8 x 64 16.6 / 19.8, 1 x 1000 x 8 x 64 33 / 16.6, 8 x 1000 x 8 x 64 33 / 39; 1 x 500 x 4 x 128 20.6 / 18.8, 1 x 1000 x 16 x 128 33.1 /
+// 33.4, 2 x 1000 x 16 x 128 35 / 56, 1 x 2000 x 16 x 128 60 / 53, 1 x 4000 x 16 x 128 112 / 83, 16 x 1000 x 16 x 128 138 / 232.
 bool prefers_tc(const LinearArgs &a, int chunk, int64_t chunks) {
     if (const char *e = std::getenv("QNN_LINEAR")) {  // one of them always (tests)
         if (std::strcmp(e, "tc") == 0) return true;
         if (std::strcmp(e, "chunks") == 0) return false;
     }
-    const int64_t blocks = a.B * a.H * a.tiles, sms = sm_count();
-    const double tc = 2.0 + (5.0 + 3.3 * (double)((a.T + 127) / 128)) * (double)((blocks + sms - 1) / sms);
-    const double per = (double)(a.parts > 1 ? a.per / chunk : chunks);
-    return tc < (a.parts > 1 ? 17.0 + (a.dk > 64 ? 9.0 : 6.0) * per
-                             : 6.0 + (a.dk > 64 ? 7.2 : 4.6) * per * (double)((blocks + 2 * sms - 1) / (2 * sms)));
+    const double units = (double)(a.B * a.H * a.tiles), sms = sm_count(), full = units * a.parts / sms;
+    const double tc = 5.5 + (1.7 + 3.3 * (double)((a.T + 127) / 128)) * std::ceil(units / sms);
+    const bool wide = a.dk > 64;
+    if (a.parts > 1) return tc < (wide ? 13.0 : 9.0) + (double)(a.per / chunk) * (wide ? 5.5 + 2.6 * full : 4.5 + 2.4 * full);
+    return tc < (wide ? 3.0 : 4.0) + (wide ? 5.8 : 4.4) * (double)chunks * std::ceil(full / (wide ? 2.0 : 3.0));
 }
 
 }  // namespace
@@ -218,11 +220,15 @@ extern "C" qnn_status qnn_linear_attention(const qnn_linear_args *args, void *st
     a.y_copy = copy_unit(p.y, B, T, p.H, p.dv, p.y_seq, p.y_frame, e);
     const uintptr_t ybits = reinterpret_cast<uintptr_t>(p.y) | (uintptr_t)((B > 1 ? p.y_seq * e : 0) | p.y_frame * e | (int64_t)p.dv * e);
     a.pairs = ybits % (2 * e) == 0;
-    // parts of a sequence: as many blocks as the SMs hold at once, but no fewer than two chunks a part
-    const int chunk = linear_chunk(p.dtype, p.dk);
+    // Parts of a sequence: as many as the SMs hold blocks of at once, of a chunk at least, where both passes take less than one: a
+    // chunk c us (3.5 to 6.5) and 2 more, in parts 13 and 1.7 c a chunk. fp32 8 x 200 x 8 x 64 by 1, 2, 3, 4, 7 parts 33, 45, 37, 30,
+    // 22 us; 1 x 1000 x 8 x 64 by 16 and 32 27 and 19; 1 x 4000 x 8 x 64 by 32, 42, 63 47, 40, 41; 1 x 1000 x 16 x 128 by 8, 16, 32 60, 64, 75;
+    // 10 x 1000 x 16 x 64 by 1 and 2 173 and 168, of fp16 124 and 141.
+    const int chunk = linear_chunk(p.dtype, p.dk), held = p.dk > 64 ? 2 : 3;
     const int64_t units = B * p.H * a.tiles, chunks = (T + chunk - 1) / chunk;
-    int64_t parts = std::max<int64_t>(1, std::min<int64_t>({(p.dk <= 64 ? 3 : 2) * (int64_t)sm_count() / units, chunks / 2, 64}));
-    const int64_t per = (chunks + parts - 1) / parts;
+    int64_t parts = std::max<int64_t>(1, std::min<int64_t>({held * (int64_t)sm_count() / units, chunks, 64}));
+    int64_t per = (chunks + parts - 1) / parts;
+    if (5 * per + 8 > 3 * chunks || (p.dk <= 64 && parts < 3)) per = chunks;
     a.parts = (int)((chunks + per - 1) / per);
     a.per = per * chunk;
     if (p.dtype == QNN_BF16 && linear_tc_fits(a) && prefers_tc(a, chunk, chunks)) {

@@ -15,8 +15,8 @@
 // every warp: 1 x 4000 x 8 x 64 fp32 125 us.)
 //
 // Bound: a warp's instructions, of which the products are a tenth, and their way into the caches. 1 x 4000 x 8 x 64 fp32, three chunks a part
-// and pass: 41 us (states 16, prefix 10, outputs 34 one by one with cold caches); 16 x 1000 x 16 x 128 fp32 510 us, fp16 354, bf16 235. Eight warps
-// a block, each half of dk, took 43 us for the first and 690 for the second: v's pieces are made twice.
+// and pass: 39 us (states 16, prefix 10, outputs 31 one by one with cold caches); 1 x 1000 x 8 x 64, a chunk a part, 19 us; 16 x 1000 x 16 x 128
+// 505 us, fp16 347, bf16 232. Eight warps a block, each half of dk, took 43 us for the first and 690 for the last: v's pieces are made twice.
 #pragma once
 
 #include <algorithm>
