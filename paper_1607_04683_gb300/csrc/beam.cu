@@ -532,6 +532,7 @@ __global__ void __launch_bounds__(kThreads, 4) beam_cluster_kernel(const SelectA
         const int64_t lo = part * a.per, hi = lo + a.per < a.V ? lo + a.per : a.V;
         of = look_at<T, VEC, EACH>(static_cast<const T *>(a.logits) + row * a.ldl, lo, hi, a.n, sh.row);
     }
+    __syncwarp();
     cluster_wait();
     if (there) {
         const uint32_t keys = cluster_addr(su32(&sh.keys[rank * a.n]), 0), to = cluster_addr(su32(&sh.parts[rank]), 0);
@@ -541,6 +542,7 @@ __global__ void __launch_bounds__(kThreads, 4) beam_cluster_kernel(const SelectA
             store_remote64(to + 8, (unsigned long long)(uint32_t)of.held << 32 | __float_as_uint(of.most));
         }
     }
+    __syncwarp();
     cluster_sync();
     if (rank == 0) select_of_few(a, b, sh.parts, sh.keys, sh.few);
 }

@@ -320,6 +320,7 @@ __global__ void __launch_bounds__(kOneThreads, 1) sort_cluster_kernel(const Sort
             }
             s.count[d] = sum;
         }
+        __syncwarp();
         cluster_sync();
         // a bin a thread: its labels in all blocks and in those before this one, and the sum of the first over smaller bins
         uint32_t total = 0, mine = 0;
@@ -359,6 +360,7 @@ __global__ void __launch_bounds__(kOneThreads, 1) sort_cluster_kernel(const Sort
                     a.id_out[to] = id[r], a.pos_out[to] = pos[r];
                 }
             }
+        __syncwarp();
         cluster_sync();  // (the last one: no block leaves while another may still read its counts)
     }
 }
