@@ -8,9 +8,9 @@
 // accumulator of the last product, and lies in a lane as the first operand of q S wants it.
 //
 // Numbers. All products are of bf16 pieces of 8 bits with fp32 sums: a bf16 input is one piece, an fp16 input two, an fp32 input
-// three (all exact). What is formed in fp32 is put in as a sum of such pieces: scores and state in two (2^-17 of each, far below a
+// three (all exact). What is formed in fp32 is put in as a sum of such pieces: scores and state in two (2^-16 of each, below a
 // 16-bit output's rounding; fp32: three), the scaled v in three (2^-25: the state is kept in fp32 and is an output). Of the products of
-// pieces those are taken that the shorter of the two sides' precisions needs: one to three for bf16, three to five for fp16, six for fp32
+// pieces those are taken that the shorter of the two sides' precisions needs: one to three for bf16, four or five for fp16, six for fp32
 // (2^-23). (tf32 instructions for fp16 and fp32 took as many, and three times the instructions around them to split operands in
 // every warp: 1 x 4000 x 8 x 64 fp32 125 us.)
 //
@@ -74,10 +74,11 @@ __device__ __forceinline__ void split_pair(float x, float y, uint32_t (&p)[N]) {
 }
 __device__ __forceinline__ float low_of(uint32_t w) { return __uint_as_float(w << 16); }
 __device__ __forceinline__ float high_of(uint32_t w) { return __uint_as_float(w & 0xffff0000u); }
-// The products (i, j) of A's and B's pieces that count, the smallest first: i + j below the larger number of pieces.
+// The products (i, j) of A's and B's pieces that count, the smallest first: i + j below the larger number of pieces, and all four of
+// two and two (a second piece is up to 2^-7 of its value: without the last product fp16 outputs were up to 2^-14 of their terms off).
 template <int A, int B, typename F>
 __device__ __forceinline__ void each_product(F f) {
-    constexpr int kMost = A > B ? A : B;
+    constexpr int kMost = A == 2 && B == 2 ? 3 : A > B ? A : B;
 #pragma unroll
     for (int sum = kMost - 1; sum >= 0; --sum)
 #pragma unroll

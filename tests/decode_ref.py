@@ -20,7 +20,10 @@ def linear(q, k, v, log_decay, scale, kind, state=None, lengths=None):
 
     mass is the same sum over magnitudes. On its way to an output a term takes: two products of up to dk + 64 terms by matrix
     instructions, 2 u each; the roundings of its factors (64 allows for those and for decays from a table); a state's rounding once a
-    chunk of 16 frames or more, three operations each. What is held in pieces is off by 2^-17 (bf16, twice) or 2^-22."""
+    chunk of 16 frames or more, three operations each. A term passes one value that is held in pieces, its score or the state. With
+    16-bit inputs those are two of 8 bits: the first is cut off, which leaves less than 2^-7 of the value's power of two 2^e, below
+    2^(e-7), where bf16 has steps of 2^(e-15); the second is rounded to those, off by 2^(e-16) at most: 2^-16. With fp32 inputs
+    products of second and third pieces are left out, 2^-7 2^-14 each and two of them."""
     H = log_decay.shape[0]
     B, T = q.shape[:2]
     dk, dv = q.shape[3], v.shape[3]
@@ -38,7 +41,7 @@ def linear(q, k, v, log_decay, scale, kind, state=None, lengths=None):
         y[:, t] = np.where(on[..., 0], scale * np.einsum("bhd,bhde->bhe", q[:, t], S), np.nan)
         mass[:, t] = abs(scale) * np.einsum("bhd,bhde->bhe", np.abs(q[:, t]), M)
     steps = 64 + 3 * T / 16
-    pieces = 2 * 2.0 ** -17 if kind == "bf16" else 4 * 2.0 ** -22
+    pieces = 2.0 ** -16 if kind != "f32" else 2 * 2.0 ** -21
     # (the outputs' sums and the states' products below 2^-126 may be lost)
     bound = ((dk / 4 + steps) * 2 * U + pieces) * mass + HALF[kind] * np.abs(y) + TINY[kind] + 1e-36
     return y, bound, S, steps * 2 * U * M + 1e-36
