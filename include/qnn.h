@@ -465,10 +465,11 @@ qnn_status qnn_linear_attention(const qnn_linear_args *args, void *stream);
  *   scores_out, parents, tokens  [B][n] out, best first: score, beam and class. Of equal scores the lowest beam, then the lowest
  *   class comes first; a slot without a candidate has score minus infinity, beam 0 and class eos. scores_out may be
  *   scores if n = K.
- * Scores are formed and compared as two fp32 terms (48 bits) and rounded once for scores_out. The sums of exponentials are of fp32 terms, right to
- * about 2^-26 (each row of a call in the same order, so that equal rows have equal sums): candidates of different beams
- * that are closer may come in either order. Within a beam the n best are those
- * of the logits, in their order as far as the scores differ. 1 <= K, n <= 128; K V < 2^31; 0 <= eos < V.
+ * Scores are formed and compared as two fp32 terms (48 bits) and rounded once for scores_out. The sums of exponentials are of fp32
+ * terms, each right to 2^-22: their logarithm is off by 2^-26 or so where many classes count, and by 2^-22 where few do (each row of a
+ * call in the same order, so that equal rows have equal sums). Candidates of different beams that are closer may come in either
+ * order. Within a beam the n best are those of the logits, in their order as far as the scores differ.
+ * 1 <= K, n <= 128; K V < 2^31; 0 <= eos < V.
  */
 qnn_status qnn_beam_select(const void *logits, int64_t ldl, int dtype, const float *scores, const uint8_t *finished, int64_t B,
                            int64_t K, int64_t V, int32_t n, int32_t eos, float *scores_out, int32_t *parents, int32_t *tokens,

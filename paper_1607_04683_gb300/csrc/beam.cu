@@ -202,7 +202,8 @@ struct SelectArgs {
 
 // exp(d) for d <= 0 by the hardware's exponential, its argument's product with log2(e) in two terms: log2(e) rounded to 24
 // bits alone moves exp(-8) by 1e-7, always the same way. kBias takes out the instruction's own (it lies low by about 2e-8), so that
-// sums of many terms are right to about 1e-8 and two beams' continuations that close are still told apart.
+// sums of many terms are right to about 1e-8 and two beams' continuations that close are still told apart (a term alone is right to
+// 2^-22: sums that one or two make are 2e-7 off at worst).
 constexpr float kLog2eRest = 1.925963033500e-08f, kBias = 2e-8f;
 __device__ __forceinline__ float exp_term(float d) { return exp2_hw(__fmaf_rn(d, kLog2eRest, __fmaf_rn(d, kLog2e, kBias))); }
 
