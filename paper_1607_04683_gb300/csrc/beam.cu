@@ -2,6 +2,7 @@
 // of the beams that were kept.
 #include <algorithm>
 #include <cfloat>
+#include <cmath>
 
 #include "elem.cuh"
 #include "qnn_device.cuh"
@@ -179,8 +180,8 @@ struct Best {
 // Selection
 // ------------------------------------------------------------------------------------------------
 
-// Of a part of a row: its largest value and the sum of exp(value - largest) as a whole number of 2^-32 (exact sums
-// of the threads' fp32 ones, in any order; ~0: not a number).
+// Of a part of a row: its largest value and the sum of exp(value - largest) as a whole number of the call's units (exact sums
+// of the threads' ones, in any order; ~0: not a number).
 struct RowPart {
     unsigned long long sum;
     float most;
@@ -197,15 +198,26 @@ struct SelectArgs {
     Logit *keys;     // [rows][parts][n]
     RowPart *parts_of;  // [rows][parts]
     int64_t K, V, per;  // per: classes of a part
+    float units, unit;  // of RowPart::sum: how many are 1, a power of two by which `per` has 62 bits, and what one is
     int n, parts, eos;
 };
 
-// exp(d) for d <= 0 by the hardware's exponential, its argument's product with log2(e) in two terms: log2(e) rounded to 24
-// bits alone moves exp(-8) by 1e-7, always the same way. kBias takes out the instruction's own (it lies low by about 2e-8), so that
-// sums of many terms are right to about 1e-8 and two beams' continuations that close are still told apart (a term alone is right to
-// 2^-22: sums that one or two make are 2e-7 off at worst).
-constexpr float kLog2eRest = 1.925963033500e-08f, kBias = 2e-8f;
-__device__ __forceinline__ float exp_term(float d) { return exp2_hw(__fmaf_rn(d, kLog2eRest, __fmaf_rn(d, kLog2e, kBias))); }
+// exp(d) for d <= 0 by the hardware's exponential, whose argument, the product with log2(e) in two terms, is rounded once. kBias takes
+// out what the instruction is off on average (it lies low by 5e-8, 7e-8 ln 2; that of 0 stays 1).
+//
+// How far a row's log sum exp is off, in 2^-24: a term's difference d from the part's largest value is rounded (|d|), as is its argument (|d| too,
+// for a factor ln 2 of log2(e) |d|), the instruction is 2^-22 off at most (4) and the bias 5e-8 (1). A tile's terms of a thread are added in
+// pairs (5 roundings for 32), tiles and threads without loss (two fp32 terms, then whole numbers). In all 10 + 2 D, D the mean of |d| by the classes'
+// probabilities, which is the entropy at most; up to 2.1 in 1700 rows of 97 to 262144 classes. (Terms added one after another into one fp32 sum: up to
+// 380 for 262144 classes of two values, as every term's rounding goes the same way. 320 x 65536 fp32 30.8 us, so 27.4; 128 x 8 x 8192 as before.)
+constexpr float kLog2eRest = 1.925963033500e-08f, kBias = 7e-8f;
+__device__ __forceinline__ float exp_term(float d) { return exp2_hw(__fmaf_rn(d, kLog2e, __fmaf_rn(d, kLog2eRest, kBias))); }
+// The sum of exp(v - from) over N values, in pairs.
+template <int N>
+__device__ __forceinline__ float exp_terms(const float *v, float from) {
+    if constexpr (N == 1) return exp_term(__fsub_rn(*v, from));
+    else return __fadd_rn(exp_terms<N / 2>(v, from), exp_terms<N / 2>(v + N / 2, from));
+}
 
 // A tile of a row: with VEC runs of eight values a thread, else neighbouring values by neighbouring threads.
 constexpr int kRun = 8;
@@ -250,13 +262,17 @@ __device__ __forceinline__ void load_tile(const T *row, int64_t base, int64_t en
 // Best::take for a tile of a row, by values alone: candidates are those no less than the n-th best of the groups' largest values (and
 // above the n-th best so far, which comes from lower classes). False, with nothing taken, where so many are equal to it that
 // they need to be told apart by their classes first. One 32-bit comparison a value instead of keys of 64: 128 x 8 x 8192
-// bf16 11 us less.
+// bf16 11 us less. `also` is called once by every thread on the way, with the tile's largest value, or minus infinity where that is
+// no larger than those before.
 constexpr int kFewCands = 512;
-template <bool VEC, int EACH>
-__device__ __forceinline__ bool take_values(Best<Logit, EACH> &s, const float (&v)[EACH], float top, int64_t base, int n) {
+template <bool VEC, int EACH, typename F>
+__device__ __forceinline__ bool take_values(Best<Logit, EACH> &s, const float (&v)[EACH], float top, int64_t base, int n, F also) {
     const float bar = s.held == n ? unordered((uint32_t)(s.last >> 32)) : -INFINITY;
     const bool pass = top > bar;
-    if (__syncthreads_or(pass) == 0) return true;
+    if (__syncthreads_or(pass) == 0) {
+        also(-INFINITY);
+        return true;
+    }
     const int lane = threadIdx.x % 32, groups = n <= 16 ? 32 : n <= 32 ? 64 : n <= 64 ? 128 : 256, size = kThreads / groups;
     float most = pass ? top : -INFINITY;
     for (int m = 1; m < size; m <<= 1) most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, m));
@@ -264,9 +280,10 @@ __device__ __forceinline__ bool take_values(Best<Logit, EACH> &s, const float (&
     if (threadIdx.x % size == 0) bests[threadIdx.x / size] = most;
     if (threadIdx.x == 0) s.wanted = s.held;
     __syncthreads();
-    float from = -INFINITY;  // the n-th largest, if there are as many
+    float from = -INFINITY, largest = -INFINITY;  // the n-th largest, if there are as many
     for (int i = lane; i < groups; i += 32) {
         const float mine = bests[i];
+        largest = fmaxf(largest, mine);
         int better = 0;
 #pragma unroll 8
         for (int j = 0; j < groups; ++j) better += bests[j] > mine;
@@ -285,6 +302,7 @@ __device__ __forceinline__ bool take_values(Best<Logit, EACH> &s, const float (&
                 const int at = atomicAdd(&s.wanted, 1);
                 if (at < kFewCands) s.list[at] = logit_key(v[e], (unsigned)place<VEC>(base, e));
             }
+    also(warp_max(largest));
     __syncthreads();
     if (s.wanted > kFewCands) return false;
     if (threadIdx.x == 0) s.count = s.wanted;
@@ -300,12 +318,12 @@ __device__ __forceinline__ bool take_values(Best<Logit, EACH> &s, const float (&
 template <int EACH>
 struct RowShared {
     Best<Logit, EACH> best;
-    float warp_most[kWarps];
     unsigned long long warp_sum[kWarps];
 };
 template <typename T, bool VEC, int EACH>
-__device__ __forceinline__ RowPart look_at(const T *x, int64_t lo, int64_t hi, int n, RowShared<EACH> &sh) {
-    float v[EACH], most = -INFINITY, sum = 0.0f;
+__device__ __forceinline__ RowPart look_at(const T *x, int64_t lo, int64_t hi, int n, float units, RowShared<EACH> &sh) {
+    float v[EACH], most = -INFINITY;  // most: of the block's values so far, which the sum's terms go by
+    Two sum = {0.0f, 0.0f};
     load_tile<T, VEC, EACH>(x, lo, hi, v);
     sh.best.start();
     for (int64_t base = lo; base < hi; base += kThreads * EACH) {
@@ -313,11 +331,16 @@ __device__ __forceinline__ RowPart look_at(const T *x, int64_t lo, int64_t hi, i
         float top = v[0];
 #pragma unroll
         for (int e = 1; e < EACH; ++e) top = fmaxf(top, v[e]);
-        if (top > most) sum = __fmul_rn(sum, exp_term(__fsub_rn(most, top))), most = top;
-        const float from = most > -INFINITY ? most : 0.0f;
-#pragma unroll
-        for (int e = 0; e < EACH; ++e) sum = __fadd_rn(sum, exp_term(__fsub_rn(v[e], from)));
-        if (!take_values<VEC, EACH>(sh.best, v, top, base, n)) {
+        auto add_up = [&](float largest) {
+            if (largest > most) {  // (NaNs stay NaNs)
+                const Two d = two_sum(most, -largest);
+                if (most > -INFINITY) sum = mul(sum, d.hi < -80.0f ? Two{0.0f, 0.0f} : exp_two(d));
+                most = largest;
+            }
+            const Two s = two_sum(sum.hi, exp_terms<EACH>(v, most > -INFINITY ? most : 0.0f));
+            sum = {s.hi, __fadd_rn(sum.lo, s.lo)};
+        };
+        if (!take_values<VEC, EACH>(sh.best, v, top, base, n, add_up)) {
             unsigned first = 0;
 #pragma unroll
             for (int e = EACH - 1; e >= 0; --e)
@@ -325,24 +348,17 @@ __device__ __forceinline__ RowPart look_at(const T *x, int64_t lo, int64_t hi, i
             sh.best.take([&](int e) { return logit_key(v[e], (unsigned)place<VEC>(base, e)); }, logit_key(top, first), n);
         }
     }
-    // the block's maximum, then the sums' parts of it
     const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
-    float m = warp_max(most);
-    if (lane == 0) sh.warp_most[warp] = m;
-    __syncthreads();
-    m = sh.warp_most[0];
-#pragma unroll
-    for (int i = 1; i < kWarps; ++i) m = fmaxf(m, sh.warp_most[i]);
-    const float share = most > -INFINITY ? __fmul_rn(sum, exp_term(__fsub_rn(most, m))) : sum;  // (NaNs pass through)
-    const bool bad = !(share >= 0.0f && share < INFINITY);
-    unsigned long long s = bad ? 0 : __float2ull_rn(__fmul_rn(share, 4294967296.0f));
+    const bool bad = !(sum.hi >= 0.0f && sum.hi < INFINITY);
+    unsigned long long s =
+        bad ? 0 : __float2ull_rn(__fmul_rn(sum.hi, units)) + (unsigned long long)__float2ll_rn(__fmul_rn(sum.lo, units));
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
     if (lane == 0) sh.warp_sum[warp] = s;
     const int any_bad = __syncthreads_or(bad);
     s = 0;
     for (int i = 0; i < kWarps; ++i) s += sh.warp_sum[i];
-    return {any_bad ? ~0ull : s, m, sh.best.held};
+    return {any_bad ? ~0ull : s, most, sh.best.held};
 }
 // A beam that is not finished and not lost has its logits looked at.
 __device__ __forceinline__ bool looked_at(const SelectArgs &a, int64_t row) {
@@ -357,7 +373,7 @@ __global__ void __launch_bounds__(kThreads, 4) beam_rows_kernel(const SelectArgs
     const int part = blockIdx.x % (unsigned)a.parts;
     if (!looked_at(a, row)) return;
     const int64_t lo = part * a.per, hi = lo + a.per < a.V ? lo + a.per : a.V;
-    const RowPart of = look_at<T, VEC, EACH>(static_cast<const T *>(a.logits) + row * a.ldl, lo, hi, a.n, sh);
+    const RowPart of = look_at<T, VEC, EACH>(static_cast<const T *>(a.logits) + row * a.ldl, lo, hi, a.n, a.units, sh);
     Logit *keys = a.keys + (row * a.parts + part) * a.n;
     for (int i = threadIdx.x; i < of.held; i += kThreads) keys[i] = sh.best.list[i];
     if (threadIdx.x == 0) a.parts_of[row * a.parts + part] = of;
@@ -393,8 +409,8 @@ struct Beams {
                             if (d < -80.0f) continue;
                             const unsigned long long whole = of.sum;
                             const float hi = __ull2float_rn(whole);
-                            const Two share = {__fmul_rn(hi, 0x1p-32f),
-                                               __fmul_rn(__ll2float_rn((long long)(whole - (unsigned long long)hi)), 0x1p-32f)};
+                            const Two share = {__fmul_rn(hi, a.unit),
+                                               __fmul_rn(__ll2float_rn((long long)(whole - (unsigned long long)hi)), a.unit)};
                             s = add(s, d == 0.0f ? share : mul(share, exp_two(two_sum(of.most, -m))));
                         }
                         l = add({m, 0.0f}, log_two(s));
@@ -531,7 +547,7 @@ __global__ void __launch_bounds__(kThreads, 4) beam_cluster_kernel(const SelectA
     RowPart of;
     if (there) {
         const int64_t lo = part * a.per, hi = lo + a.per < a.V ? lo + a.per : a.V;
-        of = look_at<T, VEC, EACH>(static_cast<const T *>(a.logits) + row * a.ldl, lo, hi, a.n, sh.row);
+        of = look_at<T, VEC, EACH>(static_cast<const T *>(a.logits) + row * a.ldl, lo, hi, a.n, a.units, sh.row);
     }
     __syncwarp();
     cluster_wait();
@@ -689,6 +705,7 @@ extern "C" qnn_status qnn_beam_select(const void *logits, int64_t ldl, int dtype
     parts = (tiles + per - 1) / per;
     if (rows * parts > INT32_MAX) return QNN_ERR_INVALID_ARG;
     a.parts = (int)parts, a.per = per * tile;
+    a.units = std::ldexp(1.0f, 61 - std::ilogb((double)a.per)), a.unit = 1.0f / a.units;  // (a term is 1 at most)
     cudaStream_t st = as_stream(stream);
     Scratch scratch;
     if (!in_cluster(a)) {

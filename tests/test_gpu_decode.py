@@ -453,6 +453,74 @@ def test_select_masks(qnn, V, kind):
     check_select(qnn, logits, scores, 100, finished.to(torch.uint8), eos=V - 1)
 
 
+def rows_of_sums(V):
+    """Rows that show how their sums of exponentials are added up: of two values, slopes either way and beyond all that counts, normal
+    ones, one class above all others, whose parts are of very different size."""
+    g = rng(V)
+    rows = [g.normal(0, 3, V), np.linspace(-8, 8, V), np.linspace(8, -8, V), np.linspace(-100, 60, V), np.zeros(V)]
+    for share in (64, 8):
+        for low in (-1.0, -3.0, -7.5, -11.3):
+            x = np.full(V, low)
+            x[g.permutation(V)[:V // share]] = 0.0
+            rows.append(x)
+    x = np.full(V, -15.7)
+    x[V // 3] = 0.0
+    rows.append(x)
+    rows.append(np.where(np.arange(V) % 97 == 96, 20.0 + np.arange(V) / V, -3.1))  # (every other tile has a new largest value)
+    return np.stack(rows)
+
+
+@pytest.mark.parametrize("kind", KINDS)
+@pytest.mark.parametrize("V", [97, 2000, 8192, 65536, 262144])
+@pytest.mark.parametrize("times", [1, 21])
+def test_select_sums_of_exponentials(qnn, V, kind, times):
+    """Scores of a row's best class where beam score and logits leave nearly nothing, so that the score's own rounding does not count, and of
+    four beams of one utterance. In 2^-24, a row's log sum exp is off by 10 + 2 D at most, D the mean of |d|, a class's distance from the largest
+    logit, by the classes' probabilities: d is rounded to fp32 (|d|), d log2(e) is (|d| again), the exponential's instruction is 2^-22 off
+    (4), what it is off on average is taken out (5e-8: less than 1), 32 terms of a thread are added in pairs (5); the sums across threads and the
+    logarithm are of 35 bits and more, and have what is left of 10. Times: once in parts of a row, and often enough that a row is one."""
+    few = gpu(rows_of_sums(V), kind)
+    x = host(few)
+    R = len(x)
+    most = x.max(1)
+    p = np.exp(x - most[:, None])
+    lse = most + np.log(p.sum(1))
+    D = (p * (most[:, None] - x)).sum(1) / p.sum(1)
+    start = gpu((lse - most).astype(np.float32))
+    want = host(start) + most - lse
+    bound = (10 + 2 * D) * U + U * np.abs(want) + 1e-15
+    logits = few.repeat(times, 1).unsqueeze(1)  # utterances of one beam
+    best, _, tokens = qnn.qnn_beam_select(logits, start.repeat(times)[:, None], 1)
+    first = np.argmax(x, 1)
+    assert (host(tokens).reshape(times, R) == first).all()
+    off = np.abs(host(best).reshape(times, R) - want)
+    assert (off <= bound).all(), (off / U, bound / U)
+    wide = few[:12].view(3, 4, V)  # four beams, of which each is looked at in parts; one candidate each, as the others are lost
+    for k in range(4):
+        scores = torch.full((3, 4), -np.inf, device="cuda")
+        scores[:, k] = start[:12].view(3, 4)[:, k]
+        best, parents, tokens = qnn.qnn_beam_select(wide, scores, 2)
+        assert (parents[:, 0] == k).all()
+        off = np.abs(host(best)[:, 0] - want[:12].reshape(3, 4)[:, k])
+        assert (off <= bound[:12].reshape(3, 4)[:, k]).all(), (off / U, bound / U)
+    assert qnn.device_status() == qnn.QNN_OK
+
+
+@pytest.mark.parametrize("V", [300, 20000, 100000])
+@pytest.mark.parametrize("rows", [1, 400])
+def test_select_not_a_number_behind_larger_values(qnn, V, rows):
+    """A NaN, or an infinity, in an earlier tile than the largest value, and one behind a far larger value: the beam has no candidates."""
+    base = np.linspace(-200, 200, V)
+    for at in (0, V // 2, V - 1):
+        for bad in (float("nan"), float("inf")):
+            x = base.copy()
+            x[at] = bad
+            logits = gpu(np.stack([x, base])[:, None].repeat(rows, 0), "f32")
+            best, parents, tokens = qnn.qnn_beam_select(logits, torch.zeros((2 * rows, 1), device="cuda"), 1, eos=7)
+            assert (best[:rows] == -np.inf).all() and (tokens[:rows] == 7).all()
+            assert torch.isfinite(best[rows:]).all() and (tokens[rows:] == V - 1).all()
+
+
 @pytest.mark.parametrize("kind", KINDS)
 def test_select_strides_and_places(qnn, kind):
     full, scores = select_inputs(5, 3, 4, 1003, kind)
