@@ -539,7 +539,7 @@ def qnn_linear_attention(q, k, v, log_decay, scale=None, state_in=None, state_ou
     hk, (hv, dv), H = k.shape[2], v.shape[2:], log_decay.shape[0]
     y = out if out is not None else _result(torch, (B, T, H, dv), ty, q, stream)
     state = (B, H, dk, dv)
-    args = _LINEAR_ARGS.pack(B, T, H, hq, hk, hv, dk, dv, kind, dk ** -0.5 if scale is None else scale,
+    args = _LINEAR_ARGS.pack(B, T, H, hq, hk, hv, dk, dv, kind, max(dk, 1) ** -0.5 if scale is None else scale,
                              *_frames(q, "q", ty, (B, T, hq, dk)), *_frames(k, "k", ty, (B, T, hk, dk)),
                              *_frames(v, "v", ty, (B, T, hv, dv)), *_frames(y, "out", ty, (B, T, H, dv)),
                              _flat(log_decay, "log_decay", f32, (H,)), _flat(state_in, "state_in", f32, state),

@@ -934,6 +934,16 @@ def test_embedding_module_captured(qnn):
         assert torch.equal(emb.weight.grad, qnn.qnn_embedding_grad(gy, ids, 40, scale=0.5))
 
 
+def test_linear_refuses_heads_of_no_values(qnn):
+    """By the library's error, also where the scale is left to the call."""
+    q, k, v, decay, state = linear_inputs(1, 2, 12, 4, 16, 16, "f32")
+    for scale in (None, 1.0):
+        with pytest.raises(qnn.QnnError):
+            qnn.qnn_linear_attention(q[..., :0], k[..., :0], v, decay, scale=scale)
+        with pytest.raises(qnn.QnnError):
+            qnn.qnn_linear_attention(q, k, v[..., :0], decay, scale=scale)
+
+
 def test_refusals(qnn):
     q, k, v, decay, state = linear_inputs(1, 2, 12, 4, 16, 16, "f32")
     run = qnn.qnn_linear_attention
