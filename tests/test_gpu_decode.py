@@ -4,6 +4,7 @@ import ctypes as C
 import os
 import subprocess
 import sys
+import threading
 
 import numpy as np
 import pytest
@@ -849,6 +850,38 @@ def test_calls_on_streams(qnn):
         for a, b in zip(got, want):
             for x, y in zip(a, b):
                 assert all(torch.equal(p, r) for p, r in zip(x, y))
+
+
+def test_calls_from_threads(qnn):
+    """All calls from four host threads at once, each on a stream of its own."""
+    sets = [calls(qnn, s) for s in range(4)]
+    want = [[f() for f in fs] for fs in sets]
+    streams = [torch.cuda.Stream() for _ in sets]
+    torch.cuda.synchronize()
+    got, errors, start = [[] for _ in sets], [], threading.Barrier(len(sets))
+
+    def work(i):
+        try:
+            torch.cuda.set_device(0)
+            start.wait()
+            for _ in range(5):
+                got[i].append([f(streams[i]) for f in sets[i]])
+        except Exception as e:  # noqa: BLE001
+            errors.append(e)
+
+    threads = [threading.Thread(target=work, args=(i,)) for i in range(len(sets))]
+    for t in threads:
+        t.start()
+    for t in threads:
+        t.join()
+    torch.cuda.synchronize()
+    assert not errors
+    for outs, refs in zip(got, want):
+        assert len(outs) == 5
+        for out in outs:
+            for x, y in zip(out, refs):
+                assert all(torch.equal(p, r) for p, r in zip(x, y))
+    assert qnn.device_status() == qnn.QNN_OK
 
 
 def test_calls_in_graphs(qnn):
