@@ -466,9 +466,11 @@ qnn_status qnn_linear_attention(const qnn_linear_args *args, void *stream);
  *   class comes first; a slot without a candidate has score minus infinity, beam 0 and class eos. scores_out may be
  *   scores if n = K.
  * Scores are formed and compared as two fp32 terms (48 bits) and rounded once for scores_out. The sums of exponentials are of fp32
- * terms, each right to 2^-22: their logarithm is off by 2^-26 or so where many classes count, and by 2^-22 where few do (each row of a
- * call in the same order, so that equal rows have equal sums). Candidates of different beams that are closer may come in either
- * order. Within a beam the n best are those of the logits, in their order as far as the scores differ.
+ * terms: a row's log(sum exp) is off by (10 + 2 D) 2^-24 at most, where D is the mean distance of a class's logit from the row's
+ * largest, by the classes' probabilities (at most their entropy, log V). 2.1 2^-24 is the most that was seen of rows of 97 to 262144
+ * classes, 2^-29 where thousands of random logits count. Each row of a call is summed in the same order, so that equal rows have equal
+ * sums. Candidates of different beams whose scores are closer than two rows' errors may come in either order. Within a beam the n
+ * best are those of the logits, in their order as far as the scores differ.
  * 1 <= K, n <= 128; K V < 2^31; 0 <= eos < V.
  */
 qnn_status qnn_beam_select(const void *logits, int64_t ldl, int dtype, const float *scores, const uint8_t *finished, int64_t B,

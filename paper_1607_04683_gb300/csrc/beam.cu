@@ -69,7 +69,7 @@ __device__ __forceinline__ Two mul(Two a, Two b) {
 }
 // ln 2 in parts of 15 bits (whose product with an exponent is exact), 24, and the rest.
 constexpr float kLn2Head = 0.693145751953125f, kLn2Mid = 1.428606765330187e-06f, kLn2Rest = 5.497923e-14f;
-// exp(x), |x| <= 80, to about 2^-40: x = n ln 2 + 8 r, exp(r) - 1 = r + r^2 / 2 + r^3 / 6 + ... (the first two terms in two fp32 terms
+// exp(x), |x| <= 80, to 2^-34 (2^-39 on average): x = n ln 2 + 8 r, exp(r) - 1 = r + r^2 / 2 + r^3 / 6 + ... (the first two terms in two fp32 terms
 // each; r^3 <= 10^-4), its square taken three times by p -> 2 p + p^2.
 __device__ __forceinline__ Two exp_two(Two x) {
     const float n = rintf(__fmul_rn(x.hi, kLog2e));
@@ -87,7 +87,7 @@ __device__ __forceinline__ Two exp_two(Two x) {
     const float scale = __int_as_float((int)(n + 127.0f) << 23);
     return {__fmul_rn(p.hi, scale), __fmul_rn(p.lo, scale)};
 }
-// log(x), 2^-10 <= x < 2^64, to about 2^-40: a first value in fp32, and the logarithm of what x exp(-value) is off 1.
+// log(x), 2^-10 <= x < 2^64, off by 2^-35 at most (2^-39 on average): a first value in fp32, and the logarithm of what x exp(-value) is off 1.
 __device__ __forceinline__ Two log_two(Two x) {
     const float y = logf(x.hi);
     const Two e = exp_two({-y, 0.0f});
