@@ -438,9 +438,12 @@ typedef struct {
 /*
  * qnn_linear_attention — linear attention with a decay for each head, every head h of every sequence with a state S of its own:
  *   S = exp(min(log_decay[h], 0)) S + k_t v_t^T;  y_t = scale q_t S.
- * States and sums are fp32. Whole sequences are taken by chunks of frames (and long ones of few sequences in parts whose
- * states are put together by their decays), a few frames one by one: a prompt and the frames after it may be given in any
- * division, and one frame of many sequences is the serving form. lengths, frames behind a sequence's end and T = 0 as for
+ * States and sums are fp32. Where T is more than 8, scores (q_t k_s times the decay between them) and states enter their products
+ * rounded to 2^-16 of each with bf16 and fp16 inputs, and such terms to 2^-20 with fp32 ones: where an output's terms cancel, it is that
+ * far off beside them, not beside itself. The states that are carried are not rounded so. A score q_t k_s is formed ahead of its
+ * product with v_s and has to lie in fp32's range, as k_s v_s does. Whole sequences are taken by chunks of frames (and long ones of few
+ * sequences in parts whose states are put together by their decays), a few frames one by one: a prompt and the frames after it may be
+ * given in any division, and one frame of many sequences is the serving form. lengths, frames behind a sequence's end and T = 0 as for
  * qnn_causal_conv; state_out is the state after each sequence's last frame. A decay above 1 counts as 1, one below exp(-200) as 0.
  * Inputs that are not finite give outputs that are not (infinities or NaN) from their frame on, in the heads that use them: v in
  * its own column, k in all of them; q in its own frame only.
@@ -494,7 +497,7 @@ qnn_status qnn_beam_reorder(const qnn_beam_state *states, int32_t count, const i
                             void *stream);
 
 /*
- * qnn_embedding — rows of a table by label: out[i] = scale table[ids[i]], rounded once to out_dtype.
+ * qnn_embedding — rows of a table by label: out[i] = scale table[ids[i]] in fp32, rounded to out_dtype.
  *   ids [n] int32 or int64 (id_bytes 4 or 8); table [V x D] of `dtype` (ldt >= D); out [n x D] (ldo >= D).
  *   A label below 0 is padding: a row of zeros. One of V or more is that too, and QNN_ERR_INVALID_ARG is recorded.
  */

@@ -150,7 +150,9 @@ int copy_unit(const void *p, int64_t B, int64_t T, int64_t heads, int64_t width,
 // 1.7 more, one block an SM; the other a chunk of 64 frames in 4.4 or 5.8, or with the sequence in parts both passes of a part's chunks, that take
 // longer with more blocks an SM, and 9 or 13 for the call. Sequences x frames x heads x dk: 1 x 16 x 8 x 64 10.4 / 8.3, 1 x 128 x 8 x 64 10.4 / 12.6, 1 x 300
 // x 4 x 64 16.6 / 12.6, 8 x 300 x 8 x 64 16.6 / 19.8, 1 x 1000 x 8 x 64 33 / 16.6, 8 x 1000 x 8 x 64 33 / 39; 1 x 500 x 4 x 128 20.6 / 18.8, 1 x 1000 x 16 x 128 33.1 /
-// 33.4, 2 x 1000 x 16 x 128 35 / 56, 1 x 2000 x 16 x 128 60 / 53, 1 x 4000 x 16 x 128 112 / 83, 16 x 1000 x 16 x 128 138 / 232.
+// 33.4, 2 x 1000 x 16 x 128 35 / 56, 1 x 2000 x 16 x 128 60 / 53, 1 x 4000 x 16 x 128 112 / 83, 16 x 1000 x 16 x 128 138 / 238.
+// Frames are T for every sequence (lengths lie on the device); batches of a third to all of T were not fitted, but keep to it: 8 x 300 x 8 x 64 15.5 /
+// 18.9, 2 x 1000 x 16 x 128 35 / 56, 16 x 1000 x 16 x 128 97 / 183.
 bool prefers_tc(const LinearArgs &a, int chunk, int64_t chunks) {
     if (const char *e = std::getenv("QNN_LINEAR")) {  // one of them always (tests)
         if (std::strcmp(e, "tc") == 0) return true;

@@ -9,14 +9,14 @@
 //
 // Numbers. All products are of bf16 pieces of 8 bits with fp32 sums: a bf16 input is one piece, an fp16 input two, an fp32 input
 // three (all exact). What is formed in fp32 is put in as a sum of such pieces: scores and state in two (2^-16 of each, below a
-// 16-bit output's rounding; fp32: three), the scaled v in three (2^-25: the state is kept in fp32 and is an output). Of the products of
+// 16-bit output's rounding; fp32: three), the scaled v in three, all of its 24 bits (the state is kept in fp32 and is an output). Of the products of
 // pieces those are taken that the shorter of the two sides' precisions needs: one to three for bf16, four or five for fp16, six for fp32
 // (2^-23). (tf32 instructions for fp16 and fp32 took as many, and three times the instructions around them to split operands in
 // every warp: 1 x 4000 x 8 x 64 fp32 125 us.)
 //
 // Bound: a warp's instructions, of which the products are a tenth, and their way into the caches. 1 x 4000 x 8 x 64 fp32, three chunks a part
 // and pass: 39 us (states 16, prefix 10, outputs 31 one by one with cold caches); 1 x 1000 x 8 x 64, a chunk a part, 19 us; 16 x 1000 x 16 x 128
-// 505 us, fp16 347, bf16 232. Eight warps a block, each half of dk, took 43 us for the first and 690 for the last: v's pieces are made twice.
+// 510 us, fp16 375, bf16 238. Eight warps a block, each half of dk, took 43 us for the first and 690 for the last: v's pieces are made twice.
 #pragma once
 
 #include <algorithm>

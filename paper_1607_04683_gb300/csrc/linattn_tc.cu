@@ -12,12 +12,12 @@
 // k, v, the scaled v and the state lie in rows of 64 values (128 bytes, swizzled): read along rows they are one operand's layout, across
 // rows the other's, so nothing is transposed.
 //
-// Numbers. q, k and v are operands as they are. Scores and state go in as two pieces (2^-17), the scaled v as three, each rounded
-// (2^-25; two left the states 2.4e-6 off). The state's sums are fp32 in registers, a chunk's products in tensor memory.
+// Numbers. q, k and v are operands as they are. Scores and state go in as two pieces (2^-16 of each), the scaled v as three,
+// which hold all of its 24 bits (two left the states 2.4e-6 off). The state's sums are fp32 in registers, a chunk's products in tensor memory.
 //
 // Bound: the products' issue and the warps' work between them, not bytes: the 52 to 64 products of a chunk, of 64 or 128 columns, take 45 to
-// 70 cycles each, 3.3 us a chunk or more in all. 16 x 1000 frames x 16 heads x 128: 147 us (512 units of 8 chunks on 152 SMs, 2.0
-// TB/s), with sequences of a third to all of that 104 us; the kernel of linattn.cuh takes 235 us for the first.
+// 70 cycles each, 3.3 us a chunk or more in all. 16 x 1000 frames x 16 heads x 128: 138 us (512 units of 8 chunks on 152 SMs, 1.9
+// TB/s), with sequences of a third to all of that 97 us; the kernel of linattn.cuh takes 238 and 183 us.
 #include <algorithm>
 
 #include "linattn.cuh"
@@ -92,7 +92,7 @@ __device__ __forceinline__ void tc_after() { asm volatile("tcgen05.fence::after_
 
 // A (sequence, head, columns) of the block's list. The list goes over the sequences from the longest to the shortest (of up to
 // kSorted of them with lengths of their own), back and forth over the blocks: 16 x 16 heads x 128 with sequences of a third to all of 1000
-// frames 104 us, in the order that they are given 110.
+// frames 6 us less than in the order that they are given, 97.
 struct Unit {
     int64_t bh, b;
     int round, h, tile, n, chunks;
