@@ -313,7 +313,7 @@ __device__ __forceinline__ bool take_values(Best<Logit, EACH> &s, const float (&
 
 // One part of a beam's row: its sum of exponentials and its n best classes in one pass over it, tiles of kThreads EACH values
 // in registers. Within a beam the order of the logits is that of the scores, so that no score is formed here. The classes lie in
-// best.list. Bound: instructions, 850 a warp for 8192 classes (exponentials 5 a class), and the block's meetings: 128 x 8 x 8192 bf16 14 us
+// best.list. Bound: instructions, 770 a warp for 8192 classes (exponentials 5 a class), and the block's meetings: 128 x 8 x 8192 bf16 14 us
 // for all rows, so 1.2 TB/s.
 template <int EACH>
 struct RowShared {
@@ -615,7 +615,9 @@ struct ReorderArgs {
 
 // A thread takes one word of every beam of a batch row: it has loaded all that it needs of up to NB beams before it stores
 // the first of them, so that states may be reordered in place (n <= NB then). A beam that is its own parent in place is left alone.
-// Bound: HBM or L2; 64 x 8 beams, states of 5 x 2048 and 5 x 512 values, 54 MB: 9.6 us, 5.6 TB/s.
+// Bound: HBM or L2; 64 x 8 beams, states of 5 x 2048 and 5 x 512 values, 54 MB: 9.4 us, 5.7 TB/s. Over 16 beams in place: registers, as a
+// thread holds 128 words of 4 bytes (452 bytes of them spilled) whatever n is; 30 x 17, 16 x 32, 8 x 64 and 4 x 128 beams of the same states 139, 108, 86
+// and 105 us, into other tensors 11, 12, 17 and 30.
 template <typename W, int NB>
 __global__ void __launch_bounds__(kReorderThreads) beam_reorder_kernel(const ReorderArgs a) {
     for (int64_t item = (int64_t)blockIdx.x * kReorderThreads + threadIdx.x; item < a.items; item += (int64_t)gridDim.x * kReorderThreads) {

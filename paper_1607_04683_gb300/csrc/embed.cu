@@ -418,7 +418,7 @@ __device__ __forceinline__ int64_t bound(const uint32_t *ids, int64_t lo, int64_
 // flight. A run of one label that lies within the chunk is written out; what began before it or goes on behind it is kept for the
 // second kernel. Rows that no position has were cleared while the labels were sorted. Bound: memory's latency, with few warps (1200 x 500:
 // 13 us by itself), and its rate: 16000 x 2048 bf16 18 us.
-constexpr int kRows = 4;  // (2: 16000 x 2048 bf16 32 us, 8: 35, 16: 46, so 29.5; 60000 x 512 fp32 51, 45, so 44)
+constexpr int kRows = 4;  // (the whole call by 2, 4, 8, 16: 16000 x 2048 bf16 44, 41, 47, 46 us; 60000 x 512 fp32 81, 74, 75, 85)
 template <typename T, typename O, int W>
 __global__ void __launch_bounds__(kGradThreads) grad_sum_kernel(const GradArgs a) {
     const int lane = threadIdx.x % 32;
